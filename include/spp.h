@@ -414,6 +414,218 @@ spp_status spp_gate_batch_noalloc(int32_t n, const spp_ready_t* ready, const flo
                                   const uint32_t* const* bitmaps, void* stream,
                                   int32_t* tokens_out, spp_gate_outcome* outcomes);
 
+/* ---- paged caches ------------------------------------------------------------------ */
+
+/* A pool of pages: the cells of many sequences in one caller-owned buffer, `page_cells`
+ * cells of every layer to a page.  It serves a fall-through (Sec. 3.5) that decodes several
+ * continuations of one state: a session's cells are imported once, forks share their pages,
+ * and only the page a fork writes into becomes its own.  Sequences are numbered 0 ..
+ * max_seqs - 1; a number is taken by spp_seq_create or spp_seq_fork and given back by
+ * spp_seq_free.
+ *
+ * The bookkeeping (tables, references, free pages) is on the host and done when a call
+ * returns.  The device work of a pool's calls -- copies and decode steps -- is enqueued on
+ * the call's stream and ordered after that of the pool's earlier calls on whatever stream,
+ * so a page freed and taken again is not written while earlier work reads it.  A pool's
+ * calls may come from several threads: they are serialized.  Work that a caller enqueues on
+ * the pages by itself (spp_paged_attention too) is the caller's to order. */
+typedef struct spp_pool_s* spp_pool_t;
+
+typedef struct {
+  int32_t n_layers, n_kv_heads, head_dim;  /* of the models whose cells it holds; head_dim
+                                              64 or 128                                  */
+  int32_t dtype;            /* spp_dtype of the cells                                     */
+  int32_t page_cells;       /* cells per page: 16, 32, 64, 128 or 256                     */
+  int32_t n_pages;          /* pages in the caller's buffer, >= 1                         */
+  int32_t max_seqs;         /* most sequences alive at once, 1..65536                     */
+} spp_pool_config;
+
+/* Where cell (layer, head, cell, dim) of a page lives: byte offset from the buffer's start
+ * of the K element = page*page_stride + layer*layer_stride + (head*k_stride[0] +
+ * cell*k_stride[1] + dim*k_stride[2]) * elem_bytes; of the V element = page*page_stride +
+ * layer*layer_stride + v_offset + (head*v_stride[0] + cell*v_stride[1] +
+ * dim*v_stride[2]) * elem_bytes.  (K is [head][cell][dim], V [head][dim][cell].) */
+typedef struct {
+  int64_t page_stride, layer_stride, v_offset;  /* bytes    */
+  int64_t k_stride[3], v_stride[3];             /* elements */
+  int32_t elem_bytes;
+} spp_page_layout;
+
+typedef struct {
+  int32_t n_pages, used_pages;   /* used: referred to by at least one sequence            */
+  int32_t shared_pages;          /* referred to by more than one                          */
+  int32_t n_seqs, max_seqs;
+} spp_pool_info_t;
+
+typedef struct {
+  int32_t n_cells;               /* the sequence's length                                 */
+  int32_t n_pages;               /* pages of its table (reserved ones among them)         */
+  int32_t decoded;               /* 1 while spp_seq_summaries has a summary of it         */
+} spp_seq_info_t;
+
+/* Bytes of the buffer a pool needs (0 for a bad configuration), and its layout. */
+size_t spp_pool_bytes(const spp_pool_config* cfg);
+spp_status spp_pool_page_layout(const spp_pool_config* cfg, spp_page_layout* out);
+
+/* A pool over a caller-owned device buffer of at least spp_pool_bytes() bytes, 16-byte
+ * aligned, on the current device.  No page is touched.  SPP_E_INVALID_ARG on a null pointer,
+ * a bad configuration, a short or misaligned buffer; SPP_E_NOMEM if the pool's device record
+ * (32 bytes a sequence) cannot be allocated. */
+spp_status spp_pool_create(const spp_pool_config* cfg, void* pages_dev, size_t bytes,
+                           spp_pool_t* out);
+/* Waits for the pool's device work, then releases it (no call may use it meanwhile). */
+spp_status spp_pool_destroy(spp_pool_t pool);
+spp_status spp_pool_info(spp_pool_t pool, spp_pool_info_t* out);
+
+/* A sequence of n_cells cells with pages of its own, whose contents the caller has written
+ * or will write (0: an empty one).  Pages are taken lowest number first, here and below.
+ * SPP_E_CAPACITY when the pages or the sequence numbers run out (then nothing changes, as
+ * for every call below). */
+spp_status spp_seq_create(spp_pool_t pool, int32_t n_cells, int32_t* seq_out);
+/* Gives up a sequence: its pages lose a reference, those without any are free. */
+spp_status spp_seq_free(spp_pool_t pool, int32_t seq);
+spp_status spp_seq_info(spp_pool_t pool, int32_t seq, spp_seq_info_t* out);
+/* The sequence's page numbers in order (host array of `cap` entries, at least its n_pages;
+ * *n_out receives how many).  With table NULL only *n_out is written. */
+spp_status spp_seq_table(spp_pool_t pool, int32_t seq, int32_t* table, int32_t cap,
+                         int32_t* n_out);
+
+/* `n` new sequences with the cells of `src`: they share its pages (those that hold cells),
+ * nothing is copied yet.  seqs_out: host array of n.  SPP_E_CAPACITY when the sequence
+ * numbers run out. */
+spp_status spp_seq_fork(spp_pool_t pool, int32_t src, int32_t n, int32_t* seqs_out);
+
+/* Makes the next `cells` cells of each of n distinct sequences writable: the page their
+ * last cell shares with another sequence is copied to a page of their own (one launch for
+ * all), and pages are added to their tables.  Lengths do not change.  spp_decode_batch does
+ * this for its one cell; a caller that writes cells itself reserves, writes and then calls
+ * spp_seq_commit.  Asynchronous on `stream`.  SPP_E_CAPACITY when the pages run out. */
+spp_status spp_seq_reserve(spp_pool_t pool, int32_t n, const int32_t* seqs, int32_t cells,
+                           void* stream);
+/* Declares the next `cells` reserved cells written: n_cells <- n_cells + cells.
+ * SPP_E_STATE if they were not reserved. */
+spp_status spp_seq_commit(spp_pool_t pool, int32_t seq, int32_t cells);
+/* Discards cells: n_cells <- min(n_cells, n), and gives up the pages past them. */
+spp_status spp_seq_truncate(spp_pool_t pool, int32_t seq, int32_t n);
+
+/* The sequence becomes a copy of the session's committed cells (its former cells are given
+ * up): every layer's cells [0, n_s) into pages of its own.  The session is only read.  Asynchronous
+ * on `stream`, ordered after the device work of the session's model as well.
+ * SPP_E_INVALID_ARG unless the session's model has the pool's layers, kv heads, head_dim and
+ * dtype and lives on its device; SPP_E_CAPACITY when the pages run out. */
+spp_status spp_seq_import(spp_pool_t pool, int32_t seq, spp_session_t session, void* stream);
+/* The session's committed state becomes a copy of the sequence: its cells [0, n_cells) of
+ * every layer are overwritten, n_s <- n_cells, its entry is dropped and its ready
+ * distribution invalidated in the same call (Sec. 3.6).  Errors as for spp_seq_import;
+ * SPP_E_CAPACITY when the cells exceed the session's capacity. */
+spp_status spp_seq_export(spp_pool_t pool, int32_t seq, spp_session_t session, void* stream);
+
+/* Moves the used pages together: with u pages in use, those numbered u and above move, in
+ * ascending order, to the free ones below u, in ascending order, and the tables follow.
+ * Afterwards pages [0, u) are in use and the buffer past them is free.  *n_moved (nullable):
+ * the pages copied.  Asynchronous on `stream`. */
+spp_status spp_pool_compact(spp_pool_t pool, void* stream, int32_t* n_moved);
+
+/* One decode step of n distinct sequences at once (the decode of Eq. (fallthrough), batched):
+ * tokens[i] (host array) is appended to seqs[i] -- its cells are written at n_cells of every
+ * layer, into a page of the sequence's own (as spp_seq_reserve) -- and the fp32 logits after
+ * it go to dists[i] (host array of device pointers, fp32[vocab] each); n_cells grows by one.
+ * Every weight is read once for up to the model's max_sessions (and max_tokens) sequences;
+ * more take further passes.  The model has the pool's layers, kv heads, head_dim and dtype
+ * and lives on its device.  Asynchronous on `stream`.  SPP_E_INVALID_ARG for a null pointer,
+ * n < 1, a sequence that does not exist or is listed twice, a token outside [0, vocab);
+ * SPP_E_CAPACITY when the pages run out or a sequence is SPP_MAX_CAPACITY cells long (then
+ * nothing ran). */
+spp_status spp_decode_batch(spp_pool_t pool, spp_model_t model, int32_t n, const int32_t* seqs,
+                            const int32_t* tokens, float* const* dists, void* stream);
+/* The reductions over the logits that the last spp_decode_batch of each sequence wrote (as
+ * spp_ready_summary; position = n_cells after it).  Blocks until the pool's device work has
+ * finished.  SPP_E_STATE for a sequence that has changed since, or was never decoded. */
+spp_status spp_seq_summaries(spp_pool_t pool, int32_t n, const int32_t* seqs, spp_summary* out);
+
+/* Attention of one new token per sequence over paged cells, the attention of
+ * spp_decode_batch: for every sequence i and query head h (which reads kv head
+ * h / (n_q_heads / n_kv_heads)),
+ *   out = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q.k_j),
+ * over the cells j < lengths[i] of layer `layer` whose page is listed: cell j is in page
+ * table[i][j / page_cells].  A table entry outside [0, n_pages) takes its cells out (a page
+ * given up from the middle); lengths beyond max_pages*page_cells are cut to it, negative
+ * ones are zero.  A sequence with no cell left gets zeros.  What lies in a page behind a sequence's
+ * last cell, or in a page that is not listed, has no influence, NaN included.
+ * The products of bf16 cells run on bf16 matrix cores with q (unless it is bf16) and p in
+ * two bf16 parts and fp32 sums: about 16 significant bits of both. */
+typedef struct {
+  spp_pool_t pool;
+  int32_t layer;
+  int32_t n_seqs;            /* 0..65535 (0: nothing is done)                             */
+  int32_t n_q_heads;         /* a multiple of the pool's n_kv_heads                       */
+  int32_t io_dtype;          /* spp_dtype of q and out                                    */
+  const void* q;             /* device, [n_seqs] rows of [n_q_heads][head_dim]            */
+  int64_t q_stride;          /* elements between rows, a multiple of 8; q 16-byte aligned */
+  const int32_t* table;      /* device, [n_seqs] rows of max_pages page numbers           */
+  int64_t table_stride;      /* entries between rows, >= max_pages                        */
+  int32_t max_pages;         /* >= 1; max_pages*page_cells < 2^31                         */
+  const int32_t* lengths;    /* device, [n_seqs]                                          */
+  float scale;               /* finite; 0 stands for 1 / sqrt(head_dim)                   */
+  void* out;                 /* device, rows as q's                                       */
+  int64_t out_stride;        /* as q_stride                                               */
+} spp_paged_attn;
+/* Bytes of workspace the call needs (0 for bad arguments, or none needed; it depends on
+ * n_seqs, n_q_heads, max_pages and the pool). */
+size_t spp_paged_attention_work_bytes(const spp_paged_attn* a);
+/* Only launches kernels (one or two) on `stream`: it may be captured into a graph, whose
+ * replays read the table and the lengths as they are then.  The workspace (device, 16-byte
+ * aligned) is written before it is read; two calls that may run at once need two.
+ * SPP_E_INVALID_ARG for a null pointer or a value outside what the fields say. */
+spp_status spp_paged_attention(const spp_paged_attn* a, void* work, size_t work_bytes,
+                               void* stream);
+
+/* ---- adjusted logits ---------------------------------------------------------------- */
+
+/* One row of spp_adjust_logits.  For every token v:
+ *   y = x                                          the logit src[v]
+ *   y = y > 0 ? y / repetition : y * repetition    if v occurs in tokens
+ *   y = y - frequency * c                          c: occurrences of v in tokens past the
+ *   y = y - (c > 0 ? presence : 0)                    first n_prompt
+ *   y = y + bias[i]                                if bias_tokens[i] = v (the last such i)
+ *   y = fill                                       if the allowed set lacks v
+ * every operation in fp32 with its own rounding.  Entries of tokens and bias_tokens
+ * outside [0, vocab) are skipped. */
+typedef struct {
+  const float* src;             /* device, [vocab]                                        */
+  float* dst;                   /* device, [vocab]; may be src                            */
+  const int32_t* tokens;        /* device, [n_tokens]: the prompt, then the answer so far */
+  const int32_t* bias_tokens;   /* device, [n_bias]                                       */
+  const float* bias;            /* device, [n_bias]                                       */
+  const uint32_t* allowed;      /* device bitmap as the gate's fast-answer set; NULL: all */
+  int32_t n_tokens, n_prompt;   /* 0 <= n_prompt <= n_tokens                              */
+  int32_t n_bias;
+  float repetition;             /* finite, > 0; 1 changes nothing                         */
+  float frequency, presence;    /* finite; 0 changes nothing                              */
+  float fill;                   /* not NaN.  The gate never serves a distribution with an
+                                   infinite value: fill with a finite one, such as
+                                   -FLT_MAX, to gate the adjusted logits                  */
+} spp_adjust;
+
+/* Bytes of workspace spp_adjust_logits needs for n rows with summaries. */
+size_t spp_adjust_logits_work_bytes(int32_t n, int32_t vocab);
+/* Penalties for repeated tokens, biases and an allowed set (a grammar's next tokens) on n
+ * rows of logits -- those of a resume or a decode step -- with the reductions a greedy step
+ * reads.  rows: host array, read during the call.  Rows do not overlap, except a dst with its
+ * own src; every pointer is on the current device.  summaries (nullable): device array of n
+ * spp_summary: argmax (lowest index on ties), top1, top2, gap and lse over the adjusted
+ * logits of the ALLOWED tokens, position 0, flags bit 0 if one of these is NaN or +-inf (lse
+ * is then NaN; a NaN is never the argmax), bit 3 if no token is allowed (gap and lse are then
+ * NaN).  Where no token qualifies argmax is -1 and top1 -inf; with one, top2 is -inf.  The
+ * workspace (device, 16-byte aligned, needed only with summaries) is written before it is
+ * read; two calls that may run at once need two.  Only launches kernels on `stream`: it may
+ * be captured into a graph (the fields above are fixed then, what the pointers name is read
+ * at each replay).  SPP_E_INVALID_ARG for n < 0, vocab outside [1, 2^24], a null pointer, or
+ * a value outside what the fields say (then nothing ran). */
+spp_status spp_adjust_logits(int32_t n, int32_t vocab, const spp_adjust* rows,
+                             spp_summary* summaries, void* work, size_t work_bytes,
+                             void* stream);
+
 /* ---- gate calibration ------------------------------------------------------------- */
 
 /* One threshold of the gate's risk-coverage curve (Sec. 2.4, Eqs. (coverage), (risk)):

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import math
 import os
 from typing import Dict, List, Optional, Sequence, Tuple
 
@@ -90,6 +91,48 @@ class spp_gate_point(ctypes.Structure):
                 ("risk_lo", ctypes.c_double), ("risk_hi", ctypes.c_double)]
 
 
+class spp_pool_config(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("page_cells", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_seqs", ctypes.c_int32)]
+
+
+class spp_page_layout(ctypes.Structure):
+    _fields_ = [("page_stride", ctypes.c_int64), ("layer_stride", ctypes.c_int64),
+                ("v_offset", ctypes.c_int64), ("k_stride", ctypes.c_int64 * 3),
+                ("v_stride", ctypes.c_int64 * 3), ("elem_bytes", ctypes.c_int32)]
+
+
+class spp_pool_info(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("used_pages", ctypes.c_int32),
+                ("shared_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
+                ("max_seqs", ctypes.c_int32)]
+
+
+class spp_seq_info(ctypes.Structure):
+    _fields_ = [("n_cells", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("decoded", ctypes.c_int32)]
+
+
+class spp_paged_attn(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("layer", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
+                ("n_q_heads", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("max_pages", ctypes.c_int32),
+                ("lengths", ctypes.c_void_p), ("scale", ctypes.c_float), ("out", ctypes.c_void_p),
+                ("out_stride", ctypes.c_int64)]
+
+
+class spp_adjust(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("tokens", ctypes.c_void_p),
+                ("bias_tokens", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("allowed", ctypes.c_void_p), ("n_tokens", ctypes.c_int32),
+                ("n_prompt", ctypes.c_int32), ("n_bias", ctypes.c_int32),
+                ("repetition", ctypes.c_float), ("frequency", ctypes.c_float),
+                ("presence", ctypes.c_float), ("fill", ctypes.c_float)]
+
+
 EXPORTS = ["spp_model_create", "spp_model_destroy", "spp_session_kv_bytes", "spp_session_kv_layout",
            "spp_session_create", "spp_session_destroy", "spp_session_id", "spp_session_restore",
            "spp_kv_append_delta", "spp_preposition", "spp_ready_summary", "spp_gate",
@@ -98,7 +141,13 @@ EXPORTS = ["spp_model_create", "spp_model_destroy", "spp_session_kv_bytes", "spp
            "spp_gate_batch", "spp_last_error", "spp_profile_preposition", "spp_kernel_class_name",
            "spp_copy_reference", "spp_pack_weight", "spp_pack_weight_mxfp4", "spp_resume",
            "spp_shift", "spp_gate_calibrate", "spp_preposition_idle", "spp_gate_batch_noalloc",
-           "spp_profile_preposition_batch"]
+           "spp_profile_preposition_batch", "spp_pool_bytes", "spp_pool_page_layout",
+           "spp_pool_create", "spp_pool_destroy", "spp_pool_info", "spp_pool_compact",
+           "spp_seq_create", "spp_seq_free", "spp_seq_info", "spp_seq_table", "spp_seq_fork",
+           "spp_seq_reserve", "spp_seq_commit", "spp_seq_truncate", "spp_seq_import",
+           "spp_seq_export", "spp_seq_summaries", "spp_decode_batch",
+           "spp_paged_attention_work_bytes", "spp_paged_attention",
+           "spp_adjust_logits_work_bytes", "spp_adjust_logits"]
 
 _lib = None
 
@@ -146,6 +195,28 @@ def lib() -> ctypes.CDLL:
         "spp_copy_reference": (st, [P, P, sz, P]),
         "spp_pack_weight": (st, [ctypes.POINTER(spp_model_config), i32, P, P, P]),
         "spp_pack_weight_mxfp4": (st, [ctypes.POINTER(spp_model_config), i32, P, P, P, P, P]),
+        "spp_pool_bytes": (sz, [ctypes.POINTER(spp_pool_config)]),
+        "spp_pool_page_layout": (st, [ctypes.POINTER(spp_pool_config), ctypes.POINTER(spp_page_layout)]),
+        "spp_pool_create": (st, [ctypes.POINTER(spp_pool_config), P, sz, ctypes.POINTER(P)]),
+        "spp_pool_destroy": (st, [P]),
+        "spp_pool_info": (st, [P, ctypes.POINTER(spp_pool_info)]),
+        "spp_pool_compact": (st, [P, P, ctypes.POINTER(i32)]),
+        "spp_seq_create": (st, [P, i32, ctypes.POINTER(i32)]),
+        "spp_seq_free": (st, [P, i32]),
+        "spp_seq_info": (st, [P, i32, ctypes.POINTER(spp_seq_info)]),
+        "spp_seq_table": (st, [P, i32, P, i32, ctypes.POINTER(i32)]),
+        "spp_seq_fork": (st, [P, i32, i32, P]),
+        "spp_seq_reserve": (st, [P, i32, P, i32, P]),
+        "spp_seq_commit": (st, [P, i32, i32]),
+        "spp_seq_truncate": (st, [P, i32, i32]),
+        "spp_seq_import": (st, [P, i32, P, P]),
+        "spp_seq_export": (st, [P, i32, P, P]),
+        "spp_seq_summaries": (st, [P, i32, P, ctypes.POINTER(spp_summary)]),
+        "spp_decode_batch": (st, [P, P, i32, P, P, P, P]),
+        "spp_paged_attention_work_bytes": (sz, [ctypes.POINTER(spp_paged_attn)]),
+        "spp_paged_attention": (st, [ctypes.POINTER(spp_paged_attn), P, sz, P]),
+        "spp_adjust_logits_work_bytes": (sz, [i32, i32]),
+        "spp_adjust_logits": (st, [i32, i32, ctypes.POINTER(spp_adjust), P, P, sz, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -507,6 +578,250 @@ def gate_batch(readies: Sequence[Ready], taus: Sequence[float], bitmaps, stream=
     name = "spp_gate_batch_noalloc" if noalloc else "spp_gate_batch"
     check(getattr(lib(), name)(n, rs, ts, bms, ctypes.c_void_p(_stream(stream)), toks, outs), name)
     return [(outs[i], toks[i]) for i in range(n)]
+
+
+class PagePool:
+    """Pages of a paged cache (spp_pool_*): sequences are numbers, the pages a device buffer
+    (`pages`: a contiguous tensor of at least the pool's bytes; else allocated here)."""
+
+    def __init__(self, n_layers: int, n_kv_heads: int, head_dim: int, bf16: bool, page_cells: int,
+                 n_pages: int, max_seqs: int = 64, pages=None, device="cuda"):
+        self.cfg = spp_pool_config(n_layers, n_kv_heads, head_dim,
+                                   SPP_DTYPE_BF16 if bf16 else SPP_DTYPE_F32, page_cells, n_pages,
+                                   max_seqs)
+        self.handle = None
+        if pages is None:
+            import torch
+            nbytes = lib().spp_pool_bytes(ctypes.byref(self.cfg))
+            pages = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+        self.pages = pages
+        if not pages.is_contiguous():
+            raise ValueError("pages must be a contiguous tensor")
+        h = ctypes.c_void_p()
+        check(lib().spp_pool_create(ctypes.byref(self.cfg), ctypes.c_void_p(_ptr(pages)),
+                                    pages.numel() * pages.element_size(), ctypes.byref(h)),
+              "spp_pool_create")
+        self.handle = h
+
+    def close(self) -> None:
+        if self.handle:
+            lib().spp_pool_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def page_layout(self) -> spp_page_layout:
+        out = spp_page_layout()
+        check(lib().spp_pool_page_layout(ctypes.byref(self.cfg), ctypes.byref(out)),
+              "spp_pool_page_layout")
+        return out
+
+    def info(self) -> spp_pool_info:
+        out = spp_pool_info()
+        check(lib().spp_pool_info(self.handle, ctypes.byref(out)), "spp_pool_info")
+        return out
+
+    def create(self, n_cells: int = 0) -> int:
+        """A sequence of n_cells cells whose contents the caller has written or will write."""
+        q = ctypes.c_int32()
+        check(lib().spp_seq_create(self.handle, n_cells, ctypes.byref(q)), "spp_seq_create")
+        return q.value
+
+    def free(self, seq: int) -> None:
+        check(lib().spp_seq_free(self.handle, seq), "spp_seq_free")
+
+    def seq_info(self, seq: int) -> spp_seq_info:
+        out = spp_seq_info()
+        check(lib().spp_seq_info(self.handle, seq, ctypes.byref(out)), "spp_seq_info")
+        return out
+
+    def table(self, seq: int) -> List[int]:
+        """The sequence's page numbers."""
+        n = ctypes.c_int32()
+        check(lib().spp_seq_table(self.handle, seq, None, 0, ctypes.byref(n)), "spp_seq_table")
+        t = (ctypes.c_int32 * max(1, n.value))()
+        check(lib().spp_seq_table(self.handle, seq, t, n.value, ctypes.byref(n)), "spp_seq_table")
+        return t[:n.value]
+
+    def fork(self, seq: int, n: int = 1) -> List[int]:
+        """n sequences that share the pages of `seq` until they are written (spp_seq_fork)."""
+        out = (ctypes.c_int32 * max(1, n))()
+        check(lib().spp_seq_fork(self.handle, seq, n, out), "spp_seq_fork")
+        return out[:n]
+
+    def reserve(self, seqs: Sequence[int], cells: int = 1, stream=None) -> None:
+        """Makes the next `cells` cells of the sequences writable (spp_seq_reserve)."""
+        arr, n = _host_i32(seqs)
+        check(lib().spp_seq_reserve(self.handle, n, arr, cells, ctypes.c_void_p(_stream(stream))),
+              "spp_seq_reserve")
+
+    def commit(self, seq: int, cells: int) -> None:
+        check(lib().spp_seq_commit(self.handle, seq, cells), "spp_seq_commit")
+
+    def truncate(self, seq: int, n: int) -> None:
+        check(lib().spp_seq_truncate(self.handle, seq, n), "spp_seq_truncate")
+
+    def import_session(self, seq: int, session: Session, stream=None) -> None:
+        """The sequence becomes a copy of the session's committed cells (spp_seq_import)."""
+        check(lib().spp_seq_import(self.handle, seq, session.handle, ctypes.c_void_p(_stream(stream))),
+              "spp_seq_import")
+
+    def export_session(self, seq: int, session: Session, stream=None) -> None:
+        """The session's committed state becomes a copy of the sequence (spp_seq_export)."""
+        check(lib().spp_seq_export(self.handle, seq, session.handle, ctypes.c_void_p(_stream(stream))),
+              "spp_seq_export")
+
+    def compact(self, stream=None) -> int:
+        """Moves the used pages to the buffer's start (spp_pool_compact); how many moved."""
+        n = ctypes.c_int32()
+        check(lib().spp_pool_compact(self.handle, ctypes.c_void_p(_stream(stream)), ctypes.byref(n)),
+              "spp_pool_compact")
+        return n.value
+
+    def summaries(self, seqs: Sequence[int]) -> List[spp_summary]:
+        """The reductions over the logits of the sequences' last decode step."""
+        arr, n = _host_i32(seqs)
+        out = (spp_summary * max(1, n))()
+        check(lib().spp_seq_summaries(self.handle, n, arr, out), "spp_seq_summaries")
+        return list(out[:n])
+
+
+def decode_batch(pool: PagePool, model: Model, seqs: Sequence[int], tokens: Sequence[int], dists,
+                 stream=None) -> None:
+    """One decode step: tokens[i] appended to seqs[i], its logits to dists[i] (spp_decode_batch)."""
+    arr, n = _host_i32(seqs)
+    toks, nt = _host_i32(tokens)
+    if nt != n or len(dists) != n:
+        raise ValueError("sequences, tokens and dists differ in number")
+    ptrs = (ctypes.c_void_p * max(1, n))(*[_ptr(d) for d in dists])
+    check(lib().spp_decode_batch(pool.handle, model.handle, n, arr, toks, ptrs,
+                                 ctypes.c_void_p(_stream(stream))), "spp_decode_batch")
+
+
+def _row_stride(t, what: str) -> int:
+    """Elements between the rows of a [n][heads][head_dim] tensor whose rows are contiguous."""
+    if t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise ValueError(f"{what}: [n][heads][head_dim] with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+class PagedAttention:
+    """spp_paged_attention over fixed tables: table [n][max_pages] and lengths [n] are int32
+    device tensors (their values may change between calls), the workspace is held here.  Each
+    call(q, out) is attention of one new token per sequence."""
+
+    def __init__(self, pool: PagePool, layer: int, n_q_heads: int, table, lengths,
+                 io_bf16: bool = True, scale: float = 0.0):
+        import torch
+        if table.dtype != torch.int32 or lengths.dtype != torch.int32 or table.dim() != 2 or \
+                lengths.shape != table.shape[:1] or not lengths.is_contiguous() or \
+                (table.numel() and table.stride(1) != 1):
+            raise ValueError("table [n][max_pages] and lengths [n]: int32, contiguous rows")
+        n, width = table.shape
+        self._keep = (pool, table, lengths)
+        self._dtype = torch.bfloat16 if io_bf16 else torch.float32
+        self._shape = (n, n_q_heads, pool.cfg.head_dim)
+        row = n_q_heads * pool.cfg.head_dim
+        dummy = pool.pages.data_ptr()
+        self._a = spp_paged_attn(pool.handle.value, layer, n, n_q_heads,
+                                 SPP_DTYPE_BF16 if io_bf16 else SPP_DTYPE_F32, dummy, row,
+                                 table.data_ptr(), table.stride(0) if n > 1 else width, width,
+                                 lengths.data_ptr(), scale, dummy, row)
+        nbytes = lib().spp_paged_attention_work_bytes(ctypes.byref(self._a))
+        self._work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=table.device)
+        self._ref = ctypes.byref(self._a)
+        self._wp = ctypes.c_void_p(self._work.data_ptr())
+        self._nb = self._work.numel()
+
+    def __call__(self, q, out, stream=None):
+        for t, what in ((q, "q"), (out, "out")):
+            if t.dtype != self._dtype or tuple(t.shape) != self._shape:
+                raise ValueError(f"{what}: {self._dtype} of shape {self._shape}")
+        a = self._a
+        a.q, a.q_stride = q.data_ptr(), _row_stride(q, "q")
+        a.out, a.out_stride = out.data_ptr(), _row_stride(out, "out")
+        rc = lib().spp_paged_attention(self._ref, self._wp, self._nb, ctypes.c_void_p(_stream(stream)))
+        if rc < 0:
+            raise SppError(rc, "spp_paged_attention")
+        return out
+
+
+@dataclasses.dataclass
+class AdjustRow:
+    """One row of adjusted logits (spp_adjust): src and dst fp32 device tensors of the
+    vocabulary, tokens / bias_tokens int32, bias fp32, allowed a bitmap of int32 words."""
+    src: object
+    dst: object
+    tokens: object = None
+    n_tokens: Optional[int] = None  # default: all of tokens
+    n_prompt: int = 0
+    repetition: float = 1.0
+    frequency: float = 0.0
+    presence: float = 0.0
+    bias_tokens: object = None
+    bias: object = None
+    allowed: object = None
+    fill: float = -math.inf
+
+
+class AdjustSummaries:
+    """The reductions of adjusted rows, device tensors [n]."""
+
+    def __init__(self, words):
+        import torch
+        f = words.view(torch.float32)
+        self.argmax, self.flags = words[:, 0], words[:, 6]
+        self.top1, self.top2, self.gap, self.lse = f[:, 1], f[:, 2], f[:, 3], f[:, 4]
+
+
+class LogitsAdjust:
+    """spp_adjust_logits with its rows marshalled once: each call() adjusts them and returns
+    their AdjustSummaries (None with summaries=False), which the next call overwrites."""
+
+    def __init__(self, vocab: int, rows: Sequence[AdjustRow], summaries: bool = True):
+        import torch
+        n = len(rows)
+        self.n, self._vocab, self._keep = n, vocab, list(rows)
+        words = (vocab + 31) // 32
+        self._rows = (spp_adjust * max(1, n))()
+        for i, r in enumerate(rows):
+            for t, what, dt, least in ((r.src, "src", torch.float32, vocab), (r.dst, "dst", torch.float32, vocab),
+                                       (r.tokens, "tokens", torch.int32, r.n_tokens or 0),
+                                       (r.bias_tokens, "bias_tokens", torch.int32, 0),
+                                       (r.bias, "bias", torch.float32, 0),
+                                       (r.allowed, "allowed", torch.int32, words)):
+                if t is None and what not in ("src", "dst"):
+                    continue
+                if t.dtype != dt or t.dim() != 1 or t.numel() < least or (t.numel() > 1 and t.stride(0) != 1):
+                    raise ValueError(f"row {i}: {what} is a contiguous {dt} vector of at least {least}")
+            nb = 0 if r.bias_tokens is None else r.bias_tokens.numel()
+            if nb != (0 if r.bias is None else r.bias.numel()):
+                raise ValueError(f"row {i}: bias and bias_tokens differ in length")
+            nt = (0 if r.tokens is None else r.tokens.numel()) if r.n_tokens is None else r.n_tokens
+            if nt and r.tokens is None:
+                raise ValueError(f"row {i}: n_tokens without tokens")
+            self._rows[i] = spp_adjust(_ptr(r.src), _ptr(r.dst), _ptr(r.tokens), _ptr(r.bias_tokens),
+                                       _ptr(r.bias), _ptr(r.allowed), nt, r.n_prompt, nb, r.repetition,
+                                       r.frequency, r.presence, r.fill)
+        self._out, self._summ, nbytes = None, None, 0
+        if summaries and n:
+            dev = rows[0].src.device
+            self._out = torch.empty(n, 7, dtype=torch.int32, device=dev)
+            self._summ = AdjustSummaries(self._out)
+            nbytes = lib().spp_adjust_logits_work_bytes(n, vocab)
+            self._work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=dev)
+        self._args = (n, vocab, self._rows, ctypes.c_void_p(_ptr(self._out)),
+                      ctypes.c_void_p(_ptr(self._work) if nbytes else 0), nbytes)
+
+    def __call__(self, stream=None):
+        rc = lib().spp_adjust_logits(*self._args, ctypes.c_void_p(_stream(stream)))
+        if rc < 0:
+            raise SppError(rc, "spp_adjust_logits")
+        return self._summ
 
 
 def pack_weight(cfg: spp_model_config, which: int, src, dst, stream=None) -> None:

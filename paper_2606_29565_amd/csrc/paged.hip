@@ -1,0 +1,463 @@
+// Paged caches: attention of one new token per sequence, the copies of pages, and the QKV
+// epilogue that writes into them.
+//
+// Attention.  For a sequence and kv head with G query heads, over its live cells j:
+//   o = sum_j p_j v_j / l,  l = sum_j p_j,  p_j = 2^(s_j - m),  s_j = scale log2(e) q.k_j,
+// in one pass with the running maximum m (the sums so far are scaled by 2^(m_old - m) when it
+// grows).  Each cell's key and value are read once (2 dh elements) and used by G heads: 4 G
+// operations a pair of bytes in bf16, so HBM bounds it and the matrix cores, a sixteenth or
+// more of whose columns are in use, keep up many times over.
+//
+// Both products are turned over so that nothing is exchanged between lanes but the maximum:
+//   S^T = K Q^T: A = 16 keys, B = the heads' queries (16 columns, G in use);
+//   O^T = V^T P^T: A = 16 dims of V^T, B = the probabilities.
+// Lane (i, g) of S^T's result holds rows 4g .. 4g+3 of column i, and as the operand B of
+// the second product it has to hold the E keys of reduction group g (E = 8 in bf16, 4 in
+// fp32) of column i.  With row r of key tile t standing for key E (r / 4) + 4 t + r % 4 of the
+// step these are the same keys: a lane's scores become its operand in place.  A step is 4 E
+// keys (E / 4 tiles); every load is 16 bytes of a key's row or of E consecutive cells of a
+// V^T row, straight from the page to the operand's registers: no LDS, no barrier.  E divides the
+// page, so a lane finds one page for its keys and one for its values per step.
+#include <algorithm>
+#include <cmath>
+
+#include "common.hpp"
+#include "paged.hpp"
+
+namespace spp {
+namespace {
+
+constexpr int kWaves = 4;      // waves of an attention workgroup, each with its own key range
+constexpr int kMaxSplits = 256;
+
+template <typename T>
+constexpr int step_keys() { return 4 * Elem<T>::kPerFrag; }
+
+// Cells of a key range: a sequence's cells dealt out evenly over at most `splits` ranges of
+// whole steps of all waves.  (On the device, from the length as it is at the launch.)
+__device__ __forceinline__ int range_cells(int len, int splits, int unit) {
+  const int units = (len + unit - 1) / unit;
+  return (units + splits - 1) / splits * unit;
+}
+
+__device__ __forceinline__ int live_cells(const PagedAttn& a, int shift, int seq) {
+  const int len = a.lengths[seq], most = a.max_pages << shift;
+  return len < 0 ? 0 : (len < most ? len : most);
+}
+
+__device__ __forceinline__ void store_out(const PagedAttn& a, int64_t i, float v) {
+  if (a.out_mode == 0) {
+    static_cast<float*>(a.out)[i] = v;
+  } else if (a.out_mode == 1) {
+    static_cast<bf16_t*>(a.out)[i].bits = f32_to_bf16(v);
+  } else {
+    store_act(static_cast<bf16_t*>(a.out), static_cast<bf16_t*>(a.out_lo), i, v);
+  }
+}
+
+// Eight or four query elements in two parts of the cells' type (hi alone in fp32).
+__device__ __forceinline__ void query_frag(const void* q, bool q_bf16, int64_t at, uint4& hi, uint4& lo, bf16_t) {
+  if (q_bf16) {
+    hi = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(q) + at);
+    lo = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(q) + at);
+  const float4 b = *reinterpret_cast<const float4*>(static_cast<const float*>(q) + at + 4);
+  split_pair(a.x, a.y, hi.x, lo.x);
+  split_pair(a.z, a.w, hi.y, lo.y);
+  split_pair(b.x, b.y, hi.z, lo.z);
+  split_pair(b.z, b.w, hi.w, lo.w);
+}
+__device__ __forceinline__ void query_frag(const void* q, bool q_bf16, int64_t at, uint4& hi, uint4& lo, float) {
+  if (q_bf16) {
+    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(q) + at);
+    hi = make_uint4(w.x << 16, w.x & 0xFFFF0000u, w.y << 16, w.y & 0xFFFF0000u);
+  } else {
+    hi = *reinterpret_cast<const uint4*>(static_cast<const float*>(q) + at);
+  }
+  lo = make_uint4(0, 0, 0, 0);
+}
+
+// The first n of a unit's elements (E of T), the others zero.
+__device__ __forceinline__ uint4 keep_first(const uint4& v, int n, bf16_t) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = n >= 2 * i + 2 ? w[i] : (n == 2 * i + 1 ? w[i] & 0xFFFFu : 0u);
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+__device__ __forceinline__ uint4 keep_first(const uint4& v, int n, float) {
+  return make_uint4(n > 0 ? v.x : 0u, n > 1 ? v.y : 0u, n > 2 ? v.z : 0u, n > 3 ? v.w : 0u);
+}
+
+// Grid (key ranges, kv heads * head tiles, sequences).  A workgroup's range is cut among its
+// waves, each of which keeps (m, l, O^T) of its own; they are merged through LDS in wave
+// order, and the workgroup writes the sequence's output when its range is the only one, else
+// its (unnormalized) sums and (m, l) for paged_join_kernel.
+template <typename T, int DH, bool QLO>
+__global__ __launch_bounds__(64 * kWaves) void paged_attn_kernel(PageView v, int64_t layer_off, PagedAttn a,
+                                                                 float scale2, int tiles, float* o_part,
+                                                                 float2* ml_part) {
+  constexpr int E = Elem<T>::kPerFrag, KT = 4 * E, NT = E / 4, NC = DH / (4 * E), ND = DH / 16;
+  constexpr int OS = DH + 4;  // row stride of the merge buffer (its 16-byte stores hit all banks)
+  __shared__ float o_lds[kWaves * 16 * OS];
+  __shared__ float2 ml_lds[kWaves * 16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i = lane & 15, g = lane >> 4;
+  const int split = blockIdx.x, splits = gridDim.x, seq = blockIdx.z;
+  const int head = blockIdx.y / tiles, tile = blockIdx.y % tiles;
+  const int G = a.n_q / v.n_kv, q0 = head * G + tile * 16, nh = min(16, G - tile * 16);
+
+  const int len = live_cells(a, v.shift, seq);
+  const int range = range_cells(len, splits, KT * kWaves);
+  const int r0 = split * range;
+  if (r0 >= len && split > 0) return;  // (the join counts the ranges alike)
+  const int r1 = min(len, r0 + range), share = range / kWaves;
+  const int k_begin = r0 + wave * share, k_end = min(r1, k_begin + share);
+  const bool solo = range >= len;  // (an empty sequence: range 0, this writes its zeros)
+
+  uint4 qh[NC], ql[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    qh[c] = ql[c] = make_uint4(0, 0, 0, 0);
+    if (i < nh)
+      query_frag(a.q, a.q_bf16, (int64_t)seq * a.q_stride + (int64_t)(q0 + i) * DH + c * KT + g * E, qh[c], ql[c],
+                 T{});
+  }
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const int P1 = (1 << v.shift) - 1;
+  const int32_t* tab = a.table + (int64_t)seq * a.table_stride;
+  const int64_t page_bytes = v.page(), half = v.half();
+  // this head's keys and values inside a page of this layer
+  const char* kbase = v.base + layer_off + ((int64_t)head * DH << v.shift) * Elem<T>::kBytes;
+  const char* vbase = kbase + half;
+  const int last_page = (len - 1) >> v.shift;
+  for (int k0 = k_begin; k0 < k_end; k0 += KT) {
+    // the block of E keys of this lane's key rows, and that of its scores and values
+    const int kb = k0 + E * (i >> 2), vb = k0 + E * g;
+    int kp = tab[min(kb >> v.shift, last_page)], vp = tab[min(vb >> v.shift, last_page)];
+    const bool k_ok = (unsigned)kp < (unsigned)v.n_pages, v_ok = (unsigned)vp < (unsigned)v.n_pages;
+    kp = k_ok ? kp : 0;  // (read, and left out below)
+    vp = v_ok ? vp : 0;
+    const char* kr = kbase + kp * page_bytes + ((kb & P1) + (i & 3)) * (DH * Elem<T>::kBytes) + g * 16;
+    const char* vr = vbase + vp * page_bytes + (((int64_t)i << v.shift) + (vb & P1)) * Elem<T>::kBytes;
+    uint4 kf[NT][NC], vf[ND];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) kf[t][c] = ld_global(kr + t * 4 * DH * Elem<T>::kBytes + c * 64);
+#pragma unroll
+    for (int d = 0; d < ND; ++d) vf[d] = ld_global(vr + (((int64_t)d * 16) << v.shift) * Elem<T>::kBytes);
+    // live keys of this lane's block
+    const int nl = v_ok ? min(k_end - vb, E) : 0;
+    const bool whole = __all(nl == E);
+    float s[E];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      f32x4 d = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        d = mma_frag(kf[t][c], qh[c], d, T{});
+        if constexpr (QLO) d = mma_frag(kf[t][c], ql[c], d, T{});
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[4 * t + j] = d[j] * scale2;
+    }
+    if (!whole) {
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (j >= nl) s[j] = -INFINITY;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) vf[d] = keep_first(vf[d], nl, T{});
+    }
+    float top = s[0];
+#pragma unroll
+    for (int j = 1; j < E; ++j) top = fmaxf(top, s[j]);
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float mn = fmaxf(m, top);
+    const float mu = mn == -INFINITY ? 0.f : mn;  // nothing live yet
+    const float alpha = exp2f(m - mu);
+    m = mn;
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      s[j] = exp2f(s[j] - mu);
+      sum += s[j];
+    }
+    l = l * alpha + sum;
+    if (!__all(alpha == 1.f)) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) acc[d] *= alpha;
+    }
+    uint4 ph, pl;
+    if constexpr (E == 8) {
+      split_pair(s[0], s[1], ph.x, pl.x);
+      split_pair(s[2], s[3], ph.y, pl.y);
+      split_pair(s[4], s[5], ph.z, pl.z);
+      split_pair(s[6], s[7], ph.w, pl.w);
+    } else {
+      ph = make_uint4(__float_as_uint(s[0]), __float_as_uint(s[1]), __float_as_uint(s[2]), __float_as_uint(s[3]));
+      pl = ph;
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      acc[d] = mma_frag(vf[d], ph, acc[d], T{});
+      if constexpr (E == 8) acc[d] = mma_frag(vf[d], pl, acc[d], T{});
+    }
+  }
+  // l over the key groups of the step
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (g == 0) ml_lds[wave * 16 + i] = make_float2(m, l);
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+    *reinterpret_cast<float4*>(o_lds + (wave * 16 + i) * OS + d * 16 + g * 4) =
+        make_float4(acc[d][0], acc[d][1], acc[d][2], acc[d][3]);
+  __syncthreads();
+  for (int e = tid; e < nh * DH; e += 64 * kWaves) {
+    const int h = e / DH, d = e % DH;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, ml_lds[w * 16 + h].x);
+    const float mu = M == -INFINITY ? 0.f : M;
+    float o = 0.f, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float2 ml = ml_lds[w * 16 + h];
+      const float f = exp2f(ml.x - mu);
+      o += f * o_lds[(w * 16 + h) * OS + d];
+      L += f * ml.y;
+    }
+    if (solo) {
+      store_out(a, (int64_t)seq * a.out_stride + (int64_t)(q0 + h) * DH + d, L == 0.f ? 0.f : o / L);
+    } else {
+      const int64_t at = ((int64_t)seq * a.n_q + q0 + h) * splits + split;
+      o_part[at * DH + d] = o;
+      if (d == 0) ml_part[at] = make_float2(M, L);
+    }
+  }
+}
+
+// Grid (query heads, sequences), DH threads: the ranges of one head joined, in order.
+template <int DH>
+__global__ __launch_bounds__(DH) void paged_join_kernel(PagedAttn a, int shift, int splits, int unit,
+                                                        const float* o_part, const float2* ml_part) {
+  const int h = blockIdx.x, seq = blockIdx.y, d = threadIdx.x;
+  const int len = live_cells(a, shift, seq);
+  const int range = range_cells(len, splits, unit);
+  if (range >= len) return;  // one range: its workgroup has written the output
+  const int n = (len + range - 1) / range;
+  const int64_t at = ((int64_t)seq * a.n_q + h) * splits;
+  float M = -INFINITY;
+  for (int s = 0; s < n; ++s) M = fmaxf(M, ml_part[at + s].x);
+  const float mu = M == -INFINITY ? 0.f : M;
+  float o = 0.f, L = 0.f;
+  for (int s = 0; s < n; ++s) {
+    const float2 ml = ml_part[at + s];
+    const float f = exp2f(ml.x - mu);
+    o += f * o_part[(at + s) * DH + d];
+    L += f * ml.y;
+  }
+  store_out(a, (int64_t)seq * a.out_stride + (int64_t)h * DH + d, L == 0.f ? 0.f : o / L);
+}
+
+// One wave per (row, head) of the fused QKV output of a step whose rows are one token of one
+// sequence each: as qkv_epilogue_kernel, with the cells written into the sequence's page.
+template <typename T>
+__global__ __launch_bounds__(64) void paged_epilogue_kernel(Shape s, StepView sv, int M, int64_t layer_off,
+                                                            PageView v, const int32_t* table, int64_t table_stride,
+                                                            const float* P, int splits, const float* ss, int nb,
+                                                            const float2* rope, float* q_out) {
+  const int r = blockIdx.x, hh = blockIdx.y;
+  const int dh = s.dh, half = dh / 2;
+  const int N = (s.n_q + 2 * s.n_kv) * dh;
+  const int64_t split_stride = (int64_t)M * N;
+  const int64_t pr = (int64_t)r * N + (int64_t)hh * dh;
+  const int kind = hh < s.n_q ? 0 : (hh < s.n_q + s.n_kv ? 1 : 2);
+  const int pos = sv.row[r].pos;
+  T* cells = nullptr;  // this layer's K of the row's page
+  if (kind) {
+    const int page = table[(int64_t)r * table_stride + (pos >> v.shift)];
+    cells = reinterpret_cast<T*>(v.base + page * v.page() + layer_off);
+  }
+  const int cell = pos & ((1 << v.shift) - 1);
+  const float inv = row_inv(ss, r, nb, s.d, s.eps);
+  for (int i = threadIdx.x; i < half; i += 64) {
+    float a = add_splits(0.f, P, split_stride, splits, pr + i) * inv;
+    float b = add_splits(0.f, P, split_stride, splits, pr + i + half) * inv;
+    if (kind < 2) {
+      const float2 cs = rope[(int64_t)r * half + i];
+      const float a2 = a * cs.x - b * cs.y;
+      const float b2 = a * cs.y + b * cs.x;
+      a = a2;
+      b = b2;
+    }
+    if (kind == 0) {
+      q_out[((int64_t)r * s.n_q + hh) * dh + i] = a;
+      q_out[((int64_t)r * s.n_q + hh) * dh + i + half] = b;
+    } else if (kind == 1) {
+      T* k = cells + (((int64_t)(hh - s.n_q) << v.shift) + cell) * dh;
+      store_elem(k, i, a);
+      store_elem(k, i + half, b);
+    } else {
+      T* vt = cells + v.half() / Elem<T>::kBytes + ((int64_t)(hh - s.n_q - s.n_kv) * dh << v.shift) + cell;
+      store_elem(vt, (int64_t)i << v.shift, a);
+      store_elem(vt, (int64_t)(i + half) << v.shift, b);
+    }
+  }
+}
+
+// Grid (blocks, pages of the list): page b[y] = page a[y], 16 bytes a thread, four in flight.
+__global__ __launch_bounds__(256) void page_copy_kernel(PageView v, PageList l) {
+  const int64_t bytes = v.page(), n16 = bytes / 16;
+  const uint4* src = reinterpret_cast<const uint4*>(v.base + l.a[blockIdx.y] * bytes);
+  uint4* dst = reinterpret_cast<uint4*>(v.base + l.b[blockIdx.y] * bytes);
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n16; i += 4 * stride) {
+    uint4 w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i + u * stride < n16) w[u] = src[i + u * stride];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i + u * stride < n16) dst[i + u * stride] = w[u];
+  }
+}
+
+// Grid (layers * 2 * kv heads, pages of the list): one head's keys or values of one page, to
+// or from the session's buffer, in 16-byte units.  Of the last page only the live cells move.
+template <typename T, bool TO_PAGES>
+__global__ __launch_bounds__(256) void page_session_kernel(PageView v, PageList l, T* kv, int64_t cap, int64_t c0,
+                                                           int cells) {
+  constexpr int E = Elem<T>::kPerFrag;
+  const int P = 1 << v.shift, dh = v.dh;
+  const int head = blockIdx.x % v.n_kv, which = blockIdx.x / v.n_kv % 2, layer = blockIdx.x / v.n_kv / 2;
+  const int64_t at = c0 + (int64_t)blockIdx.y * P;                 // first cell of the page
+  const int live = min(P, cells - (int)blockIdx.y * P);            // its live cells
+  T* page = reinterpret_cast<T*>(v.base + l.a[blockIdx.y] * v.page() + (2 * layer + which) * v.half()) +
+            ((int64_t)head * dh << v.shift);
+  T* sess = kv + ((int64_t)(2 * layer + which) * v.n_kv + head) * cap * dh;
+  if (which == 0) {  // rows of a cell: [cell][dim] on both sides
+    T* s0 = sess + at * dh;
+    const int n = live * dh / E;
+    for (int u = threadIdx.x; u < n; u += 256) {
+      if (TO_PAGES)
+        reinterpret_cast<uint4*>(page)[u] = reinterpret_cast<const uint4*>(s0)[u];
+      else
+        reinterpret_cast<uint4*>(s0)[u] = reinterpret_cast<const uint4*>(page)[u];
+    }
+    return;
+  }
+  const int row = P / E;  // units of a V^T row of the page
+  for (int u = threadIdx.x; u < dh * row; u += 256) {
+    const int d = u / row, c = u % row * E;
+    if (c >= live) continue;
+    T* p = page + ((int64_t)d << v.shift) + c;
+    T* s = sess + d * cap + at + c;
+    T* dst = TO_PAGES ? p : s;
+    const T* src = TO_PAGES ? s : p;
+    if (c + E <= live) {
+      *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
+    } else {  // the cells past the last stay as they are
+      for (int e = 0; e < live - c; ++e) dst[e] = src[e];
+    }
+  }
+}
+
+template <typename T, int DH>
+hipError_t launch_attn(const PageView& v, int64_t layer_off, const PagedAttn& a, int splits, void* work,
+                       hipStream_t st) {
+  const int G = a.n_q / v.n_kv, tiles = (G + 15) / 16;
+  const float scale = a.scale != 0.f ? a.scale : (float)(1.0 / std::sqrt((double)DH));
+  const float scale2 = (float)(scale * 1.4426950408889634);
+  float* o_part = static_cast<float*>(work);
+  float2* ml_part = reinterpret_cast<float2*>(o_part + (int64_t)a.n * a.n_q * splits * DH);
+  const dim3 grid(splits, v.n_kv * tiles, a.n), block(64 * kWaves);
+  if (Elem<T>::kBytes == 2 && !a.q_bf16)
+    SPP_LAUNCH((paged_attn_kernel<T, DH, Elem<T>::kBytes == 2>), grid, block, 0, st, v, layer_off, a, scale2, tiles,
+               o_part, ml_part);
+  else
+    SPP_LAUNCH((paged_attn_kernel<T, DH, false>), grid, block, 0, st, v, layer_off, a, scale2, tiles, o_part, ml_part);
+  if (splits > 1)
+    SPP_LAUNCH((paged_join_kernel<DH>), dim3(a.n_q, a.n), dim3(DH), 0, st, a, v.shift, splits,
+               step_keys<T>() * kWaves, o_part, ml_part);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+namespace k {
+
+int paged_splits(const PageView& v, int n, int n_q, int max_pages) {
+  const int tiles = (n_q / v.n_kv + 15) / 16;
+  const int unit = (v.elem == 2 ? step_keys<bf16_t>() : step_keys<float>()) * kWaves;
+  const int64_t wgs = (int64_t)n * v.n_kv * tiles;
+  const int64_t most = (((int64_t)max_pages << v.shift) + unit - 1) / unit;
+  const int64_t want = (1024 + wgs - 1) / wgs;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, (int64_t)kMaxSplits}));
+}
+
+size_t paged_work_bytes(const PageView& v, int n, int n_q, int max_pages) {
+  const int splits = paged_splits(v, n, n_q, max_pages);
+  return splits == 1 ? 0 : (size_t)n * n_q * splits * (v.dh + 2) * 4;
+}
+
+hipError_t paged_attention(const PageView& v, int layer, const PagedAttn& a, void* work, hipStream_t st) {
+  if (a.n <= 0) return hipSuccess;
+  const int splits = paged_splits(v, a.n, a.n_q, a.max_pages);
+  const int64_t off = 2 * v.half() * layer;
+  if (v.elem == 2)
+    return v.dh == 128 ? launch_attn<bf16_t, 128>(v, off, a, splits, work, st)
+                       : launch_attn<bf16_t, 64>(v, off, a, splits, work, st);
+  return v.dh == 128 ? launch_attn<float, 128>(v, off, a, splits, work, st)
+                     : launch_attn<float, 64>(v, off, a, splits, work, st);
+}
+
+hipError_t page_copy(const PageView& v, const PageList& l, int n, hipStream_t st) {
+  if (n <= 0) return hipSuccess;
+  if (n > kPageBatch) return hipErrorInvalidValue;
+  // 4 units a thread, at most 64 workgroups a page and about 4096 in all
+  const int64_t blocks = (v.page() / 16 + 1023) / 1024;
+  const int per = (int)std::min<int64_t>(blocks, std::max(64, 4096 / n));
+  SPP_LAUNCH(page_copy_kernel, dim3(per, n), dim3(256), 0, st, v, l);
+  return hipGetLastError();
+}
+
+hipError_t page_session(const PageView& v, const PageList& l, int n, void* kv, int64_t cap, int64_t c0, int cells,
+                        bool to_pages, hipStream_t st) {
+  if (n <= 0) return hipSuccess;
+  if (n > kPageBatch) return hipErrorInvalidValue;
+  const dim3 grid(v.n_layers * 2 * v.n_kv, n), block(256);
+#define SPP_SESSION(T, D) \
+  SPP_LAUNCH((page_session_kernel<T, D>), grid, block, 0, st, v, l, static_cast<T*>(kv), cap, c0, cells)
+  if (v.elem == 2) {
+    if (to_pages) SPP_SESSION(bf16_t, true); else SPP_SESSION(bf16_t, false);
+  } else {
+    if (to_pages) SPP_SESSION(float, true); else SPP_SESSION(float, false);
+  }
+#undef SPP_SESSION
+  return hipGetLastError();
+}
+
+hipError_t paged_epilogue(const Shape& s, const StepView& sv, int n_rows, int layer, const PageView& v,
+                          const int32_t* table, int64_t table_stride, const float* partials, int splits,
+                          const float* ss, const float2* rope, float* q_out, hipStream_t st) {
+  const dim3 grid(n_rows, s.n_q + 2 * s.n_kv);
+  const int64_t off = 2 * v.half() * layer;
+  if (s.bf16)
+    SPP_LAUNCH((paged_epilogue_kernel<bf16_t>), grid, dim3(64), 0, st, s, sv, n_rows, off, v, table, table_stride,
+               partials, splits, ss, res_blocks(s), rope, q_out);
+  else
+    SPP_LAUNCH((paged_epilogue_kernel<float>), grid, dim3(64), 0, st, s, sv, n_rows, off, v, table, table_stride,
+               partials, splits, ss, res_blocks(s), rope, q_out);
+  return hipGetLastError();
+}
+
+}  // namespace k
+}  // namespace spp

@@ -1,10 +1,6 @@
 // Host runtime behind the C ABI (include/spp.h): models, sessions, the ready-
 // distribution record with its epoch, the step scheduler that packs entries into
 // one device pass, the gate's decision logic and the invalidation discipline.
-#include "spp.h"
-
-#include <hip/hip_runtime.h>
-
 #include <algorithm>
 #include <chrono>
 #include <cmath>
@@ -18,8 +14,8 @@
 #include <unordered_map>
 #include <vector>
 
-#include "kernels.hpp"
 #include "plans.hpp"
+#include "runtime.hpp"
 
 using namespace spp;
 
@@ -48,11 +44,9 @@ bool recorder_events(hipEvent_t* start, hipEvent_t* stop) {
   return true;
 }
 
-}  // namespace spp
-
 namespace {
-
 thread_local std::string t_err;
+}
 
 spp_status fail(spp_status st, const char* fmt, ...) {
   char buf[512];
@@ -64,97 +58,9 @@ spp_status fail(spp_status st, const char* fmt, ...) {
   return st;
 }
 
-#define HIPCHK(expr)                                                                     \
-  do {                                                                                   \
-    hipError_t e_ = (expr);                                                              \
-    if (e_ != hipSuccess) return fail(SPP_E_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
+}  // namespace spp
 
-int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
-
-// A device buffer that grows on demand.  Growing frees the old block, so the caller
-// must make sure no queued work still uses it.
-struct DevBuf {
-  void* p = nullptr;
-  size_t bytes = 0;
-};
-
-// Per-kernel timing for spp_profile_preposition (dispatch events, see LaunchRecorder).
-using Prof = LaunchRecorder;
-
-struct Model {
-  spp_model_config cfg{};
-  Shape s{};
-  int device = 0;
-  int n_cu = 256;                     // compute units of the device (attention work sizing)
-  size_t elem = 2;
-  const void* embed = nullptr;
-  const void* final_norm = nullptr;
-  const void* lm_head = nullptr;
-  const float* lm_bias = nullptr;
-  std::vector<const void*> attn_norm, wq, wk, wv, wo, mlp_norm, wg, wu, wd;  // wq..wd tiled
-  bool fp4 = false;                   // wq..wd are MXFP4 codes (tiled), scales in wsc
-  std::vector<const void*> wsc[7];    // tiled e8m0 scales per spp_weight_kind (MXFP4)
-  std::vector<void*> owned;           // library-owned packed copies (weights_packed == 0)
-  void* lm_tiled = nullptr;           // packed LM head for the batched path (max_sessions > 1)
-  int slab[5] = {1, 1, 1, 1, 1};      // tiled-layout slab (K-steps) of QKV, O, gate/up, down, LM head
-  // work buffers
-  float* x = nullptr;
-  void* h = nullptr;
-  void* q = nullptr;
-  void* att = nullptr;
-  void* act = nullptr;
-  float* part = nullptr;
-  size_t part_elems = 0;              // floats of `part`
-  char* small = nullptr;              // one allocation: the scan buffers, ss, range, rope and z
-  float* ss = nullptr;                // row sums of squares [max_tokens][res_blocks]
-  uint32_t* range = nullptr;          // the step's fp16 range word per segment [kMaxSegments]
-  float2* rope = nullptr;
-  void* z = nullptr;
-  float* logits_rows = nullptr;
-  ScanPartial* gate_parts = nullptr; // two scan buffers of k::kScanBufBytes, side by side
-  ScanPartial* lm_parts = nullptr;
-  ScanResult* gate_host = nullptr;   // pinned, device-mapped [64] results, then the done word
-  ScanResult* gate_dev = nullptr;
-  uint32_t gate_seq = 0;
-  uint32_t gate_late = 0;            // a scan that its call gave up on and that may still run (0: none)
-  DevBuf o_part, ml_part, params_dev;
-  char* params_host = nullptr;
-  size_t params_host_bytes = 0;
-  hipEvent_t params_free = nullptr;  // the last params upload has been consumed
-  hipEvent_t step_done = nullptr;    // the last step has finished with the work buffers
-  hipEvent_t chunk_end[2] = {};      // ends of the last two layer chunks of a yielding pass
-  bool step_recorded = false;
-  std::mutex mu;       // one step at a time per model (work buffers)
-  std::mutex gate_mu;  // one gate scan at a time per model (gate buffers)
-};
-
-struct Session {
-  Model* m = nullptr;
-  int id = 0;
-  int capacity = 0, cap_stride = 0, budget = 0;
-  void* kv = nullptr;
-  size_t kv_bytes = 0;
-  std::mutex mu;
-  int n_s = 0;
-  std::vector<int32_t> entry;  // the pre-positioned entry (speculative cells n_s..)
-  bool valid = false;
-  uint64_t epoch = 0;
-  int position = -1;
-  float* dist = nullptr;
-  hipEvent_t done = nullptr;
-  uint64_t decoded_epoch = ~0ull;  // epoch whose device work was seen finished
-  ScanResult* summary = nullptr;  // device slot written by the LM head
-  // Released with the last reference: a gate that looked the session up by its id keeps
-  // it alive until it returns, even when spp_session_destroy runs meanwhile.
-  ~Session() {
-    if (done) {
-      hipEventSynchronize(done);
-      hipEventDestroy(done);
-    }
-    if (summary) hipFree(summary);
-  }
-};
+namespace {
 
 // Sessions by id.  Calls that take a ready handle (a value naming the session by id)
 // hold a reference for their duration; spp_session_destroy drops the registry's.
@@ -186,15 +92,6 @@ spp_status ensure_dev(Model& m, DevBuf& b, size_t bytes) {
   return SPP_OK;
 }
 
-struct SegReq {
-  Session* s;
-  const int32_t* tok;
-  int len;
-  int n_past;
-  float* dist;
-  const uint32_t* bitmap;
-};
-
 #define LAUNCH(cls, call)                                                                  \
   do {                                                                                     \
     if (prof) prof->cur = (cls);                                                           \
@@ -202,15 +99,6 @@ struct SegReq {
     if (prof) prof->cur = -1;                                                              \
     if (e_ != hipSuccess) return fail(SPP_E_HIP, "%s: %s", #call, hipGetErrorString(e_)); \
   } while (0)
-
-// Cooperative yield of an idle-window pass (Sec. 3.1): the layers are enqueued in chunks,
-// at most two chunks ahead of the device, and before each chunk the caller's flag is read;
-// once it is set, nothing more is enqueued and the pass ends when the device has drained.
-struct YieldCtl {
-  const volatile uint32_t* flag;
-  int chunk;       // layers per chunk
-  bool yielded;
-};
 
 // Before chunk c (c >= 1) of a yielding pass: mark the end of chunk c-1, then wait until
 // chunk c-2 has finished (two chunks in flight keep the device busy while the host
@@ -242,12 +130,17 @@ bool chunk_gate(Model& m, YieldCtl& y, int c, hipStream_t st, spp_status* rc) {
   return true;
 }
 
+}  // namespace
+
+namespace spp {
+
 // One device pass over the packed rows of `segs` (all of the same model).  With
 // `logits`, also the LM head and reductions at each segment's last row.  With `y`, the
-// pass yields as described at YieldCtl (then y->yielded is set and no logits are made).
+// pass yields as described at YieldCtl (then y->yielded is set and no logits are made).  With
+// `cache`, the rows' cells are where it says (each segment one row of a paged sequence).
 // Caller holds m.mu and every session's mutex.
 spp_status run_step(Model& m, const SegReq* segs, int nseg, bool logits, hipStream_t st,
-                    Prof* prof, YieldCtl* y = nullptr) {
+                    Prof* prof, YieldCtl* y, StepCache* cache) {
   const Shape& s = m.s;
   const int G = s.n_q / s.n_kv;
   int rows = 0;
@@ -276,12 +169,13 @@ spp_status run_step(Model& m, const SegReq* segs, int nseg, bool logits, hipStre
   std::vector<int> row0(nseg + 1, 0);
   for (int i = 0; i < nseg; ++i) row0[i + 1] = row0[i] + segs[i].len;
   auto seg_of = [&](int i) {
-    return Segment{segs[i].s->kv, segs[i].s->cap_stride, segs[i].n_past, row0[i], segs[i].len};
+    const Session* ss = segs[i].s;
+    return Segment{ss ? ss->kv : nullptr, ss ? ss->cap_stride : 0, segs[i].n_past, row0[i], segs[i].len};
   };
   std::vector<AttnItem> items;
   std::vector<AttnGroup> groups;
   const int RG = attn_rows(s);
-  {
+  if (!cache) {
     int64_t total_blocks = 0;
     for (int i = 0; i < nseg; ++i) {
       const int R = segs[i].len * G;
@@ -342,12 +236,15 @@ spp_status run_step(Model& m, const SegReq* segs, int nseg, bool logits, hipStre
   off = round_up(off + sizeof(AttnItem) * items.size(), 16);
   const size_t off_gr = off;
   off = round_up(off + sizeof(AttnGroup) * groups.size(), 16);
+  const size_t off_cache = off;
+  if (cache) off = round_up(off + cache->record_bytes(), 16);
   const size_t bytes = off;
 
   spp_status rc;
   if ((rc = ensure_dev(m, m.params_dev, bytes)) != SPP_OK) return rc;
   // attention partials: fp16 normalized outputs for bf16 models, fp32 sums for fp32 models
-  if ((rc = ensure_dev(m, m.o_part, items.size() * RG * s.dh * (s.bf16 ? 2 : 4))) != SPP_OK) return rc;
+  const size_t part_bytes = cache ? cache->part_bytes() : items.size() * RG * s.dh * (s.bf16 ? 2 : 4);
+  if ((rc = ensure_dev(m, m.o_part, part_bytes)) != SPP_OK) return rc;
   if ((rc = ensure_dev(m, m.ml_part, items.size() * RG * sizeof(float2))) != SPP_OK) return rc;
 
   // the pinned staging record is reused: wait until its last upload was consumed
@@ -377,11 +274,12 @@ spp_status run_step(Model& m, const SegReq* segs, int nseg, bool logits, hipStre
     hp->seg[i] = seg_of(i);
     for (int j = 0; j < segs[i].len; ++j, ++r) {
       tok[r] = segs[i].tok[j];
-      ri[r] = RowInfo{segs[i].s->kv, segs[i].s->cap_stride, segs[i].n_past + j, i, 0};
+      ri[r] = RowInfo{hp->seg[i].kv, hp->seg[i].cap, segs[i].n_past + j, i, 0};
     }
   }
   if (!items.empty()) memcpy(m.params_host + off_it, items.data(), sizeof(AttnItem) * items.size());
   if (!groups.empty()) memcpy(m.params_host + off_gr, groups.data(), sizeof(AttnGroup) * groups.size());
+  if (cache) cache->fill(m.params_host + off_cache, static_cast<char*>(m.params_dev.p) + off_cache);
 
   // ---- order after the previous step of this model, whatever stream it ran on
   if (m.step_recorded) HIPCHK(hipStreamWaitEvent(st, m.step_done, 0));
@@ -422,13 +320,19 @@ spp_status run_step(Model& m, const SegReq* segs, int nseg, bool logits, hipStre
     WeightCat wqkv{{m.wq[l], m.wk[l], m.wv[l]}, {0, nq, nq + nkv, nq + 2 * nkv}, m.slab[0],
                    {sc(SPP_W_Q, l), sc(SPP_W_K, l), sc(SPP_W_V, l)}};
     LAUNCH(KC_GEMM_QKV, gemm(s, p_qkv, m.h, h_lo, M, d, wqkv, nq + 2 * nkv, m.part, st));
-    LAUNCH(KC_QKV_EPI, k::qkv_epilogue(s, dp, M, l, m.part, p_qkv.splits, m.ss, m.rope, m.q, q_lo,
-                                       m.range, st));
-    LAUNCH(KC_ATTN, k::attention(s, dp, n_items, l, m.q, q_lo, m.o_part.p,
-                                 static_cast<float2*>(m.ml_part.p), m.att, att_lo, m.range, st));
-    LAUNCH(KC_ATTN_COMBINE, k::attention_combine(s, dp, n_groups, m.o_part.p,
-                                                 static_cast<float2*>(m.ml_part.p), m.att, att_lo,
-                                                 st));
+    if (cache) {  // (q in fp32: the hi and lo arrays of bf16 models take as many bytes)
+      float* q32 = static_cast<float*>(m.q);
+      LAUNCH(KC_QKV_EPI, cache->epilogue(dp, M, l, m.part, p_qkv.splits, m.ss, m.rope, q32, st));
+      LAUNCH(KC_ATTN, cache->attention(l, q32, m.o_part.p, m.att, att_lo, st));
+    } else {
+      LAUNCH(KC_QKV_EPI, k::qkv_epilogue(s, dp, M, l, m.part, p_qkv.splits, m.ss, m.rope, m.q, q_lo,
+                                         m.range, st));
+      LAUNCH(KC_ATTN, k::attention(s, dp, n_items, l, m.q, q_lo, m.o_part.p,
+                                   static_cast<float2*>(m.ml_part.p), m.att, att_lo, m.range, st));
+      LAUNCH(KC_ATTN_COMBINE, k::attention_combine(s, dp, n_groups, m.o_part.p,
+                                                   static_cast<float2*>(m.ml_part.p), m.att, att_lo,
+                                                   st));
+    }
     WeightCat wo{{m.wo[l], nullptr, nullptr}, {0, d, d, d}, m.slab[1], {sc(SPP_W_O, l), nullptr, nullptr}};
     LAUNCH(KC_GEMM_O, gemm(s, p_o, m.att, att_lo, M, nq, wo, d, m.part, st));
     LAUNCH(KC_RESID_NORM, k::residual(s, M, m.part, p_o.splits, m.x, m.mlp_norm[l], m.h, h_lo, m.ss,
@@ -451,7 +355,7 @@ spp_status run_step(Model& m, const SegReq* segs, int nseg, bool logits, hipStre
     if (nseg == 1) {
       const float* xr = m.x + (int64_t)(segs[0].len - 1) * d;
       LAUNCH(KC_LMHEAD, k::lmhead_gemv(s, xr, m.final_norm, m.lm_head, m.lm_bias, segs[0].dist,
-                                       segs[0].bitmap, m.lm_parts, segs[0].s->summary, m.range,
+                                       segs[0].bitmap, m.lm_parts, segs[0].summary, m.range,
                                        st));
     } else {
       LAUNCH(KC_LMHEAD, k::final_norm_rows(s, dp, nseg, m.x, m.final_norm, m.z, z_lo, st));
@@ -462,7 +366,7 @@ spp_status run_step(Model& m, const SegReq* segs, int nseg, bool logits, hipStre
       for (int i = 0; i < nseg; ++i) {
         job.dist[i] = segs[i].dist;
         job.bitmap[i] = segs[i].bitmap;
-        job.result[i] = segs[i].s->summary;
+        job.result[i] = segs[i].summary;
         job.flag_src[i] = m.range + i;
       }
       job.src = m.logits_rows;
@@ -502,6 +406,10 @@ void fill_summary(const ScanResult& r, int position, spp_summary* out) {
   out->position = position;
   out->flags = r.flags & 7u;
 }
+
+}  // namespace spp
+
+namespace {
 
 spp_gate_outcome decide(const ScanResult& r, float tau, int32_t* token) {
   *token = -1;
@@ -590,9 +498,6 @@ spp_status wait_done(Model& m, uint32_t seq, hipStream_t st) {
 }
 
 }  // namespace
-
-struct spp_model_s : Model {};
-struct spp_session_s : Session {};
 
 extern "C" {
 
@@ -965,7 +870,7 @@ spp_status spp_kv_append_delta(spp_session_t s, const int32_t* tokens, int32_t n
   std::lock_guard<std::mutex> mk(m.mu);
   for (int off = 0; off < n; off += m.cfg.max_tokens) {
     const int len = std::min(n - off, m.cfg.max_tokens);
-    SegReq r{s, tokens + off, len, s->n_s + off, nullptr, nullptr};
+    SegReq r{s, tokens + off, len, s->n_s + off, nullptr, nullptr, s->summary};
     rc = run_step(m, &r, 1, false, static_cast<hipStream_t>(stream), nullptr);
     if (rc != SPP_OK) return rc;
   }
@@ -999,7 +904,7 @@ static spp_status preposition_impl(spp_session_t s, const int32_t* entry, int32_
   hipSetDevice(m.device);
   {
     std::lock_guard<std::mutex> mk(m.mu);
-    SegReq r{s, entry, L, s->n_s, dist, bitmap};
+    SegReq r{s, entry, L, s->n_s, dist, bitmap, s->summary};
     rc = run_step(m, &r, 1, true, static_cast<hipStream_t>(stream), prof, y);
     if (rc != SPP_OK) return rc;
     if (y && y->yielded) {  // the entry cells written so far stay uncommitted
@@ -1057,7 +962,8 @@ spp_status spp_resume(spp_session_t s, const int32_t* delta, int32_t n, float* d
     for (int off = 0; off < n; off += m.cfg.max_tokens) {
       const int len = std::min(n - off, m.cfg.max_tokens);
       const bool last = off + len == n;
-      SegReq r{s, delta + off, len, s->n_s + off, last ? dist : nullptr, last ? bitmap : nullptr};
+      SegReq r{s, delta + off, len, s->n_s + off, last ? dist : nullptr, last ? bitmap : nullptr,
+               s->summary};
       rc = run_step(m, &r, 1, last, st, nullptr);
       if (rc != SPP_OK) {
         s->n_s += off;  // the chunks already written stay committed
@@ -1474,7 +1380,7 @@ static spp_status preposition_batch_impl(int32_t n, const spp_session_t* session
       continue;
     }
     out_status[i] = SPP_OK;
-    reqs.push_back(SegReq{s, entries[i], lengths[i], s->n_s, dists[i], nullptr});
+    reqs.push_back(SegReq{s, entries[i], lengths[i], s->n_s, dists[i], nullptr, s->summary});
     req_of.push_back(i);
   }
   hipSetDevice(m.device);
