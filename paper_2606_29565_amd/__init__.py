@@ -724,8 +724,8 @@ class PagedAttention:
         n, width = table.shape
         self._keep = (pool, table, lengths)
         self._dtype = torch.bfloat16 if io_bf16 else torch.float32
-        self._shape = (n, n_q_heads, pool.cfg.head_dim)
-        row = n_q_heads * pool.cfg.head_dim
+        self._shape = torch.Size((n, n_q_heads, pool.cfg.head_dim))
+        self._row = row = n_q_heads * pool.cfg.head_dim
         dummy = pool.pages.data_ptr()
         self._a = spp_paged_attn(pool.handle.value, layer, n, n_q_heads,
                                  SPP_DTYPE_BF16 if io_bf16 else SPP_DTYPE_F32, dummy, row,
@@ -738,12 +738,12 @@ class PagedAttention:
         self._nb = self._work.numel()
 
     def __call__(self, q, out, stream=None):
-        for t, what in ((q, "q"), (out, "out")):
-            if t.dtype != self._dtype or tuple(t.shape) != self._shape:
-                raise ValueError(f"{what}: {self._dtype} of shape {self._shape}")
+        if q.dtype != self._dtype or out.dtype != self._dtype or q.shape != self._shape or \
+                out.shape != self._shape:
+            raise ValueError(f"q and out: {self._dtype} of shape {tuple(self._shape)}")
         a = self._a
-        a.q, a.q_stride = q.data_ptr(), _row_stride(q, "q")
-        a.out, a.out_stride = out.data_ptr(), _row_stride(out, "out")
+        a.q, a.q_stride = q.data_ptr(), self._row if q.is_contiguous() else _row_stride(q, "q")
+        a.out, a.out_stride = out.data_ptr(), self._row if out.is_contiguous() else _row_stride(out, "out")
         rc = lib().spp_paged_attention(self._ref, self._wp, self._nb, ctypes.c_void_p(_stream(stream)))
         if rc < 0:
             raise SppError(rc, "spp_paged_attention")

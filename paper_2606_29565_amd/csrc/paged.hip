@@ -17,7 +17,16 @@
 // step these are the same keys: a lane's scores become its operand in place.  A step is 4 E
 // keys (E / 4 tiles); every load is 16 bytes of a key's row or of E consecutive cells of a
 // V^T row, straight from the page to the operand's registers: no LDS, no barrier.  E divides the
-// page, so a lane finds one page for its keys and one for its values per step.
+// page, so a lane finds one page for its keys and one for its values of such a step.
+//
+// A trip of the loop takes two of these steps (64 keys in bf16, 32 in fp32): a V^T row of a page
+// of 64 cells or more is then read in whole 128-byte lines.  (One step a trip read each line in
+// two halves, a trip apart, with as many cells in flight on an XCD as its L2 holds: 231 us for 64 sequences
+// of U[1024, 8192] cells, 8 heads of 128, 1.14 GB, against 220, and 289 against 259 with
+// loads that bypass the L2.)
+// The next trip's keys are loaded once this trip's scores are formed, its values once this
+// trip's sums are: one register set of each (236 of the 256 that two waves a SIMD have), and
+// always one of the two in flight.
 #include <algorithm>
 #include <cmath>
 
@@ -31,7 +40,7 @@ constexpr int kWaves = 4;      // waves of an attention workgroup, each with its
 constexpr int kMaxSplits = 256;
 
 template <typename T>
-constexpr int step_keys() { return 4 * Elem<T>::kPerFrag; }
+constexpr int step_keys() { return 8 * Elem<T>::kPerFrag; }
 
 // Cells of a key range: a sequence's cells dealt out evenly over at most `splits` ranges of
 // whole steps of all waves.  (On the device, from the length as it is at the launch.)
@@ -96,10 +105,10 @@ __device__ __forceinline__ uint4 keep_first(const uint4& v, int n, float) {
 // order, and the workgroup writes the sequence's output when its range is the only one, else
 // its (unnormalized) sums and (m, l) for paged_join_kernel.
 template <typename T, int DH, bool QLO>
-__global__ __launch_bounds__(64 * kWaves) void paged_attn_kernel(PageView v, int64_t layer_off, PagedAttn a,
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PageView v, int64_t layer_off, PagedAttn a,
                                                                  float scale2, int tiles, float* o_part,
                                                                  float2* ml_part) {
-  constexpr int E = Elem<T>::kPerFrag, KT = 4 * E, NT = E / 4, NC = DH / (4 * E), ND = DH / 16;
+  constexpr int E = Elem<T>::kPerFrag, KT = 4 * E, KS = 2 * KT, NT = E / 4, NC = DH / (4 * E), ND = DH / 16;
   constexpr int OS = DH + 4;  // row stride of the merge buffer (its 16-byte stores hit all banks)
   __shared__ float o_lds[kWaves * 16 * OS];
   __shared__ float2 ml_lds[kWaves * 16];
@@ -110,7 +119,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_kernel(PageView v, int
   const int G = a.n_q / v.n_kv, q0 = head * G + tile * 16, nh = min(16, G - tile * 16);
 
   const int len = live_cells(a, v.shift, seq);
-  const int range = range_cells(len, splits, KT * kWaves);
+  const int range = range_cells(len, splits, KS * kWaves);
   const int r0 = split * range;
   if (r0 >= len && split > 0) return;  // (the join counts the ranges alike)
   const int r1 = min(len, r0 + range), share = range / kWaves;
@@ -137,79 +146,141 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_kernel(PageView v, int
   const char* kbase = v.base + layer_off + ((int64_t)head * DH << v.shift) * Elem<T>::kBytes;
   const char* vbase = kbase + half;
   const int last_page = (len - 1) >> v.shift;
-  for (int k0 = k_begin; k0 < k_end; k0 += KT) {
-    // the block of E keys of this lane's key rows, and that of its scores and values
-    const int kb = k0 + E * (i >> 2), vb = k0 + E * g;
-    int kp = tab[min(kb >> v.shift, last_page)], vp = tab[min(vb >> v.shift, last_page)];
-    const bool k_ok = (unsigned)kp < (unsigned)v.n_pages, v_ok = (unsigned)vp < (unsigned)v.n_pages;
-    kp = k_ok ? kp : 0;  // (read, and left out below)
-    vp = v_ok ? vp : 0;
-    const char* kr = kbase + kp * page_bytes + ((kb & P1) + (i & 3)) * (DH * Elem<T>::kBytes) + g * 16;
-    const char* vr = vbase + vp * page_bytes + (((int64_t)i << v.shift) + (vb & P1)) * Elem<T>::kBytes;
-    uint4 kf[NT][NC], vf[ND];
+  const int trips = k_begin < k_end ? (k_end - k_begin + KS - 1) / KS : 0;
+
+  // Page numbers (not yet checked) of this lane's keys and values, by step half.
+  int kp[2], vp[2], vq[2];  // next step's; and the values' of the step whose keys are issued
+  auto pages = [&](int k) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int u = 0; u < 2; ++u) {
+      const int k0 = k_begin + k * KS + u * KT;
+      kp[u] = tab[min((k0 + E * (i >> 2)) >> v.shift, last_page)];
+      vp[u] = tab[min((k0 + E * g) >> v.shift, last_page)];
+    }
+  };
+  uint4 kf[2][NT][NC], vf[2][ND];
+  // The loads of step k's keys, after those of the next step's page numbers: so the wait for
+  // these, a step on, is not one for the cells.  (A page that is not listed: page 0 is read,
+  // and left out by the mask.)
+  auto issue_keys = [&](int k) {
+    const char* kr[2];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) kf[t][c] = ld_global(kr + t * 4 * DH * Elem<T>::kBytes + c * 64);
+    for (int u = 0; u < 2; ++u) {
+      const int kb = k_begin + k * KS + u * KT + E * (i >> 2);
+      kr[u] = kbase + ((unsigned)kp[u] < (unsigned)v.n_pages ? kp[u] : 0) * page_bytes +
+              ((kb & P1) + (i & 3)) * (DH * Elem<T>::kBytes) + g * 16;
+      vq[u] = vp[u];
+    }
+    pages(k + 1);
 #pragma unroll
-    for (int d = 0; d < ND; ++d) vf[d] = ld_global(vr + (((int64_t)d * 16) << v.shift) * Elem<T>::kBytes);
-    // live keys of this lane's block
-    const int nl = v_ok ? min(k_end - vb, E) : 0;
-    const bool whole = __all(nl == E);
-    float s[E];
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      f32x4 d = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        d = mma_frag(kf[t][c], qh[c], d, T{});
-        if constexpr (QLO) d = mma_frag(kf[t][c], ql[c], d, T{});
+        for (int c = 0; c < NC; ++c) kf[u][t][c] = ld_global(kr[u] + t * 4 * DH * Elem<T>::kBytes + c * 64);
+  };
+  int nl[2];  // live keys of this lane's blocks
+  auto issue_values = [&](int k) {
+    const char* vr[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int vb = k_begin + k * KS + u * KT + E * g;
+      const bool ok = (unsigned)vq[u] < (unsigned)v.n_pages;
+      nl[u] = ok ? min(k_end - vb, E) : 0;
+      vr[u] = vbase + (ok ? vq[u] : 0) * page_bytes + (((int64_t)i << v.shift) + (vb & P1)) * Elem<T>::kBytes;
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) vf[u][d] = ld_global(vr[u] + (((int64_t)d * 16) << v.shift) * Elem<T>::kBytes);
+  };
+  float s[2][E];
+  auto scores = [&]() {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        f32x4 d = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          d = mma_frag(kf[u][t][c], qh[c], d, T{});
+          if constexpr (QLO) d = mma_frag(kf[u][t][c], ql[c], d, T{});
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[u][4 * t + j] = d[j];
       }
+  };
+  auto fold = [&]() {
+    const bool whole = __all(nl[0] == E && nl[1] == E);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[4 * t + j] = d[j] * scale2;
-    }
-    if (!whole) {
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int j = 0; j < E; ++j)
-        if (j >= nl) s[j] = -INFINITY;
+      for (int j = 0; j < E; ++j) s[u][j] = whole || j < nl[u] ? s[u][j] * scale2 : -INFINITY;
+    float top = s[0][0];
 #pragma unroll
-      for (int d = 0; d < ND; ++d) vf[d] = keep_first(vf[d], nl, T{});
-    }
-    float top = s[0];
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int j = 1; j < E; ++j) top = fmaxf(top, s[j]);
+      for (int j = 0; j < E; ++j) top = fmaxf(top, s[u][j]);
     top = fmaxf(top, __shfl_xor(top, 16, 64));
     top = fmaxf(top, __shfl_xor(top, 32, 64));
     const float mn = fmaxf(m, top);
     const float mu = mn == -INFINITY ? 0.f : mn;  // nothing live yet
-    const float alpha = exp2f(m - mu);
+    const float alpha = __builtin_amdgcn_exp2f(m - mu);
     m = mn;
     float sum = 0.f;
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-      s[j] = exp2f(s[j] - mu);
-      sum += s[j];
-    }
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        s[u][j] = __builtin_amdgcn_exp2f(s[u][j] - mu);
+        sum += s[u][j];
+      }
     l = l * alpha + sum;
     if (!__all(alpha == 1.f)) {
 #pragma unroll
       for (int d = 0; d < ND; ++d) acc[d] *= alpha;
     }
-    uint4 ph, pl;
-    if constexpr (E == 8) {
-      split_pair(s[0], s[1], ph.x, pl.x);
-      split_pair(s[2], s[3], ph.y, pl.y);
-      split_pair(s[4], s[5], ph.z, pl.z);
-      split_pair(s[6], s[7], ph.w, pl.w);
-    } else {
-      ph = make_uint4(__float_as_uint(s[0]), __float_as_uint(s[1]), __float_as_uint(s[2]), __float_as_uint(s[3]));
-      pl = ph;
-    }
 #pragma unroll
-    for (int d = 0; d < ND; ++d) {
-      acc[d] = mma_frag(vf[d], ph, acc[d], T{});
-      if constexpr (E == 8) acc[d] = mma_frag(vf[d], pl, acc[d], T{});
+    for (int u = 0; u < 2; ++u) {
+      uint4 ph, pl;
+      if constexpr (E == 8) {
+        split_pair(s[u][0], s[u][1], ph.x, pl.x);
+        split_pair(s[u][2], s[u][3], ph.y, pl.y);
+        split_pair(s[u][4], s[u][5], ph.z, pl.z);
+        split_pair(s[u][6], s[u][7], ph.w, pl.w);
+      } else {
+        ph = make_uint4(__float_as_uint(s[u][0]), __float_as_uint(s[u][1]), __float_as_uint(s[u][2]),
+                        __float_as_uint(s[u][3]));
+      }
+      if (!whole) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d) vf[u][d] = keep_first(vf[u][d], nl[u], T{});
+      }
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        acc[d] = mma_frag(vf[u][d], ph, acc[d], T{});
+        if constexpr (E == 8) acc[d] = mma_frag(vf[u][d], pl, acc[d], T{});
+      }
     }
+  };
+  // The next step's keys are on their way from the moment this step's scores are formed, its
+  // values from the end of this step's sums: one set of registers each.
+  if (trips > 0) {
+    pages(0);
+    issue_keys(0);
+    issue_values(0);
+    for (int k = 0; k + 1 < trips; ++k) {
+      scores();
+      __builtin_amdgcn_sched_barrier(0);
+      issue_keys(k + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      fold();
+      __builtin_amdgcn_sched_barrier(0);
+      issue_values(k + 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    scores();
+    fold();
   }
   // l over the key groups of the step
   l += __shfl_xor(l, 16, 64);
@@ -230,7 +301,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_kernel(PageView v, int
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const float2 ml = ml_lds[w * 16 + h];
-      const float f = exp2f(ml.x - mu);
+      const float f = __builtin_amdgcn_exp2f(ml.x - mu);
       o += f * o_lds[(w * 16 + h) * OS + d];
       L += f * ml.y;
     }
@@ -407,12 +478,13 @@ hipError_t launch_attn(const PageView& v, int64_t layer_off, const PagedAttn& a,
   const float scale2 = (float)(scale * 1.4426950408889634);
   float* o_part = static_cast<float*>(work);
   float2* ml_part = reinterpret_cast<float2*>(o_part + (int64_t)a.n * a.n_q * splits * DH);
-  const dim3 grid(splits, v.n_kv * tiles, a.n), block(64 * kWaves);
+  const dim3 grid(splits, v.n_kv * tiles, a.n);
   if (Elem<T>::kBytes == 2 && !a.q_bf16)
-    SPP_LAUNCH((paged_attn_kernel<T, DH, Elem<T>::kBytes == 2>), grid, block, 0, st, v, layer_off, a, scale2, tiles,
-               o_part, ml_part);
+    SPP_LAUNCH((paged_attn_kernel<T, DH, Elem<T>::kBytes == 2>), grid, dim3(64 * kWaves), 0, st, v, layer_off, a,
+               scale2, tiles, o_part, ml_part);
   else
-    SPP_LAUNCH((paged_attn_kernel<T, DH, false>), grid, block, 0, st, v, layer_off, a, scale2, tiles, o_part, ml_part);
+    SPP_LAUNCH((paged_attn_kernel<T, DH, false>), grid, dim3(64 * kWaves), 0, st, v, layer_off, a, scale2, tiles,
+               o_part, ml_part);
   if (splits > 1)
     SPP_LAUNCH((paged_join_kernel<DH>), dim3(a.n_q, a.n), dim3(kMaxSplits), 0, st, a, v.shift, splits,
                step_keys<T>() * kWaves, o_part, ml_part);
@@ -423,13 +495,21 @@ hipError_t launch_attn(const PageView& v, int64_t layer_off, const PagedAttn& a,
 
 namespace k {
 
+// Ranges of a sequence and kv head.  A range is at least one step of its workgroup's waves (256
+// cells in bf16, 128 in fp32).
+//  - A table of at most four such steps: one range, without the second launch (37 sequences of up
+//    to 700 cells, 2 heads of 64 in bf16: 8.0 us; in three ranges 5.2 and 3.6 for the join).
+//  - Else about 1024 workgroups over all, two rounds of two to a CU (three sequences of 32749
+//    cells, 8 heads of 128: 77 us; aiming at 2048 83, at 4096 89), but at least four ranges each, which even
+//    out sequences of unequal lengths (64 of U[1024, 8192] cells, 8 heads of 128: 220 us; two
+//    ranges each 230, three 225, eight 219; ranges of 1024 cells at most, however many 263).
 int paged_splits(const PageView& v, int n, int n_q, int max_pages) {
   const int tiles = (n_q / v.n_kv + 15) / 16;
   const int unit = (v.elem == 2 ? step_keys<bf16_t>() : step_keys<float>()) * kWaves;
-  const int64_t wgs = (int64_t)n * v.n_kv * tiles;
   const int64_t most = (((int64_t)max_pages << v.shift) + unit - 1) / unit;
-  const int64_t want = (1024 + wgs - 1) / wgs;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, (int64_t)kMaxSplits}));
+  if (most <= 4) return 1;
+  const int64_t want = std::max<int64_t>(4, 1024 / ((int64_t)n * v.n_kv * tiles));
+  return (int)std::min<int64_t>({want, most, (int64_t)kMaxSplits});
 }
 
 size_t paged_work_bytes(const PageView& v, int n, int n_q, int max_pages) {
