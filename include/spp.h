@@ -598,8 +598,8 @@ typedef struct {
   const int32_t* bias_tokens;   /* device, [n_bias]                                       */
   const float* bias;            /* device, [n_bias]                                       */
   const uint32_t* allowed;      /* device bitmap as the gate's fast-answer set; NULL: all */
-  int32_t n_tokens, n_prompt;   /* 0 <= n_prompt <= n_tokens                              */
-  int32_t n_bias;
+  int32_t n_tokens, n_prompt;   /* 0 <= n_prompt <= n_tokens <= 2^30                      */
+  int32_t n_bias;               /* 0..2^30                                                */
   float repetition;             /* finite, > 0; 1 changes nothing                         */
   float frequency, presence;    /* finite; 0 changes nothing                              */
   float fill;                   /* not NaN.  The gate never serves a distribution with an

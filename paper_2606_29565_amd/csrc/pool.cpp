@@ -626,6 +626,7 @@ spp_status spp_adjust_logits(int32_t n, int32_t vocab, const spp_adjust* rows, s
     if (!r.src || !r.dst || r.n_tokens < 0 || r.n_bias < 0 || (r.n_tokens && !r.tokens) ||
         (r.n_bias && (!r.bias_tokens || !r.bias)))
       return fail(SPP_E_INVALID_ARG, "row %d: null pointer or negative count", i);
+    if (r.n_tokens > (1 << 30) || r.n_bias > (1 << 30)) return fail(SPP_E_INVALID_ARG, "row %d: a list over 2^30", i);
     if (r.n_prompt < 0 || r.n_prompt > r.n_tokens) return fail(SPP_E_INVALID_ARG, "row %d: n_prompt", i);
     if (!(r.repetition > 0.f) || !std::isfinite(r.repetition) || !std::isfinite(r.frequency) ||
         !std::isfinite(r.presence) || std::isnan(r.fill))
