@@ -8,9 +8,12 @@
 // token needs to know of the history -- whether it occurs, and how often past the prompt -- is
 // gathered per workgroup: it owns a slice of the vocabulary, reads the whole list of tokens
 // (from L2 after the first workgroup; a history is a few KB against 8 bytes per token of the
-// vocabulary) and counts those of its slice in LDS with integer atomics, whose order does not matter.  The
-// largest index of a bias entry is kept the same way, so the last entry of a token counts.
-// Nothing of the vocabulary's size besides the logits is written, cleared or read again.
+// vocabulary) and counts those of its slice in LDS with integer atomics, whose order does not
+// matter.  The largest index of a bias entry is kept the same way, so the last entry of a token
+// counts.  Nothing of the vocabulary's size besides the logits is written, cleared or read again.
+// Measured (with the launch that merges the slices' reductions): 64 rows of 128256 27.0 us,
+// 2.4 TB/s; without lists and reductions 32 rows take 7.0 us, a copy of them 6.0.  One row is
+// launches and latency: 9.8 us.
 #include "reduce.hpp"
 #include "paged.hpp"
 
@@ -19,9 +22,14 @@ namespace {
 
 constexpr int kTpb = 256;
 
+// The rows of one launch travel as its argument: few or, within 4 KB, many.  (With the argument
+// of many rows a call of one took 0.4 us longer.)
+constexpr int kFewRows = 4, kManyRows = 48;
+template <int R>
 struct AdjustBatch {
-  spp_adjust row[kAdjustRows];
+  spp_adjust row[R];
 };
+static_assert(sizeof(AdjustBatch<kManyRows>) + 16 <= 4096, "a kernel's argument");
 
 struct Penalties {
   float repetition, frequency, presence;
@@ -43,23 +51,29 @@ __device__ __forceinline__ float adjust_one(float y, const Penalties& p, uint32_
 // Grid (slices, rows), UNITS * 1024 tokens a slice.  A row's tokens are cut into units of four
 // at 16-byte boundaries of src (unit u holds tokens 4u - a .. 4u - a + 3, a the elements that
 // src starts past such a boundary), so that all whole units are 16-byte accesses whatever the
-// row's alignment; unit u of the slice belongs to thread u % 256.  LDS: a count (bit 31: seen
-// in the prompt) and, with biases, a bias entry per token of the slice.
-template <int UNITS>
-__global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch jobs, ScanPartial* parts) {
+// row's alignment; unit u of the slice belongs to thread u % 256.
+//
+// An instruction for every token of 32 rows of 128256 takes the chip 0.1 us: what counts is the
+// instructions each token costs.  So the few tokens with a penalty or bias are adjusted one at
+// a time: a thread puts its logits into LDS, goes over those of them that were counted, and
+// takes them back.  (64 rows of 128256 with 2000 tokens and 100 biases, with the summaries: a wave that
+// adjusts all its tokens wherever one lane needs it 32.3 us, a list of the touched tokens made by
+// the counting 30.4, this 27.0.)
+template <int UNITS, int R>
+__global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs, ScanPartial* parts) {
   constexpr int S = UNITS * 4 * kTpb;
-  extern __shared__ uint32_t lds[];
+  __shared__ __align__(16) float xs[S];        // the slice's logits
+  __shared__ __align__(16) uint32_t cnt[S];    // occurrences past the prompt; bit 31: in the prompt
+  __shared__ __align__(16) uint32_t bias_at[S];  // last bias entry of the token, plus one
   __shared__ ScanPartial red[4];
   const spp_adjust r = jobs.row[blockIdx.y];
   const Penalties pen{r.repetition, r.frequency, r.presence};
   const int tid = threadIdx.x;
-  uint32_t* cnt = lds;
-  uint32_t* bias_at = lds + S;  // (present when some row of the launch has biases)
   const int a = (int)((reinterpret_cast<uintptr_t>(r.src) & 15) / 4);
   const bool pair = ((reinterpret_cast<uintptr_t>(r.src) ^ reinterpret_cast<uintptr_t>(r.dst)) & 15) == 0;
   const int v0 = (int)blockIdx.x * S - a;  // first token of the slice (before the row: skipped)
   const bool penal = r.n_tokens > 0 && (r.repetition != 1.f || r.frequency != 0.f || r.presence != 0.f);
-  const bool biased = r.n_bias > 0, masked = r.allowed != nullptr;
+  const bool biased = r.n_bias > 0, masked = r.allowed != nullptr, sparse = penal || biased;
   const int n_tokens = penal ? r.n_tokens : 0;
 
   // The lists' first entries, then the slice's logits and mask are on their way while LDS is
@@ -102,63 +116,79 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch jobs, S
       w[u][0] = r.allowed[min(max(t, 0), V - 1) >> 5];
       w[u][1] = r.allowed[min(max(t + 3, 0), V - 1) >> 5];
     }
-  const uint4 zero = make_uint4(0, 0, 0, 0);
-  if (penal)
-    for (int i = tid; i < S / 4; i += kTpb) reinterpret_cast<uint4*>(cnt)[i] = zero;
-  if (biased)
-    for (int i = tid; i < S / 4; i += kTpb) reinterpret_cast<uint4*>(bias_at)[i] = zero;
-  __syncthreads();
-  // (a slice's tokens below 0 or from V on are none of the row's: entries there are skipped)
-  const int lo = max(v0, 0), hi = min(v0 + S, V);
-  for (int i0 = tid; i0 - tid < n_tokens; i0 += AHEAD * kTpb) {
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (i0 + u * kTpb < n_tokens && tok[u] >= lo && tok[u] < hi) {
-        if (i0 + u * kTpb < r.n_prompt)
-          atomicOr(cnt + (tok[u] - v0), 0x80000000u);
-        else
-          atomicAdd(cnt + (tok[u] - v0), 1u);
-      }
-    if (i0 - tid + AHEAD * kTpb < n_tokens) tokens_at(i0 + AHEAD * kTpb);
-  }
-  for (int i = tid; i - tid < r.n_bias; i += kTpb) {
-    if (i < r.n_bias && bt >= lo && bt < hi) atomicMax(bias_at + (bt - v0), (uint32_t)i + 1);
-    if (i - tid + kTpb < r.n_bias) bt = r.bias_tokens[min(i + kTpb, r.n_bias - 1)];
-  }
-  __syncthreads();
 
-  // Adjusted and stored; then x holds the allowed values, -inf elsewhere.
+  if (sparse) {
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      reinterpret_cast<uint4*>(cnt)[u * kTpb + tid] = zero;
+      if (biased) reinterpret_cast<uint4*>(bias_at)[u * kTpb + tid] = zero;
+    }
+    __syncthreads();
+    // (a slice's tokens below 0 or from V on are none of the row's: entries there are skipped)
+    const int lo = max(v0, 0), hi = min(v0 + S, V);
+    for (int i0 = tid; i0 - tid < n_tokens; i0 += AHEAD * kTpb) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (i0 + u * kTpb < n_tokens && tok[u] >= lo && tok[u] < hi) {
+          if (i0 + u * kTpb < r.n_prompt)
+            atomicOr(cnt + (tok[u] - v0), 0x80000000u);
+          else
+            atomicAdd(cnt + (tok[u] - v0), 1u);
+        }
+      if (i0 - tid + AHEAD * kTpb < n_tokens) tokens_at(i0 + AHEAD * kTpb);
+    }
+    for (int i = tid; i - tid < r.n_bias; i += kTpb) {
+      if (i < r.n_bias && bt >= lo && bt < hi) atomicMax(bias_at + (bt - v0), (uint32_t)i + 1);
+      if (i - tid + kTpb < r.n_bias) bt = r.bias_tokens[min(i + kTpb, r.n_bias - 1)];
+    }
+    __syncthreads();
+    uint32_t touched = 0;  // of the thread's own tokens, a bit each
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      reinterpret_cast<float4*>(xs)[u * kTpb + tid] = make_float4(x[u][0], x[u][1], x[u][2], x[u][3]);
+      uint4 c = reinterpret_cast<const uint4*>(cnt)[u * kTpb + tid];
+      if (biased) {
+        const uint4 b = reinterpret_cast<const uint4*>(bias_at)[u * kTpb + tid];
+        c = make_uint4(c.x | b.x, c.y | b.y, c.z | b.z, c.w | b.w);
+      }
+      touched |= ((c.x ? 1u : 0u) | (c.y ? 2u : 0u) | (c.z ? 4u : 0u) | (c.w ? 8u : 0u)) << (4 * u);
+    }
+    for (uint32_t todo = touched; todo; todo &= todo - 1) {
+      const int f = __ffs(todo) - 1, at = 4 * (f / 4 * kTpb + tid) + f % 4;
+      const uint32_t b = biased ? bias_at[at] : 0u;
+      xs[at] = adjust_one(xs[at], pen, cnt[at], b, b ? r.bias[b - 1] : 0.f);
+    }
+    if (touched)
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        const float4 q = reinterpret_cast<const float4*>(xs)[u * kTpb + tid];
+        x[u][0] = q.x; x[u][1] = q.y; x[u][2] = q.z; x[u][3] = q.w;
+      }
+  }
+
+  // Masked and stored; then x holds the allowed values, -inf elsewhere.
   uint32_t live = 0;  // a bit per value: in the row and allowed
+  bool odd = false;   // one of these is NaN or +-inf
 #pragma unroll
   for (int u = 0; u < UNITS; ++u) {
-    const int at = 4 * (u * kTpb + tid), t = v0 + at;
-    uint4 c = zero, ba = zero;
-    if (penal) c = *reinterpret_cast<const uint4*>(cnt + at);
-    if (biased) ba = *reinterpret_cast<const uint4*>(bias_at + at);
-    if (c.x | c.y | c.z | c.w | ba.x | ba.y | ba.z | ba.w) {
-      const uint32_t cs[4] = {c.x, c.y, c.z, c.w}, bs[4] = {ba.x, ba.y, ba.z, ba.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float bias = 0.f;
-        if (bs[e]) bias = r.bias[bs[e] - 1];
-        x[u][e] = adjust_one(x[u][e], pen, cs[e], bs[e], bias);
-      }
-    }
-    uint32_t bits = 0xFu;
+    const int t = v0 + 4 * (u * kTpb + tid);
     const bool whole = t >= t_lo && t <= t_hi;
+    uint32_t bits = 0xFu;
     if (!whole) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (t + e < 0 || t + e >= V) bits &= ~(1u << e);
     }
     const uint32_t in_row = bits;
-    // bits t & 31 and up of the two words side by side; before the row (t < 0, bits left out
-    // above) the first word is that of token 0
-    if (masked)
+    float y[4] = {x[u][0], x[u][1], x[u][2], x[u][3]};
+    if (masked) {
+      // bits t & 31 and up of the two words side by side; before the row (t < 0, bits left out
+      // above) the first word is that of token 0
       bits &= t >= 0 ? (uint32_t)((((uint64_t)w[u][1] << 32) | w[u][0]) >> (t & 31)) : w[u][0] << (-t & 3);
-    float y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (bits >> e) & 1u ? x[u][e] : r.fill;
+      for (int e = 0; e < 4; ++e) y[e] = (bits >> e) & 1u ? y[e] : r.fill;
+    }
     if (pair && whole) {
       *reinterpret_cast<float4*>(r.dst + t) = make_float4(y[0], y[1], y[2], y[3]);
     } else {
@@ -166,41 +196,68 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch jobs, S
       for (int e = 0; e < 4; ++e)
         if ((in_row >> e) & 1u) r.dst[t + e] = y[e];
     }
-    live |= bits << (4 * u);
+    if (masked || !whole) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool ok = (bits >> e) & 1u;
+        odd |= ok && !(fabsf(x[u][e]) < INFINITY);
+        x[u][e] = ok ? x[u][e] : -INFINITY;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd |= !(fabsf(x[u][e]) < INFINITY);
+    }
+    live |= (bits & 0xFu) << (4 * u);
   }
   if (!parts) return;
-  // The two largest of the thread's allowed values (NaN is none), the index of the largest,
-  // lowest on ties, and the sum of exponentials: the values are all there, so it needs no
-  // running maximum.
-  Acc acc;
-  acc_init(acc);
+
+  // The slice's partial from the largest value on: the thread's two largest (v_max and v_med
+  // take NaN for none), the workgroup's largest; only where a thread holds it, its index; the
+  // sums of exponentials against it.
+  float v1 = -INFINITY, v2 = -INFINITY;
 #pragma unroll
   for (int u = 0; u < UNITS; ++u)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const bool ok = (live >> (4 * u + e)) & 1u;
-      acc.nonfinite |= ok && !(fabsf(x[u][e]) < INFINITY);
-      x[u][e] = ok ? x[u][e] : -INFINITY;
       const float y = fmaxf(x[u][e], -INFINITY);  // (NaN -> -inf)
-      acc.t.i1 = y > acc.t.v1 ? v0 + 4 * (u * kTpb + tid) + e : acc.t.i1;
-      acc.t.v2 = __builtin_amdgcn_fmed3f(y, acc.t.v1, acc.t.v2);
-      acc.t.v1 = fmaxf(acc.t.v1, y);
+      v2 = __builtin_amdgcn_fmed3f(y, v1, v2);
+      v1 = fmaxf(v1, y);
     }
-  if (acc.t.i1 == 0x7FFFFFFF && live) {  // nothing above -inf: the first allowed -inf
+  Acc acc;
+  acc.t = Top2{v1, v2, 0x7FFFFFFF};
+  acc.m = wave_max(v1);
+  acc.s = 0.f;
+  acc.nonfinite = odd;
+  if (v1 == acc.m && live) {
 #pragma unroll
     for (int u = UNITS - 1; u >= 0; --u)
 #pragma unroll
       for (int e = 3; e >= 0; --e)
-        if ((live >> (4 * u + e)) & 1u && x[u][e] == x[u][e]) acc.t.i1 = v0 + 4 * (u * kTpb + tid) + e;
+        if ((live >> (4 * u + e)) & 1u && x[u][e] == v1) acc.t.i1 = v0 + 4 * (u * kTpb + tid) + e;
   }
-  acc.m = acc.t.v1;
-  if (acc.m > -INFINITY)
+  if (acc.m > -INFINITY) {
 #pragma unroll
     for (int u = 0; u < UNITS; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc.s += __expf(x[u][e] - acc.m);
-  acc = block_acc<true>(acc, red);
-  if (tid == 0) parts[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = to_partial(acc);
+      for (int e = 0; e < 4; ++e) acc.s += __builtin_amdgcn_exp2f((x[u][e] - acc.m) * 1.44269504f);
+  }
+  // over the wave: the sums in a fixed order, the lowest index of the largest, the second
+  // largest among the others' largest and its holder's second
+  acc.s = wave_sum(acc.s);
+  int first = acc.t.i1;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) first = min(first, __shfl_xor(first, o, 64));
+  acc.t.v2 = wave_max(first != 0x7FFFFFFF && acc.t.i1 == first ? v2 : v1);
+  acc.t.v1 = acc.m;
+  acc.t.i1 = first;
+  acc.nonfinite = __any(odd) ? 1u : 0u;
+  if ((tid & 63) == 0) red[tid >> 6] = to_partial(acc);
+  __syncthreads();
+  if (tid == 0) {
+    Acc all = from_partial(red[0]);
+    for (int k = 1; k < kTpb / 64; ++k) acc_merge<true>(all, from_partial(red[k]));
+    parts[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = to_partial(all);
+  }
 }
 
 // Grid (rows), one wave each: the slices' partials merged in a fixed order.
@@ -223,14 +280,10 @@ __global__ __launch_bounds__(64) void adjust_merge_kernel(int nb, const ScanPart
   out[blockIdx.x] = s;
 }
 
-// Tokens of a slice: 1024 to 4096, so that a launch has about a thousand workgroups.
-int slice_units(int n, int vocab) {
-  const int64_t want = (int64_t)vocab * n / 1024;
-#ifdef UMAX
-  if (want > 1024) return UMAX;
-#endif
-  return want <= 1024 ? 1 : (want <= 2048 ? 2 : 4);
-}
+// Tokens of a slice: 1024 while that makes under 2048 workgroups, else 2048, which halves how
+// often a history is read (64 rows of 128256 with 2000 tokens each: 27.0 us, with 1024 30.1;
+// 17 rows of 152063 with 700: 12.9 and 14.3).
+int slice_units(int n, int vocab) { return (int64_t)vocab * n <= 2048 * 1024 ? 1 : 2; }
 // Slices of a row, whatever its alignment.
 int slices(int units, int vocab) { return (vocab + 3 + units * 4 * kTpb - 1) / (units * 4 * kTpb); }
 
@@ -242,26 +295,26 @@ size_t adjust_work_bytes(int n, int vocab) {
   return (size_t)n * slices(slice_units(n, vocab), vocab) * sizeof(ScanPartial);
 }
 
+template <int R>
+void launch_rows(int units, int nb, int m, int vocab, const spp_adjust* rows, ScanPartial* parts, hipStream_t st) {
+  AdjustBatch<R> b{};
+  for (int i = 0; i < m; ++i) b.row[i] = rows[i];
+  if (units == 1)
+    SPP_LAUNCH((adjust_kernel<1, R>), dim3(nb, m), dim3(kTpb), 0, st, vocab, b, parts);
+  else
+    SPP_LAUNCH((adjust_kernel<2, R>), dim3(nb, m), dim3(kTpb), 0, st, vocab, b, parts);
+}
+
 hipError_t adjust_logits(int n, int vocab, const spp_adjust* rows, spp_summary* summaries, void* work,
                          hipStream_t st) {
   const int units = slice_units(n, vocab), nb = slices(units, vocab);
-  for (int r0 = 0; r0 < n; r0 += kAdjustRows) {
-    const int m = n - r0 < kAdjustRows ? n - r0 : kAdjustRows;
-    AdjustBatch b{};
-    bool bias = false;
-    for (int i = 0; i < m; ++i) {
-      b.row[i] = rows[r0 + i];
-      bias |= rows[r0 + i].n_bias > 0;
-    }
+  for (int r0 = 0; r0 < n; r0 += kManyRows) {
+    const int m = n - r0 < kManyRows ? n - r0 : kManyRows;
     ScanPartial* parts = summaries ? static_cast<ScanPartial*>(work) + (int64_t)r0 * nb : nullptr;
-    const unsigned shm = (bias ? 2u : 1u) * units * 4 * kTpb * 4;
-    const dim3 grid(nb, m), block(kTpb);
-    if (units == 1)
-      SPP_LAUNCH(adjust_kernel<1>, grid, block, shm, st, vocab, b, parts);
-    else if (units == 2)
-      SPP_LAUNCH(adjust_kernel<2>, grid, block, shm, st, vocab, b, parts);
+    if (m <= kFewRows)
+      launch_rows<kFewRows>(units, nb, m, vocab, rows + r0, parts, st);
     else
-      SPP_LAUNCH(adjust_kernel<4>, grid, block, shm, st, vocab, b, parts);
+      launch_rows<kManyRows>(units, nb, m, vocab, rows + r0, parts, st);
   }
   if (summaries)
     SPP_LAUNCH(adjust_merge_kernel, dim3(n), dim3(64), 0, st, nb, static_cast<const ScanPartial*>(work),

@@ -39,9 +39,6 @@ struct PageList {
   int32_t a[kPageBatch], b[kPageBatch];
 };
 
-// Rows of logits adjusted in one launch, likewise.
-constexpr int kAdjustRows = 32;
-
 namespace k {
 
 // Key ranges per sequence and kv head of a call: a rule on n, the heads and the table's width.
