@@ -428,7 +428,8 @@ spp_status spp_gate_batch_noalloc(int32_t n, const spp_ready_t* ready, const flo
  * the call's stream and ordered after that of the pool's earlier calls on whatever stream,
  * so a page freed and taken again is not written while earlier work reads it.  A pool's
  * calls may come from several threads: they are serialized.  Work that a caller enqueues on
- * the pages by itself (spp_paged_attention too) is the caller's to order. */
+ * the pages by itself (spp_paged_attention too) is the caller's to order.  A pool's calls are
+ * not for capture into a graph (spp_paged_attention is). */
 typedef struct spp_pool_s* spp_pool_t;
 
 typedef struct {
@@ -535,7 +536,7 @@ spp_status spp_pool_compact(spp_pool_t pool, void* stream, int32_t* n_moved);
  * and lives on its device.  Asynchronous on `stream`.  SPP_E_INVALID_ARG for a null pointer,
  * n < 1, a sequence that does not exist or is listed twice, a token outside [0, vocab);
  * SPP_E_CAPACITY when the pages run out or a sequence is SPP_MAX_CAPACITY cells long (then
- * nothing ran). */
+ * nothing ran).  After SPP_E_HIP the sequences of finished passes have grown, the others not. */
 spp_status spp_decode_batch(spp_pool_t pool, spp_model_t model, int32_t n, const int32_t* seqs,
                             const int32_t* tokens, float* const* dists, void* stream);
 /* The reductions over the logits that the last spp_decode_batch of each sequence wrote (as

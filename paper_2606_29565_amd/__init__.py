@@ -580,6 +580,9 @@ def gate_batch(readies: Sequence[Ready], taus: Sequence[float], bitmaps, stream=
     return [(outs[i], toks[i]) for i in range(n)]
 
 
+_ShortTable = ctypes.c_int32 * 64
+
+
 class PagePool:
     """Pages of a paged cache (spp_pool_*): sequences are numbers, the pages a device buffer
     (`pages`: a contiguous tensor of at least the pool's bytes; else allocated here)."""
@@ -590,6 +593,7 @@ class PagePool:
                                    SPP_DTYPE_BF16 if bf16 else SPP_DTYPE_F32, page_cells, n_pages,
                                    max_seqs)
         self.handle = None
+        self._lib = lib()
         if pages is None:
             import torch
             nbytes = lib().spp_pool_bytes(ctypes.byref(self.cfg))
@@ -632,7 +636,9 @@ class PagePool:
         return q.value
 
     def free(self, seq: int) -> None:
-        check(lib().spp_seq_free(self.handle, seq), "spp_seq_free")
+        rc = self._lib.spp_seq_free(self.handle, seq)
+        if rc < 0:
+            raise SppError(rc, "spp_seq_free")
 
     def seq_info(self, seq: int) -> spp_seq_info:
         out = spp_seq_info()
@@ -641,10 +647,11 @@ class PagePool:
 
     def table(self, seq: int) -> List[int]:
         """The sequence's page numbers."""
-        n = ctypes.c_int32()
-        check(lib().spp_seq_table(self.handle, seq, None, 0, ctypes.byref(n)), "spp_seq_table")
-        t = (ctypes.c_int32 * max(1, n.value))()
-        check(lib().spp_seq_table(self.handle, seq, t, n.value, ctypes.byref(n)), "spp_seq_table")
+        n, t = ctypes.c_int32(), _ShortTable()
+        if self._lib.spp_seq_table(self.handle, seq, t, len(t), ctypes.byref(n)) < 0:  # a longer one?
+            check(self._lib.spp_seq_table(self.handle, seq, None, 0, ctypes.byref(n)), "spp_seq_table")
+            t = (ctypes.c_int32 * max(1, n.value))()
+            check(self._lib.spp_seq_table(self.handle, seq, t, n.value, ctypes.byref(n)), "spp_seq_table")
         return t[:n.value]
 
     def fork(self, seq: int, n: int = 1) -> List[int]:
@@ -778,6 +785,15 @@ class AdjustSummaries:
         self.top1, self.top2, self.gap, self.lse = f[:, 1], f[:, 2], f[:, 3], f[:, 4]
 
 
+def _vector(t, dtype, least: int, row: int, what: str) -> Optional[int]:
+    """The device pointer of a contiguous tensor of at least `least` elements (None: no tensor)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < least:
+        raise ValueError(f"row {row}: {what} is a contiguous {dtype} tensor of at least {least}")
+    return t.data_ptr()
+
+
 class LogitsAdjust:
     """spp_adjust_logits with its rows marshalled once: each call() adjusts them and returns
     their AdjustSummaries (None with summaries=False), which the next call overwrites."""
@@ -789,24 +805,21 @@ class LogitsAdjust:
         words = (vocab + 31) // 32
         self._rows = (spp_adjust * max(1, n))()
         for i, r in enumerate(rows):
-            for t, what, dt, least in ((r.src, "src", torch.float32, vocab), (r.dst, "dst", torch.float32, vocab),
-                                       (r.tokens, "tokens", torch.int32, r.n_tokens or 0),
-                                       (r.bias_tokens, "bias_tokens", torch.int32, 0),
-                                       (r.bias, "bias", torch.float32, 0),
-                                       (r.allowed, "allowed", torch.int32, words)):
-                if t is None and what not in ("src", "dst"):
-                    continue
-                if t.dtype != dt or t.dim() != 1 or t.numel() < least or (t.numel() > 1 and t.stride(0) != 1):
-                    raise ValueError(f"row {i}: {what} is a contiguous {dt} vector of at least {least}")
-            nb = 0 if r.bias_tokens is None else r.bias_tokens.numel()
-            if nb != (0 if r.bias is None else r.bias.numel()):
-                raise ValueError(f"row {i}: bias and bias_tokens differ in length")
             nt = (0 if r.tokens is None else r.tokens.numel()) if r.n_tokens is None else r.n_tokens
             if nt and r.tokens is None:
                 raise ValueError(f"row {i}: n_tokens without tokens")
-            self._rows[i] = spp_adjust(_ptr(r.src), _ptr(r.dst), _ptr(r.tokens), _ptr(r.bias_tokens),
-                                       _ptr(r.bias), _ptr(r.allowed), nt, r.n_prompt, nb, r.repetition,
-                                       r.frequency, r.presence, r.fill)
+            nb = 0 if r.bias_tokens is None else r.bias_tokens.numel()
+            if nb != (0 if r.bias is None else r.bias.numel()):
+                raise ValueError(f"row {i}: bias and bias_tokens differ in length")
+            if r.src is None or r.dst is None:
+                raise ValueError(f"row {i}: src and dst are needed")
+            self._rows[i] = spp_adjust(
+                _vector(r.src, torch.float32, vocab, i, "src"), _vector(r.dst, torch.float32, vocab, i, "dst"),
+                _vector(r.tokens, torch.int32, nt, i, "tokens"),
+                _vector(r.bias_tokens, torch.int32, nb, i, "bias_tokens"),
+                _vector(r.bias, torch.float32, nb, i, "bias"),
+                _vector(r.allowed, torch.int32, words, i, "allowed"), nt, r.n_prompt, nb, r.repetition,
+                r.frequency, r.presence, r.fill)
         self._out, self._summ, nbytes = None, None, 0
         if summaries and n:
             dev = rows[0].src.device

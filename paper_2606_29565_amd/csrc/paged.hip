@@ -413,61 +413,88 @@ __global__ __launch_bounds__(64) void paged_epilogue_kernel(Shape s, StepView sv
   }
 }
 
-// Grid (blocks, pages of the list): page b[y] = page a[y], 16 bytes a thread, four in flight.
+// Grid (blocks, pages of the list): page b[y] = page a[y], an equal stretch for each block, four
+// 16-byte units of a thread in flight.  No load is in a branch (past the end the last unit is
+// read again), so none is waited for by itself.  (One page of 2 MiB to 64 others 25 us, 5.4 TB/s of
+// writes; 16 pages moved 11.5 us, 5.8 TB/s.  Units dealt to the blocks in turn 24 and 15.5;
+// with branches around the loads 44 and 21.)
 __global__ __launch_bounds__(256) void page_copy_kernel(PageView v, PageList l) {
-  const int64_t bytes = v.page(), n16 = bytes / 16;
-  const uint4* src = reinterpret_cast<const uint4*>(v.base + l.a[blockIdx.y] * bytes);
-  uint4* dst = reinterpret_cast<uint4*>(v.base + l.b[blockIdx.y] * bytes);
-  const int64_t stride = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n16; i += 4 * stride) {
-    uint4 w[4];
+  const int64_t bytes = v.page(), units = bytes / 16;
+  const u32x4* src = reinterpret_cast<const u32x4*>(v.base + l.a[blockIdx.y] * bytes);
+  u32x4* dst = reinterpret_cast<u32x4*>(v.base + l.b[blockIdx.y] * bytes);
+  const int64_t per = (units + gridDim.x - 1) / gridDim.x, u0 = blockIdx.x * per, u1 = min(u0 + per, units);
+  for (int64_t u = u0 + threadIdx.x; u < u1; u += 4 * 256) {
+    u32x4 w[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i + u * stride < n16) w[u] = src[i + u * stride];
+    for (int k = 0; k < 4; ++k) w[k] = src[min(u + k * 256, u1 - 1)];
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i + u * stride < n16) dst[i + u * stride] = w[u];
+    for (int k = 0; k < 4; ++k)
+      if (u + k * 256 < u1) dst[u + k * 256] = w[k];
   }
 }
 
-// Grid (layers * 2 * kv heads, pages of the list): one head's keys or values of one page, to
-// or from the session's buffer, in 16-byte units.  Of the last page only the live cells move.
+// Grid (pages of the list, fastest, times layers * 2 * kv heads): one head's keys or values of one
+// page, to or from the session's buffer, in 16-byte units.  Of the last page only the live
+// cells move.  (Neighbouring workgroups take neighbouring pages, so that the pieces of a V^T row
+// are read close in time: 8100 cells of 4 layers of the 8B shape, 265 MB, into pages of 64 in 55.9 us,
+// 4.7 TB/s; heads fastest 64.5.  Several pages to a workgroup: no shorter.)
 template <typename T, bool TO_PAGES>
-__global__ __launch_bounds__(256) void page_session_kernel(PageView v, PageList l, T* kv, int64_t cap, int64_t c0,
-                                                           int cells) {
+__global__ __launch_bounds__(256) void page_session_kernel(PageView v, PageList l, int n_pages, T* kv, int64_t cap,
+                                                           int64_t c0, int cells) {
   constexpr int E = Elem<T>::kPerFrag;
   const int P = 1 << v.shift, dh = v.dh;
-  const int head = blockIdx.x % v.n_kv, which = blockIdx.x / v.n_kv % 2, layer = blockIdx.x / v.n_kv / 2;
-  const int64_t at = c0 + (int64_t)blockIdx.y * P;                 // first cell of the page
-  const int live = min(P, cells - (int)blockIdx.y * P);            // its live cells
-  T* page = reinterpret_cast<T*>(v.base + l.a[blockIdx.y] * v.page() + (2 * layer + which) * v.half()) +
+  const int pg = blockIdx.x % n_pages, hd = blockIdx.x / n_pages;
+  const int head = hd % v.n_kv, which = hd / v.n_kv % 2, layer = hd / v.n_kv / 2;
+  const int64_t at = c0 + (int64_t)pg * P;                 // first cell of the page
+  const int live = min(P, cells - pg * P);            // its live cells
+  T* page = reinterpret_cast<T*>(v.base + l.a[pg] * v.page() + (2 * layer + which) * v.half()) +
             ((int64_t)head * dh << v.shift);
   T* sess = kv + ((int64_t)(2 * layer + which) * v.n_kv + head) * cap * dh;
   if (which == 0) {  // rows of a cell: [cell][dim] on both sides
     T* s0 = sess + at * dh;
     const int n = live * dh / E;
-    for (int u = threadIdx.x; u < n; u += 256) {
-      if (TO_PAGES)
-        reinterpret_cast<uint4*>(page)[u] = reinterpret_cast<const uint4*>(s0)[u];
-      else
-        reinterpret_cast<uint4*>(s0)[u] = reinterpret_cast<const uint4*>(page)[u];
+    const u32x4* src = reinterpret_cast<const u32x4*>(TO_PAGES ? s0 : page);
+    u32x4* dst = reinterpret_cast<u32x4*>(TO_PAGES ? page : s0);
+    for (int u0 = threadIdx.x; u0 < n; u0 += 4 * 256) {
+      u32x4 w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = src[min(u0 + k * 256, n - 1)];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (u0 + k * 256 < n) dst[u0 + k * 256] = w[k];
     }
     return;
   }
-  const int row = P / E;  // units of a V^T row of the page
-  for (int u = threadIdx.x; u < dh * row; u += 256) {
-    const int d = u / row, c = u % row * E;
-    if (c >= live) continue;
-    T* p = page + ((int64_t)d << v.shift) + c;
-    T* s = sess + d * cap + at + c;
-    T* dst = TO_PAGES ? p : s;
-    const T* src = TO_PAGES ? s : p;
-    if (c + E <= live) {
-      *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
-    } else {  // the cells past the last stay as they are
-      for (int e = 0; e < live - c; ++e) dst[e] = src[e];
+  // rows of a dim: P cells of the page, cap of the session; the live whole units, then what the
+  // last unit holds of live cells (the cells past the last stay as they are)
+  const int full = live / E, rs = v.shift - (E == 8 ? 3 : 2);  // 1 << rs units a row
+  for (int u0 = threadIdx.x; full && u0 < dh << rs; u0 += 4 * 256) {
+    u32x4 w[4];
+    T *p[4], *s[4];
+    bool ok[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int u = u0 + k * 256, d = u >> rs, c = u & ((1 << rs) - 1);
+      ok[k] = d < dh && c < full;
+      p[k] = page + (ok[k] ? ((d << v.shift) + c * E) : 0);
+      s[k] = sess + at + (ok[k] ? d * cap + c * E : 0);
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const u32x4*>(TO_PAGES ? s[k] : p[k]);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (ok[k]) *reinterpret_cast<u32x4*>(TO_PAGES ? p[k] : s[k]) = w[k];
   }
+  if (live % E)
+    for (int d = threadIdx.x; d < dh; d += 256)
+      for (int c = full * E; c < live; ++c) {
+        T* p = page + ((int64_t)d << v.shift) + c;
+        T* s = sess + d * cap + at + c;
+        if (TO_PAGES) *p = *s; else *s = *p;
+      }
 }
 
 template <typename T, int DH>
@@ -542,9 +569,9 @@ hipError_t page_session(const PageView& v, const PageList& l, int n, void* kv, i
                         bool to_pages, hipStream_t st) {
   if (n <= 0) return hipSuccess;
   if (n > kPageBatch) return hipErrorInvalidValue;
-  const dim3 grid(v.n_layers * 2 * v.n_kv, n), block(256);
+  const dim3 grid(v.n_layers * 2 * v.n_kv * n), block(256);
 #define SPP_SESSION(T, D) \
-  SPP_LAUNCH((page_session_kernel<T, D>), grid, block, 0, st, v, l, static_cast<T*>(kv), cap, c0, cells)
+  SPP_LAUNCH((page_session_kernel<T, D>), grid, block, 0, st, v, l, n, static_cast<T*>(kv), cap, c0, cells)
   if (v.elem == 2) {
     if (to_pages) SPP_SESSION(bf16_t, true); else SPP_SESSION(bf16_t, false);
   } else {

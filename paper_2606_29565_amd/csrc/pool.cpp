@@ -23,7 +23,7 @@ struct Seq {
   int summary_at = -1;          // length after the decode step whose summary is kept (-1: none)
 };
 
-using FreePages = std::priority_queue<int32_t, std::vector<int32_t>, std::greater<int32_t>>;
+using Lowest = std::priority_queue<int32_t, std::vector<int32_t>, std::greater<int32_t>>;
 
 }  // namespace
 
@@ -32,9 +32,10 @@ struct spp_pool_s {
   PageView v{};
   int device = 0;
   std::vector<int32_t> refs;     // sequences that list a page
-  FreePages free_pages;          // lowest first
+  Lowest free_pages;          // lowest first
   std::vector<Seq> seqs;
-  int n_seqs = 0;
+  Lowest free_seqs;           // sequence numbers, lowest first
+  int n_seqs = 0, n_shared = 0;
   ScanResult* summary = nullptr;  // device, one slot per sequence
   hipEvent_t done = nullptr;      // the pool's device work so far
   bool recorded = false;
@@ -100,7 +101,9 @@ int32_t take_page(spp_pool_s& p) {
 }
 
 void drop_page(spp_pool_s& p, int32_t pg) {
-  if (--p.refs[pg] == 0) p.free_pages.push(pg);
+  const int32_t left = --p.refs[pg];
+  if (left == 1) --p.n_shared;
+  if (left == 0) p.free_pages.push(pg);
 }
 
 void drop_pages_from(spp_pool_s& p, Seq& s, size_t first) {
@@ -108,15 +111,13 @@ void drop_pages_from(spp_pool_s& p, Seq& s, size_t first) {
   if (s.pages.size() > first) s.pages.resize(first);
 }
 
+// Takes the lowest free sequence number (the caller has counted that there is one).
 int32_t take_seq(spp_pool_s& p) {
-  for (int i = 0; i < p.cfg.max_seqs; ++i)
-    if (!p.seqs[i].live) {
-      p.seqs[i] = Seq{};
-      p.seqs[i].live = true;
-      ++p.n_seqs;
-      return i;
-    }
-  return -1;
+  const int32_t q = p.free_seqs.top();
+  p.free_seqs.pop();
+  p.seqs[q].live = true;
+  ++p.n_seqs;
+  return q;
 }
 
 // The pool's device work is one line: `st` continues after all of it, and note_work marks
@@ -174,7 +175,9 @@ spp_status reserve(spp_pool_s& p, int32_t n, const int32_t* seqs, int32_t cells,
   if (need > (int64_t)p.free_pages.size())
     return fail(SPP_E_CAPACITY, "%lld pages needed, %zu free", (long long)need, p.free_pages.size());
   std::vector<std::pair<int32_t, int32_t>> moves;
+  std::vector<int32_t*> moved;  // the table entries of the moves
   moves.reserve(n);  // (what can throw comes before the first change)
+  moved.reserve(n);
   for (int i = 0; i < n; ++i) p.seqs[seqs[i]].pages.reserve(pages_for(p, (int64_t)p.seqs[seqs[i]].n + cells));
   for (int i = 0; i < n; ++i) {
     Seq& s = p.seqs[seqs[i]];
@@ -183,6 +186,7 @@ spp_status reserve(spp_pool_s& p, int32_t n, const int32_t* seqs, int32_t cells,
       if (p.refs[pg] > 1) {
         const int32_t own = take_page(p);
         moves.push_back({pg, own});
+        moved.push_back(&pg);
         drop_page(p, pg);
         pg = own;
       }
@@ -190,7 +194,14 @@ spp_status reserve(spp_pool_s& p, int32_t n, const int32_t* seqs, int32_t cells,
     const int want = pages_for(p, (int64_t)s.n + cells);
     while ((int)s.pages.size() < want) s.pages.push_back(take_page(p));
   }
-  return copy_pages(p, moves, st);
+  const spp_status rc = copy_pages(p, moves, st);
+  if (rc != SPP_OK)  // the pages stay shared (each still has the reference of another)
+    for (size_t i = 0; i < moves.size(); ++i) {
+      drop_page(p, moves[i].second);
+      if (p.refs[moves[i].first]++ == 1) ++p.n_shared;
+      *moved[i] = moves[i].first;
+    }
+  return rc;
 }
 
 spp_status check_model(const spp_pool_s& p, const Model& m) {
@@ -332,8 +343,11 @@ spp_status spp_pool_create(const spp_pool_config* cfg, void* pages, size_t bytes
     p->refs.assign(cfg->n_pages, 0);
     std::vector<int32_t> all(cfg->n_pages);
     for (int32_t i = 0; i < cfg->n_pages; ++i) all[i] = i;
-    p->free_pages = FreePages(std::greater<int32_t>(), std::move(all));
+    p->free_pages = Lowest(std::greater<int32_t>(), std::move(all));
     p->seqs.resize(cfg->max_seqs);
+    std::vector<int32_t> numbers(cfg->max_seqs);
+    for (int32_t i = 0; i < cfg->max_seqs; ++i) numbers[i] = i;
+    p->free_seqs = Lowest(std::greater<int32_t>(), std::move(numbers));
     if (hipEventCreateWithFlags(&p->done, hipEventDisableTiming) != hipSuccess ||
         hipMalloc((void**)&p->summary, sizeof(ScanResult) * cfg->max_seqs) != hipSuccess)
       return fail(SPP_E_NOMEM, "pool resources");
@@ -352,7 +366,7 @@ spp_status spp_pool_info(spp_pool_t p, spp_pool_info_t* out) {
   std::lock_guard<std::mutex> lk(p->mu);
   out->n_pages = p->cfg.n_pages;
   out->used_pages = p->cfg.n_pages - (int32_t)p->free_pages.size();
-  out->shared_pages = (int32_t)std::count_if(p->refs.begin(), p->refs.end(), [](int32_t r) { return r > 1; });
+  out->shared_pages = p->n_shared;
   out->n_seqs = p->n_seqs;
   out->max_seqs = p->cfg.max_seqs;
   return SPP_OK;
@@ -384,6 +398,7 @@ spp_status spp_seq_free(spp_pool_t p, int32_t seq) {
     if (const spp_status rc = check_seq(*p, seq); rc != SPP_OK) return rc;
     drop_pages_from(*p, p->seqs[seq], 0);
     p->seqs[seq] = Seq{};
+    p->free_seqs.push(seq);
     --p->n_seqs;
     return SPP_OK;
   });
@@ -427,7 +442,11 @@ spp_status spp_seq_fork(spp_pool_t p, int32_t src, int32_t n, int32_t* seqs_out)
       p->seqs[q].pages = std::move(tables[i]);
       seqs_out[i] = q;
     }
-    for (int j = 0; j < held; ++j) p->refs[p->seqs[src].pages[j]] += n;
+    for (int j = 0; j < held; ++j) {
+      int32_t& r = p->refs[p->seqs[src].pages[j]];
+      if (r == 1) ++p->n_shared;
+      r += n;
+    }
     return SPP_OK;
   });
 }
@@ -489,7 +508,9 @@ spp_status spp_seq_import(spp_pool_t p, int32_t seq, spp_session_t s, void* stre
     while ((int)q.pages.size() < want) q.pages.push_back(take_page(*p));
     q.n = s->n_s;
     q.summary_at = -1;
-    return copy_session(*p, q.pages, q.n, *s, true, static_cast<hipStream_t>(stream));
+    const spp_status rc = copy_session(*p, q.pages, q.n, *s, true, static_cast<hipStream_t>(stream));
+    if (rc != SPP_OK) q.n = 0;  // (what a failed copy leaves are no cells)
+    return rc;
   });
 }
 
@@ -532,7 +553,7 @@ spp_status spp_pool_compact(spp_pool_t p, void* stream, int32_t* n_moved) {
     for (Seq& s : p->seqs)
       for (int32_t& pg : s.pages) pg = to[pg];
     for (const auto& mv : moves) std::swap(p->refs[mv.first], p->refs[mv.second]);
-    p->free_pages = FreePages(std::greater<int32_t>(), std::move(rest));
+    p->free_pages = Lowest(std::greater<int32_t>(), std::move(rest));
     if (n_moved) *n_moved = (int32_t)moves.size();
     return SPP_OK;
   });
