@@ -11,9 +11,9 @@
 // vocabulary) and counts those of its slice in LDS with integer atomics, whose order does not
 // matter.  The largest index of a bias entry is kept the same way, so the last entry of a token
 // counts.  Nothing of the vocabulary's size besides the logits is written, cleared or read again.
-// Measured (with the launch that merges the slices' reductions): 64 rows of 128256 27.0 us,
-// 2.4 TB/s; without lists and reductions 32 rows take 7.0 us, a copy of them 6.0.  One row is
-// launches and latency: 9.8 us.
+// Measured (with the launch that merges the slices' reductions): 64 rows of 128256 26.3 us,
+// 2.5 TB/s; without lists and reductions 32 rows take 7.0 us, a copy of them 6.0.  One row is
+// launches and latency: 9.6 us.
 #include "reduce.hpp"
 #include "paged.hpp"
 
@@ -55,14 +55,13 @@ __device__ __forceinline__ float adjust_one(float y, const Penalties& p, uint32_
 //
 // An instruction for every token of 32 rows of 128256 takes the chip 0.1 us: what counts is the
 // instructions each token costs.  So the few tokens with a penalty or bias are adjusted one at
-// a time: a thread puts its logits into LDS, goes over those of them that were counted, and
-// takes them back.  (64 rows of 128256 with 2000 tokens and 100 biases, with the summaries: a wave that
+// a time: a thread goes over those of its tokens that were counted, reads their logits again,
+// leaves the results where their counts were, and takes them from there.  (64 rows of 128256 with 2000 tokens and 100 biases, with the summaries: a wave that
 // adjusts all its tokens wherever one lane needs it 32.3 us, a list of the touched tokens made by
-// the counting 30.4, this 27.0.)
+// the counting 30.4, their logits kept in LDS 27.0, this 26.3.)
 template <int UNITS, int R>
 __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs, ScanPartial* parts) {
   constexpr int S = UNITS * 4 * kTpb;
-  __shared__ __align__(16) float xs[S];        // the slice's logits
   __shared__ __align__(16) uint32_t cnt[S];    // occurrences past the prompt; bit 31: in the prompt
   __shared__ __align__(16) uint32_t bias_at[S];  // last bias entry of the token, plus one
   __shared__ ScanPartial red[4];
@@ -146,7 +145,6 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
     uint32_t touched = 0;  // of the thread's own tokens, a bit each
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-      reinterpret_cast<float4*>(xs)[u * kTpb + tid] = make_float4(x[u][0], x[u][1], x[u][2], x[u][3]);
       uint4 c = reinterpret_cast<const uint4*>(cnt)[u * kTpb + tid];
       if (biased) {
         const uint4 b = reinterpret_cast<const uint4*>(bias_at)[u * kTpb + tid];
@@ -157,13 +155,16 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
     for (uint32_t todo = touched; todo; todo &= todo - 1) {
       const int f = __ffs(todo) - 1, at = 4 * (f / 4 * kTpb + tid) + f % 4;
       const uint32_t b = biased ? bias_at[at] : 0u;
-      xs[at] = adjust_one(xs[at], pen, cnt[at], b, b ? r.bias[b - 1] : 0.f);
+      cnt[at] = __float_as_uint(adjust_one(r.src[v0 + at], pen, cnt[at], b, b ? r.bias[b - 1] : 0.f));
     }
     if (touched)
 #pragma unroll
       for (int u = 0; u < UNITS; ++u) {
-        const float4 q = reinterpret_cast<const float4*>(xs)[u * kTpb + tid];
-        x[u][0] = q.x; x[u][1] = q.y; x[u][2] = q.z; x[u][3] = q.w;
+        const uint4 q = reinterpret_cast<const uint4*>(cnt)[u * kTpb + tid];
+        const uint32_t qs[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if ((touched >> (4 * u + e)) & 1u) x[u][e] = __uint_as_float(qs[e]);
       }
   }
 
@@ -281,8 +282,8 @@ __global__ __launch_bounds__(64) void adjust_merge_kernel(int nb, const ScanPart
 }
 
 // Tokens of a slice: 1024 while that makes under 2048 workgroups, else 2048, which halves how
-// often a history is read (64 rows of 128256 with 2000 tokens each: 27.0 us, with 1024 30.1;
-// 17 rows of 152063 with 700: 12.9 and 14.3).
+// often a history is read (64 rows of 128256 with 2000 tokens each: 26.3 us, with 1024 30.1;
+// 17 rows of 152063 with 700: 12.8 and 14.3).
 int slice_units(int n, int vocab) { return (int64_t)vocab * n <= 2048 * 1024 ? 1 : 2; }
 // Slices of a row, whatever its alignment.
 int slices(int units, int vocab) { return (vocab + 3 + units * 4 * kTpb - 1) / (units * 4 * kTpb); }
