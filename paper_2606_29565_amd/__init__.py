@@ -276,6 +276,14 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream
 
 
+def _stream_of(stream, device: int) -> Optional[int]:
+    """As _stream, with the current stream of that device for None."""
+    if stream is None:
+        import torch
+        return torch.cuda.current_stream(device).cuda_stream
+    return _stream(stream)
+
+
 def _host_i32(tokens) -> Tuple[ctypes.Array, int]:
     vals = [int(t) for t in tokens]
     arr = (ctypes.c_int32 * max(1, len(vals)))(*vals)
@@ -599,8 +607,9 @@ class PagePool:
             nbytes = lib().spp_pool_bytes(ctypes.byref(self.cfg))
             pages = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
         self.pages = pages
-        if not pages.is_contiguous():
-            raise ValueError("pages must be a contiguous tensor")
+        if not pages.is_contiguous() or not pages.is_cuda:
+            raise ValueError("pages must be a contiguous device tensor")
+        self.device = pages.get_device()
         h = ctypes.c_void_p()
         check(lib().spp_pool_create(ctypes.byref(self.cfg), ctypes.c_void_p(_ptr(pages)),
                                     pages.numel() * pages.element_size(), ctypes.byref(h)),
@@ -663,8 +672,8 @@ class PagePool:
     def reserve(self, seqs: Sequence[int], cells: int = 1, stream=None) -> None:
         """Makes the next `cells` cells of the sequences writable (spp_seq_reserve)."""
         arr, n = _host_i32(seqs)
-        check(lib().spp_seq_reserve(self.handle, n, arr, cells, ctypes.c_void_p(_stream(stream))),
-              "spp_seq_reserve")
+        check(lib().spp_seq_reserve(self.handle, n, arr, cells,
+                                    ctypes.c_void_p(_stream_of(stream, self.device))), "spp_seq_reserve")
 
     def commit(self, seq: int, cells: int) -> None:
         check(lib().spp_seq_commit(self.handle, seq, cells), "spp_seq_commit")
@@ -674,19 +683,19 @@ class PagePool:
 
     def import_session(self, seq: int, session: Session, stream=None) -> None:
         """The sequence becomes a copy of the session's committed cells (spp_seq_import)."""
-        check(lib().spp_seq_import(self.handle, seq, session.handle, ctypes.c_void_p(_stream(stream))),
-              "spp_seq_import")
+        check(lib().spp_seq_import(self.handle, seq, session.handle,
+                                   ctypes.c_void_p(_stream_of(stream, self.device))), "spp_seq_import")
 
     def export_session(self, seq: int, session: Session, stream=None) -> None:
         """The session's committed state becomes a copy of the sequence (spp_seq_export)."""
-        check(lib().spp_seq_export(self.handle, seq, session.handle, ctypes.c_void_p(_stream(stream))),
-              "spp_seq_export")
+        check(lib().spp_seq_export(self.handle, seq, session.handle,
+                                   ctypes.c_void_p(_stream_of(stream, self.device))), "spp_seq_export")
 
     def compact(self, stream=None) -> int:
         """Moves the used pages to the buffer's start (spp_pool_compact); how many moved."""
         n = ctypes.c_int32()
-        check(lib().spp_pool_compact(self.handle, ctypes.c_void_p(_stream(stream)), ctypes.byref(n)),
-              "spp_pool_compact")
+        check(lib().spp_pool_compact(self.handle, ctypes.c_void_p(_stream_of(stream, self.device)),
+                                     ctypes.byref(n)), "spp_pool_compact")
         return n.value
 
     def summaries(self, seqs: Sequence[int]) -> List[spp_summary]:
@@ -706,7 +715,7 @@ def decode_batch(pool: PagePool, model: Model, seqs: Sequence[int], tokens: Sequ
         raise ValueError("sequences, tokens and dists differ in number")
     ptrs = (ctypes.c_void_p * max(1, n))(*[_ptr(d) for d in dists])
     check(lib().spp_decode_batch(pool.handle, model.handle, n, arr, toks, ptrs,
-                                 ctypes.c_void_p(_stream(stream))), "spp_decode_batch")
+                                 ctypes.c_void_p(_stream_of(stream, pool.device))), "spp_decode_batch")
 
 
 def _row_stride(t, what: str) -> int:
@@ -718,15 +727,19 @@ def _row_stride(t, what: str) -> int:
 
 class PagedAttention:
     """spp_paged_attention over fixed tables: table [n][max_pages] and lengths [n] are int32
-    device tensors (their values may change between calls), the workspace is held here.  Each
-    call(q, out) is attention of one new token per sequence."""
+    device tensors (their values may change between calls), the workspace is held here: one
+    call at a time, and the object lives until its calls have finished.  Each call(q, out) is
+    attention of one new token per sequence, rows of [n_q_heads][head_dim]."""
 
     def __init__(self, pool: PagePool, layer: int, n_q_heads: int, table, lengths,
                  io_bf16: bool = True, scale: float = 0.0):
         import torch
+        self._dev = dev = pool.device
+        if table.get_device() != dev or lengths.get_device() != dev:
+            raise ValueError("table and lengths are on the pool's device")
         if table.dtype != torch.int32 or lengths.dtype != torch.int32 or table.dim() != 2 or \
                 lengths.shape != table.shape[:1] or not lengths.is_contiguous() or \
-                (table.numel() and table.stride(1) != 1):
+                (table.shape[1] > 1 and table.stride(1) != 1):
             raise ValueError("table [n][max_pages] and lengths [n]: int32, contiguous rows")
         n, width = table.shape
         self._keep = (pool, table, lengths)
@@ -748,10 +761,12 @@ class PagedAttention:
         if q.dtype != self._dtype or out.dtype != self._dtype or q.shape != self._shape or \
                 out.shape != self._shape:
             raise ValueError(f"q and out: {self._dtype} of shape {tuple(self._shape)}")
+        if q.get_device() != self._dev or out.get_device() != self._dev or not self._keep[0].handle:
+            raise ValueError("q and out are on the pool's device, the pool is open")
         a = self._a
         a.q, a.q_stride = q.data_ptr(), self._row if q.is_contiguous() else _row_stride(q, "q")
         a.out, a.out_stride = out.data_ptr(), self._row if out.is_contiguous() else _row_stride(out, "out")
-        rc = lib().spp_paged_attention(self._ref, self._wp, self._nb, ctypes.c_void_p(_stream(stream)))
+        rc = lib().spp_paged_attention(self._ref, self._wp, self._nb, ctypes.c_void_p(_stream_of(stream, self._dev)))
         if rc < 0:
             raise SppError(rc, "spp_paged_attention")
         return out
@@ -785,23 +800,29 @@ class AdjustSummaries:
         self.top1, self.top2, self.gap, self.lse = f[:, 1], f[:, 2], f[:, 3], f[:, 4]
 
 
-def _vector(t, dtype, least: int, row: int, what: str) -> Optional[int]:
-    """The device pointer of a contiguous tensor of at least `least` elements (None: no tensor)."""
+def _vector(t, dtype, least: int, dev: int, row: int, what: str) -> Optional[int]:
+    """The pointer of a contiguous tensor of at least `least` elements on device dev (None: none)."""
     if t is None:
         return None
-    if t.dtype != dtype or not t.is_contiguous() or t.numel() < least:
-        raise ValueError(f"row {row}: {what} is a contiguous {dtype} tensor of at least {least}")
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < least or t.get_device() != dev or dev < 0:
+        raise ValueError(f"row {row}: {what} is a contiguous {dtype} tensor of at least {least} "
+                         f"elements on the device of the first row")
     return t.data_ptr()
 
 
 class LogitsAdjust:
     """spp_adjust_logits with its rows marshalled once: each call() adjusts them and returns
-    their AdjustSummaries (None with summaries=False), which the next call overwrites."""
+    their AdjustSummaries (None with summaries=False), which the next call overwrites.  The
+    workspace is held here: one call at a time, and the object lives until its calls have
+    finished."""
 
     def __init__(self, vocab: int, rows: Sequence[AdjustRow], summaries: bool = True):
         import torch
         n = len(rows)
-        self.n, self._vocab, self._keep = n, vocab, list(rows)
+        self.n, self._keep = n, list(rows)
+        if any(r.src is None or r.dst is None for r in rows):
+            raise ValueError("a row has a src and a dst")
+        self._dev = dev = rows[0].src.get_device() if n else -1
         words = (vocab + 31) // 32
         self._rows = (spp_adjust * max(1, n))()
         for i, r in enumerate(rows):
@@ -811,26 +832,29 @@ class LogitsAdjust:
             nb = 0 if r.bias_tokens is None else r.bias_tokens.numel()
             if nb != (0 if r.bias is None else r.bias.numel()):
                 raise ValueError(f"row {i}: bias and bias_tokens differ in length")
-            if r.src is None or r.dst is None:
-                raise ValueError(f"row {i}: src and dst are needed")
             self._rows[i] = spp_adjust(
-                _vector(r.src, torch.float32, vocab, i, "src"), _vector(r.dst, torch.float32, vocab, i, "dst"),
-                _vector(r.tokens, torch.int32, nt, i, "tokens"),
-                _vector(r.bias_tokens, torch.int32, nb, i, "bias_tokens"),
-                _vector(r.bias, torch.float32, nb, i, "bias"),
-                _vector(r.allowed, torch.int32, words, i, "allowed"), nt, r.n_prompt, nb, r.repetition,
-                r.frequency, r.presence, r.fill)
+                _vector(r.src, torch.float32, vocab, dev, i, "src"),
+                _vector(r.dst, torch.float32, vocab, dev, i, "dst"),
+                _vector(r.tokens, torch.int32, nt, dev, i, "tokens"),
+                _vector(r.bias_tokens, torch.int32, nb, dev, i, "bias_tokens"),
+                _vector(r.bias, torch.float32, nb, dev, i, "bias"),
+                _vector(r.allowed, torch.int32, words, dev, i, "allowed"), nt, r.n_prompt, nb,
+                r.repetition, r.frequency, r.presence, r.fill)
         self._out, self._summ, nbytes = None, None, 0
         if summaries and n:
-            dev = rows[0].src.device
-            self._out = torch.empty(n, 7, dtype=torch.int32, device=dev)
+            self._out = torch.empty(n, 7, dtype=torch.int32, device=rows[0].src.device)
             self._summ = AdjustSummaries(self._out)
             nbytes = lib().spp_adjust_logits_work_bytes(n, vocab)
-            self._work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=dev)
+            self._work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self._out.device)
         self._args = (n, vocab, self._rows, ctypes.c_void_p(_ptr(self._out)),
                       ctypes.c_void_p(_ptr(self._work) if nbytes else 0), nbytes)
 
     def __call__(self, stream=None):
+        if not self.n:
+            return None
+        import torch
+        if torch.cuda.current_device() != self._dev:
+            raise ValueError(f"the rows are on device {self._dev}, which is not the current one")
         rc = lib().spp_adjust_logits(*self._args, ctypes.c_void_p(_stream(stream)))
         if rc < 0:
             raise SppError(rc, "spp_adjust_logits")

@@ -218,7 +218,7 @@ def test_refused_rows():
     for bad in (dict(src=x.double(), dst=x), dict(src=x[:50], dst=x), dict(src=x, dst=None),
                 dict(src=x, dst=x, tokens=t.long()), dict(src=x, dst=x, n_tokens=3),
                 dict(src=x, dst=x, tokens=t, n_tokens=5), dict(src=x, dst=x, bias_tokens=t),
-                dict(src=x, dst=x, allowed=t[:3])):
+                dict(src=x, dst=x, allowed=t[:3]), dict(src=x.cpu(), dst=x), dict(src=x, dst=x, tokens=t.cpu())):
         with pytest.raises((ValueError, AttributeError)):
             spp.LogitsAdjust(100, [spp.AdjustRow(**bad)])
     assert not x.any()

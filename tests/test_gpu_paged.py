@@ -431,3 +431,18 @@ def test_refusals_on_the_device():
         att(x.float(), x)
     flat = torch.zeros(4 * 64 + 8, device="cuda").bfloat16()
     refused(spp.SPP_E_INVALID_ARG, att, flat[1:257].view(1, 4, 64), torch.empty_like(x))  # misaligned
+    for bad in ((table.cpu(), lens), (table, lens.cpu()), (table.long(), lens), (table, lens[:0]), (table[0], lens)):
+        with pytest.raises(ValueError):
+            spp.PagedAttention(pool, 0, 4, *bad)
+    with pytest.raises(ValueError):
+        att(x.cpu(), x)
+    with pytest.raises(ValueError):
+        spp.PagePool(2, 2, 64, True, 16, 4, pages=torch.zeros(4 * 2 * 2 * 2 * 16 * 64 * 2, dtype=torch.uint8))
+    with pytest.raises(spp.SppError):
+        spp.PagePool(2, 2, 64, True, 16, 4, pages=torch.zeros(64, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(spp.SppError):
+        spp.PagePool(2, 2, 64, True, 24, 4)
+    pool.close()
+    with pytest.raises(ValueError):
+        att(x, torch.empty_like(x))
+    refused(spp.SPP_E_INVALID_ARG, spp.decode_batch, pool, b.model, [a], [1], d[:1])
