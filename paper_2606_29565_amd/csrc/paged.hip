@@ -524,19 +524,23 @@ namespace k {
 
 // Ranges of a sequence and kv head.  A range is at least one step of its workgroup's waves (256
 // cells in bf16, 128 in fp32).
-//  - A table of at most four such steps: one range, without the second launch (37 sequences of up
-//    to 700 cells, 2 heads of 64 in bf16: 8.0 us; in three ranges 5.2 and 3.6 for the join).
+//  - A table of two such steps at most: one range, without the second launch (a sequence of 256
+//    cells, 4 heads of 64 in fp32: 6.5 us, in two ranges 7.7), and one of four where
+//    the sequences and heads are 128 workgroups already (32 sequences of 1000 cells, 8 heads of
+//    128 in bf16, 256 workgroups: 27.8 us, in four ranges 32.9; 16 of them 19.1 and 17.4, of 700
+//    cells 14.5 and 16.0; one of them 17.7 and 9.8).
 //  - Else about 1024 workgroups over all, two rounds of two to a CU (three sequences of 32749
-//    cells, 8 heads of 128: 77 us; aiming at 2048 83, at 4096 89), but at least four ranges each, which even
-//    out sequences of unequal lengths (64 of U[1024, 8192] cells, 8 heads of 128: 220 us; two
-//    ranges each 230, three 225, eight 219; ranges of 1024 cells at most, however many 263).
+//    cells, 8 heads of 128: 77 us; aiming at 2048 83, at 4096 89), but up to four ranges of eight
+//    steps or more each, which even out sequences of unequal lengths (64 of U[1024, 8192] cells,
+//    8 heads of 128: 220 us; two ranges each 230, three 225, eight 219; ranges of 1024 cells at
+//    most, however many, 263; 128 of up to 2000 cells: one range 125 us, two 134, four 142).
 int paged_splits(const PageView& v, int n, int n_q, int max_pages) {
   const int tiles = (n_q / v.n_kv + 15) / 16;
   const int unit = (v.elem == 2 ? step_keys<bf16_t>() : step_keys<float>()) * kWaves;
-  const int64_t most = (((int64_t)max_pages << v.shift) + unit - 1) / unit;
-  if (most <= 4) return 1;
-  const int64_t want = std::max<int64_t>(4, 1024 / ((int64_t)n * v.n_kv * tiles));
-  return (int)std::min<int64_t>({want, most, (int64_t)kMaxSplits});
+  const int64_t most = (((int64_t)max_pages << v.shift) + unit - 1) / unit, wgs = (int64_t)n * v.n_kv * tiles;
+  if (most <= (wgs >= 128 ? 4 : 2)) return 1;
+  const int64_t want = std::max<int64_t>(std::min<int64_t>(4, most / 8), 1024 / wgs);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, (int64_t)kMaxSplits}));
 }
 
 size_t paged_work_bytes(const PageView& v, int n, int n_q, int max_pages) {
