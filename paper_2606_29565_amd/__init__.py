@@ -819,7 +819,7 @@ class LogitsAdjust:
     def __init__(self, vocab: int, rows: Sequence[AdjustRow], summaries: bool = True):
         import torch
         n = len(rows)
-        self.n, self._keep = n, list(rows)
+        self.n, self._keep, self._current_device = n, list(rows), torch.cuda.current_device
         if any(r.src is None or r.dst is None for r in rows):
             raise ValueError("a row has a src and a dst")
         self._dev = dev = rows[0].src.get_device() if n else -1
@@ -852,8 +852,7 @@ class LogitsAdjust:
     def __call__(self, stream=None):
         if not self.n:
             return None
-        import torch
-        if torch.cuda.current_device() != self._dev:
+        if self._current_device() != self._dev:
             raise ValueError(f"the rows are on device {self._dev}, which is not the current one")
         rc = lib().spp_adjust_logits(*self._args, ctypes.c_void_p(_stream(stream)))
         if rc < 0:

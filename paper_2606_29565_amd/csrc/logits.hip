@@ -11,8 +11,8 @@
 // vocabulary) and counts those of its slice in LDS with integer atomics, whose order does not
 // matter.  The largest index of a bias entry is kept the same way, so the last entry of a token
 // counts.  Nothing of the vocabulary's size besides the logits is written, cleared or read again.
-// Measured (with the launch that merges the slices' reductions): 64 rows of 128256 26.3 us,
-// 2.5 TB/s; without lists and reductions 32 rows take 7.0 us, a copy of them 6.0.  One row is
+// Measured (with the launch that merges the slices' reductions): 64 rows of 128256 23.8 us,
+// 2.8 TB/s; without lists and reductions 32 rows take 6.3 us, a copy of them 6.0.  One row is
 // launches and latency: 9.6 us.
 #include "reduce.hpp"
 #include "paged.hpp"
@@ -48,17 +48,47 @@ __device__ __forceinline__ float adjust_one(float y, const Penalties& p, uint32_
   return bias_at ? y + bias : y;
 }
 
+// The allowed bits of the unit whose first token is t, from the words of its first and last token
+// inside the row (before the row, t < 0, the first word is that of token 0).
+__device__ __forceinline__ uint32_t mask_bits(const uint32_t (&w)[2], int t) {
+  const uint32_t b = t >= 0 ? (uint32_t)((((uint64_t)w[1] << 32) | w[0]) >> (t & 31)) : w[0] << (-t & 3);
+  return b & 0xFu;
+}
+
+// A reduction over the wave in a fixed order, the result in every lane: within rows of 16 lanes,
+// then across them, by data-parallel moves (`none` comes in where a lane has no source).
+template <typename T, typename F>
+__device__ __forceinline__ T wave_reduce(T v, T none, F op) {
+  static_assert(sizeof(T) == 4, "one register");
+  const int n = __builtin_bit_cast(int, none);
+#define SPP_STEP(CTRL, ROWS)                                                              \
+  v = op(v, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(n, __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, false)))
+  SPP_STEP(0x111, 0xF);  // row_shr 1, 2, 4, 8: lane 15 of a row has its row's
+  SPP_STEP(0x112, 0xF);
+  SPP_STEP(0x114, 0xF);
+  SPP_STEP(0x118, 0xF);
+  SPP_STEP(0x142, 0xA);  // lane 15 of rows 0 and 2 to rows 1 and 3
+  SPP_STEP(0x143, 0xC);  // lane 31 to rows 2 and 3: lane 63 has all
+#undef SPP_STEP
+  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
 // Grid (slices, rows), UNITS * 1024 tokens a slice.  A row's tokens are cut into units of four
 // at 16-byte boundaries of src (unit u holds tokens 4u - a .. 4u - a + 3, a the elements that
 // src starts past such a boundary), so that all whole units are 16-byte accesses whatever the
 // row's alignment; unit u of the slice belongs to thread u % 256.
 //
 // An instruction for every token of 32 rows of 128256 takes the chip 0.1 us: what counts is the
-// instructions each token costs.  So the few tokens with a penalty or bias are adjusted one at
-// a time: a thread goes over those of its tokens that were counted, reads their logits again,
-// leaves the results where their counts were, and takes them from there.  (64 rows of 128256 with 2000 tokens and 100 biases, with the summaries: a wave that
-// adjusts all its tokens wherever one lane needs it 32.3 us, a list of the touched tokens made by
-// the counting 30.4, their logits kept in LDS 27.0, this 26.3.)
+// instructions each token costs.  So
+//  - the few tokens with a penalty or bias are adjusted one at a time: a thread goes over those
+//    of its tokens that were counted, reads their logits again, leaves the results where their
+//    counts were, and takes them from there;
+//  - a slice of whole units has a path without a look at the row's ends;
+//  - the reductions start from the wave's largest value (no running maximum, the index only where
+//    it is), by data-parallel moves.
+// 64 rows of 128256 with 2000 tokens and 100 biases, with the summaries: 23.8 us.  A wave that
+// adjusts all its tokens wherever one lane needs it 32.3; a list of the touched tokens made by
+// the counting 30.4; their logits kept in LDS 27.0; without the last two of these points 26.3.
 template <int UNITS, int R>
 __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs, ScanPartial* parts) {
   constexpr int S = UNITS * 4 * kTpb;
@@ -116,6 +146,7 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
       w[u][1] = r.allowed[min(max(t + 3, 0), V - 1) >> 5];
     }
 
+  constexpr uint32_t kAll = (1u << (4 * UNITS)) - 1;
   if (sparse) {
     const uint4 zero = make_uint4(0, 0, 0, 0);
 #pragma unroll
@@ -169,52 +200,52 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
   }
 
   // Masked and stored; then x holds the allowed values, -inf elsewhere.
-  uint32_t live = 0;  // a bit per value: in the row and allowed
-  bool odd = false;   // one of these is NaN or +-inf
+  uint32_t live = kAll;   // a bit per value: in the row and allowed
+  float low = INFINITY;   // the smallest allowed value
+  if (pair && v0 >= t_lo && v0 + S - 4 <= t_hi) {  // the slice is whole units
 #pragma unroll
-  for (int u = 0; u < UNITS; ++u) {
-    const int t = v0 + 4 * (u * kTpb + tid);
-    const bool whole = t >= t_lo && t <= t_hi;
-    uint32_t bits = 0xFu;
-    if (!whole) {
+    for (int u = 0; u < UNITS; ++u) {
+      const int t = v0 + 4 * (u * kTpb + tid);
+      float4* dst = reinterpret_cast<float4*>(r.dst + t);
+      if (masked) {
+        const uint32_t bits = mask_bits(w[u], t);
+        float y[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (t + e < 0 || t + e >= V) bits &= ~(1u << e);
+        for (int e = 0; e < 4; ++e) {
+          const bool ok = (bits >> e) & 1u;
+          y[e] = ok ? x[u][e] : r.fill;
+          low = fminf(low, ok ? x[u][e] : INFINITY);
+          x[u][e] = ok ? x[u][e] : -INFINITY;
+        }
+        *dst = make_float4(y[0], y[1], y[2], y[3]);
+        live = (live & ~(0xFu << (4 * u))) | bits << (4 * u);
+      } else {
+        *dst = make_float4(x[u][0], x[u][1], x[u][2], x[u][3]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) low = fminf(low, x[u][e]);
+      }
     }
-    const uint32_t in_row = bits;
-    float y[4] = {x[u][0], x[u][1], x[u][2], x[u][3]};
-    if (masked) {
-      // bits t & 31 and up of the two words side by side; before the row (t < 0, bits left out
-      // above) the first word is that of token 0
-      bits &= t >= 0 ? (uint32_t)((((uint64_t)w[u][1] << 32) | w[u][0]) >> (t & 31)) : w[u][0] << (-t & 3);
+  } else {
+    live = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = (bits >> e) & 1u ? y[e] : r.fill;
-    }
-    if (pair && whole) {
-      *reinterpret_cast<float4*>(r.dst + t) = make_float4(y[0], y[1], y[2], y[3]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if ((in_row >> e) & 1u) r.dst[t + e] = y[e];
-    }
-    if (masked || !whole) {
+    for (int u = 0; u < UNITS; ++u) {
+      const int t = v0 + 4 * (u * kTpb + tid);
+      const uint32_t bits = masked ? mask_bits(w[u], t) : 0xFu;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bool ok = (bits >> e) & 1u;
-        odd |= ok && !(fabsf(x[u][e]) < INFINITY);
+        const bool in = t + e >= 0 && t + e < V, ok = in && ((bits >> e) & 1u);
+        if (in) r.dst[t + e] = ok ? x[u][e] : r.fill;
+        low = fminf(low, ok ? x[u][e] : INFINITY);
         x[u][e] = ok ? x[u][e] : -INFINITY;
+        live |= (uint32_t)ok << (4 * u + e);
       }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) odd |= !(fabsf(x[u][e]) < INFINITY);
     }
-    live |= (bits & 0xFu) << (4 * u);
   }
   if (!parts) return;
 
-  // The slice's partial from the largest value on: the thread's two largest (v_max and v_med
-  // take NaN for none), the workgroup's largest; only where a thread holds it, its index; the
-  // sums of exponentials against it.
+  // The slice's partial, from the largest value on: the thread's two largest (v_max and v_med
+  // take NaN for none), the wave's largest, its index where a thread holds it, and the sum of
+  // exponentials against it.  Of what is not finite, NaN and +inf show in that sum, -inf in `low`.
   float v1 = -INFINITY, v2 = -INFINITY;
 #pragma unroll
   for (int u = 0; u < UNITS; ++u)
@@ -225,33 +256,34 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
       v1 = fmaxf(v1, y);
     }
   Acc acc;
-  acc.t = Top2{v1, v2, 0x7FFFFFFF};
-  acc.m = wave_max(v1);
+  acc.m = wave_reduce(v1, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
   acc.s = 0.f;
-  acc.nonfinite = odd;
-  if (v1 == acc.m && live) {
+  const int base = v0 + 4 * tid;
+  int at = 0x7FFFFFFF;  // of the thread's value equal to the wave's largest, the lowest index
+  if (acc.m > -INFINITY) {
+    int off = -1;
 #pragma unroll
     for (int u = UNITS - 1; u >= 0; --u)
 #pragma unroll
-      for (int e = 3; e >= 0; --e)
-        if ((live >> (4 * u + e)) & 1u && x[u][e] == v1) acc.t.i1 = v0 + 4 * (u * kTpb + tid) + e;
-  }
-  if (acc.m > -INFINITY) {
+      for (int e = 3; e >= 0; --e) off = x[u][e] == acc.m ? 4 * kTpb * u + e : off;
+    at = off >= 0 ? base + off : at;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc.s += __builtin_amdgcn_exp2f((x[u][e] - acc.m) * 1.44269504f);
-  }
-  // over the wave: the sums in a fixed order, the lowest index of the largest, the second
-  // largest among the others' largest and its holder's second
-  acc.s = wave_sum(acc.s);
-  int first = acc.t.i1;
+    acc.s = wave_reduce(acc.s, 0.f, [](float p, float q) { return p + q; });
+  } else if (live) {  // nothing above -inf: the first allowed -inf
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) first = min(first, __shfl_xor(first, o, 64));
-  acc.t.v2 = wave_max(first != 0x7FFFFFFF && acc.t.i1 == first ? v2 : v1);
-  acc.t.v1 = acc.m;
-  acc.t.i1 = first;
-  acc.nonfinite = __any(odd) ? 1u : 0u;
+    for (int u = UNITS - 1; u >= 0; --u)
+#pragma unroll
+      for (int e = 3; e >= 0; --e)
+        if ((live >> (4 * u + e)) & 1u && x[u][e] == x[u][e]) at = base + 4 * kTpb * u + e;
+  }
+  const int first = wave_reduce(at, 0x7FFFFFFF, [](int p, int q) { return min(p, q); });
+  // the second largest: among the others' largest and the holder's second
+  const float next = wave_reduce(at == first ? v2 : v1, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
+  acc.t = Top2{acc.m, next, first};
+  acc.nonfinite = __any(low == -INFINITY) || !(acc.s < INFINITY) || (acc.m == -INFINITY && __any(live != 0)) ? 1u : 0u;
   if ((tid & 63) == 0) red[tid >> 6] = to_partial(acc);
   __syncthreads();
   if (tid == 0) {
@@ -282,8 +314,9 @@ __global__ __launch_bounds__(64) void adjust_merge_kernel(int nb, const ScanPart
 }
 
 // Tokens of a slice: 1024 while that makes under 2048 workgroups, else 2048, which halves how
-// often a history is read (64 rows of 128256 with 2000 tokens each: 26.3 us, with 1024 30.1;
-// 17 rows of 152063 with 700: 12.8 and 14.3).
+// often a history is read and the instructions of a workgroup beside its tokens' own (64 rows of
+// 128256 with 2000 tokens each: 23.8 us; with slices of 4096, half as many waves to a CU, 25.1;
+// 17 rows of 152063 with 700: 12.2 and 12.3).
 int slice_units(int n, int vocab) { return (int64_t)vocab * n <= 2048 * 1024 ? 1 : 2; }
 // Slices of a row, whatever its alignment.
 int slices(int units, int vocab) { return (vocab + 3 + units * 4 * kTpb - 1) / (units * 4 * kTpb); }
