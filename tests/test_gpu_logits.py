@@ -142,6 +142,14 @@ def test_nonfinite_logits_ties_and_masked_values():
     plans.append((base, one))                               # one token: no second
     f = base.copy(); f[9] = -3.4028235e38
     plans.append((f, None))
+    g = base.copy(); g[4999] = 3.4028235e38; g[17] = -3.4028235e38
+    plans.append((g, None))                                 # the whole range of the type
+    h = base.copy(); h[20] = -np.inf
+    plans.append((h, None))                                 # an -inf among others
+    ok = np.zeros(V, bool); ok[[20, 21, 4000]] = True
+    plans.append((h, ok))                                   # ... and allowed
+    h2 = np.full(V, -np.inf, np.float32); h2[20] = np.nan
+    plans.append((h2, ok))                                  # nothing finite is allowed
     src = torch.stack([torch.from_numpy(p[0]) for p in plans]).cuda()
     rows = [spp.AdjustRow(src[i], src[i], allowed=None if p[1] is None else _bitmap(torch, p[1]), fill=-3.4028235e38)
             for i, p in enumerate(plans)]                   # in place
@@ -150,6 +158,23 @@ def test_nonfinite_logits_ties_and_masked_values():
         y, ok = _expect(p[0], allowed=p[1], fill=-3.4028235e38)
         assert np.array_equal(src[i].cpu().numpy(), y, equal_nan=True), i
         _check_row(y, ok, s, i)
+
+
+def test_the_same_call_gives_the_same_bits():
+    import torch
+    import paper_2606_29565_amd as spp
+    V, n = 60000, 70
+    g = torch.Generator(device="cuda").manual_seed(8)
+    src = torch.empty(n, V, device="cuda").normal_(0, 2, generator=g)
+    tok = torch.randint(0, 500, (n, 3000), generator=g, device="cuda").int()
+    got = []
+    for _ in range(3):
+        out = torch.empty_like(src)
+        s = spp.LogitsAdjust(V, [spp.AdjustRow(src[i], out[i], tokens=tok[i], n_prompt=1000, repetition=1.3,
+                                               frequency=0.01, presence=0.2) for i in range(n)])()
+        got.append((out, s.argmax.clone(), s.top1.clone(), s.top2.clone(), s.lse.clone()))
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
 
 
 def test_adjusted_logits_are_gated_and_replayed_from_a_graph():

@@ -73,6 +73,8 @@ CASES = [
     (6, 2, 64, False, True, 64, [129, 64], 0.0),
     (8, 8, 128, False, False, 16, [33, 200], 0.5),
     (16, 1, 64, True, False, 64, [16385], 0.0),
+    (12, 4, 128, False, False, 64, [1, 500, 4500], 0.1),
+    (32, 8, 128, True, False, 16, [700] * 20 + [1, 0, 1007], 0.0),   # one range to a sequence and head
 ]
 
 
@@ -147,6 +149,16 @@ def test_attention_rows_with_strides_and_workspace_of_garbage():
     plain = att(q.contiguous(), torch.empty(3, 4, 64, device="cuda").bfloat16())
     assert torch.equal(holder[:, 1:5], plain)
     assert bool((holder[:, 0] == 9).all()) and bool((holder[:, 5] == 9).all())
+
+
+def test_attention_of_no_sequence():
+    import torch
+    import paper_2606_29565_amd as spp
+    pool, _, _ = _pool(torch, spp, 1, 2, 64, True, 16, 4)
+    q = torch.empty(0, 4, 64, device="cuda").bfloat16()
+    table = torch.empty(0, 3, dtype=torch.int32, device="cuda")
+    att = spp.PagedAttention(pool, 0, 4, table, torch.empty(0, dtype=torch.int32, device="cuda"))
+    assert att(q, torch.empty_like(q)).shape == q.shape
 
 
 def test_attention_scale_and_offsets_past_32_bits():
