@@ -318,8 +318,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PageView v, 
 // Grid (query heads, sequences), 256 threads: the ranges of one head joined.  Thread s first
 // takes range s's factor; then DH / 4 threads cover the row and the groups of so many threads
 // take the ranges in turn, four of a thread's loads in flight; the groups' sums are added in
-// order.  (One thread a column and every range in a row took 20.7 us for the 64 to 128 ranges of one
-// long sequence, 128 x 32 heads; this takes 4.3.)
+// order.  (One thread a column and every range in a row took 20.7 us for 64 ranges of 32 heads of
+// 128; this takes 4.2.)
 template <int DH>
 __global__ __launch_bounds__(kMaxSplits) void paged_join_kernel(PagedAttn a, int shift, int splits, int unit,
                                                                 const float* o_part, const float2* ml_part) {
