@@ -552,7 +552,8 @@ spp_status spp_seq_summaries(spp_pool_t pool, int32_t n, const int32_t* seqs, sp
  * table[i][j / page_cells].  A table entry outside [0, n_pages) takes its cells out (a page
  * given up from the middle); lengths beyond max_pages*page_cells are cut to it, negative
  * ones are zero.  A sequence with no cell left gets zeros.  What lies in a page behind a sequence's
- * last cell, or in a page that is not listed, has no influence, NaN included.
+ * last cell, or in a page that is not listed, has no influence, NaN included (an infinite or
+ * NaN element of a live cell gives NaN where it is used).
  * The products of bf16 cells run on bf16 matrix cores with q (unless it is bf16) and p in
  * two bf16 parts and fp32 sums: about 16 significant bits of both. */
 typedef struct {
@@ -612,8 +613,9 @@ typedef struct {
 size_t spp_adjust_logits_work_bytes(int32_t n, int32_t vocab);
 /* Penalties for repeated tokens, biases and an allowed set (a grammar's next tokens) on n
  * rows of logits -- those of a resume or a decode step -- with the reductions a greedy step
- * reads.  rows: host array, read during the call.  Rows do not overlap, except a dst with its
- * own src; every pointer is on the current device.  summaries (nullable): device array of n
+ * reads.  rows: host array, read during the call.  No dst overlaps what another row reads or
+ * writes, nor its own row's src unless it is the same; every pointer is 4-byte aligned and on
+ * the current device.  summaries (nullable): device array of n
  * spp_summary: argmax (lowest index on ties), top1, top2, gap and lse over the adjusted
  * logits of the ALLOWED tokens, position 0, flags bit 0 if one of these is NaN or +-inf (lse
  * is then NaN; a NaN is never the argmax), bit 3 if no token is allowed (gap and lse are then

@@ -602,8 +602,8 @@ class PagePool:
                                    max_seqs)
         self.handle = None
         self._lib = lib()
+        import torch
         if pages is None:
-            import torch
             nbytes = lib().spp_pool_bytes(ctypes.byref(self.cfg))
             pages = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
         self.pages = pages
@@ -611,9 +611,10 @@ class PagePool:
             raise ValueError("pages must be a contiguous device tensor")
         self.device = pages.get_device()
         h = ctypes.c_void_p()
-        check(lib().spp_pool_create(ctypes.byref(self.cfg), ctypes.c_void_p(_ptr(pages)),
-                                    pages.numel() * pages.element_size(), ctypes.byref(h)),
-              "spp_pool_create")
+        with torch.cuda.device(self.device):  # (the pool is the current device's)
+            check(lib().spp_pool_create(ctypes.byref(self.cfg), ctypes.c_void_p(_ptr(pages)),
+                                        pages.numel() * pages.element_size(), ctypes.byref(h)),
+                  "spp_pool_create")
         self.handle = h
 
     def close(self) -> None:

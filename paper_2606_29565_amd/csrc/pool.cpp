@@ -275,6 +275,7 @@ struct PagedStep : StepCache {
 };
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
 spp_status check_attn(const spp_paged_attn* a) {
   if (!a || !a->pool) return fail(SPP_E_INVALID_ARG, "null argument");
@@ -295,6 +296,8 @@ spp_status check_attn(const spp_paged_attn* a) {
     return fail(SPP_E_INVALID_ARG, "rows of q and out: %lld elements at least, multiples of 8, 16-byte aligned",
                 (long long)row);
   if (a->table_stride < a->max_pages) return fail(SPP_E_INVALID_ARG, "table_stride < max_pages");
+  if (!aligned4(a->table) || !aligned4(a->lengths))
+    return fail(SPP_E_INVALID_ARG, "table and lengths are 4-byte aligned");
   return SPP_OK;
 }
 
@@ -647,6 +650,9 @@ spp_status spp_adjust_logits(int32_t n, int32_t vocab, const spp_adjust* rows, s
     if (!r.src || !r.dst || r.n_tokens < 0 || r.n_bias < 0 || (r.n_tokens && !r.tokens) ||
         (r.n_bias && (!r.bias_tokens || !r.bias)))
       return fail(SPP_E_INVALID_ARG, "row %d: null pointer or negative count", i);
+    if (!aligned4(r.src) || !aligned4(r.dst) || !aligned4(r.tokens) || !aligned4(r.bias_tokens) ||
+        !aligned4(r.bias) || !aligned4(r.allowed))
+      return fail(SPP_E_INVALID_ARG, "row %d: pointers are 4-byte aligned", i);
     if (r.n_tokens > (1 << 30) || r.n_bias > (1 << 30)) return fail(SPP_E_INVALID_ARG, "row %d: a list over 2^30", i);
     if (r.n_prompt < 0 || r.n_prompt > r.n_tokens) return fail(SPP_E_INVALID_ARG, "row %d: n_prompt", i);
     if (!(r.repetition > 0.f) || !std::isfinite(r.repetition) || !std::isfinite(r.frequency) ||
@@ -654,6 +660,7 @@ spp_status spp_adjust_logits(int32_t n, int32_t vocab, const spp_adjust* rows, s
       return fail(SPP_E_INVALID_ARG, "row %d: repetition must be > 0, penalties finite, fill a number", i);
   }
   if (n == 0) return SPP_OK;
+  if (!aligned4(summaries)) return fail(SPP_E_INVALID_ARG, "summaries are 4-byte aligned");
   const size_t need = summaries ? k::adjust_work_bytes(n, vocab) : 0;
   if (need && (!work || work_bytes < need || !aligned16(work)))
     return fail(SPP_E_INVALID_ARG, "workspace of %zu bytes, need %zu, 16-byte aligned", work ? work_bytes : 0, need);

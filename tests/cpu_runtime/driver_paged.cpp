@@ -413,7 +413,7 @@ void refusals() {
   CHECK(spp_paged_attention(&good, nullptr, need, nullptr) == SPP_E_INVALID_ARG);
   CHECK(spp_paged_attention(&good, (char*)x + 4, need, nullptr) == SPP_E_INVALID_ARG);
   CHECK(spp_paged_attention(nullptr, x, need, nullptr) == SPP_E_INVALID_ARG);
-  for (int bad = 0; bad < 18; ++bad) {
+  for (int bad = 0; bad < 20; ++bad) {
     spp_paged_attn c = good;
     switch (bad) {
       case 0: c.pool = nullptr; break;
@@ -433,6 +433,8 @@ void refusals() {
       case 14: c.lengths = nullptr; break;
       case 15: c.scale = INFINITY; break;
       case 16: c.out = (char*)x + 2; break;
+      case 18: c.table = (const int32_t*)((const char*)tab + 2); break;
+      case 19: c.lengths = (const int32_t*)((const char*)len + 1); break;
       case 17: c.n_q_heads = 65536; c.q_stride = c.out_stride = 1 << 23; break;
     }
     CHECK(spp_paged_attention_work_bytes(&c) == 0);
@@ -453,7 +455,7 @@ void refusals() {
   CHECK(spp_adjust_logits(1, kV, nullptr, nullptr, nullptr, 0, nullptr) == SPP_E_INVALID_ARG);
   CHECK(spp_adjust_logits(1, kV, &row, sum, nullptr, 0, nullptr) == SPP_E_INVALID_ARG);
   CHECK(spp_adjust_logits_work_bytes(0, kV) == 0 && spp_adjust_logits_work_bytes(1, -5) == 0);
-  for (int bad = 0; bad < 12; ++bad) {
+  for (int bad = 0; bad < 15; ++bad) {
     spp_adjust r = row;
     switch (bad) {
       case 0: r.src = nullptr; break;
@@ -468,6 +470,9 @@ void refusals() {
       case 9: r.frequency = NAN; break;
       case 10: r.presence = INFINITY; break;
       case 11: r.fill = NAN; break;
+      case 12: r.src = (const float*)((const char*)r.src + 2); break;
+      case 13: r.allowed = (const uint32_t*)((const char*)tab + 1); break;
+      case 14: r.tokens = tab; r.n_tokens = (1 << 30) + 1; break;
     }
     CHECK(spp_adjust_logits(1, kV, &r, nullptr, nullptr, 0, nullptr) == SPP_E_INVALID_ARG);
   }
