@@ -511,7 +511,8 @@ spp_status spp_seq_truncate(spp_pool_t pool, int32_t seq, int32_t n);
 
 /* The sequence becomes a copy of the session's committed cells (its former cells are given
  * up): every layer's cells [0, n_s) into pages of its own.  The session is only read.  Asynchronous
- * on `stream`, ordered after the device work of the session's model as well.
+ * on `stream`, ordered after the device work of the session's model as well, and before its
+ * next (as spp_seq_export).
  * SPP_E_INVALID_ARG unless the session's model has the pool's layers, kv heads, head_dim and
  * dtype and lives on its device; SPP_E_CAPACITY when the pages run out. */
 spp_status spp_seq_import(spp_pool_t pool, int32_t seq, spp_session_t session, void* stream);

@@ -37,12 +37,11 @@ struct spp_pool_s {
   Lowest free_seqs;           // sequence numbers, lowest first
   int n_seqs = 0, n_shared = 0;
   ScanResult* summary = nullptr;  // device, one slot per sequence
-  hipEvent_t done = nullptr;      // the pool's device work so far
+  std::shared_ptr<Event> done;    // the pool's device work so far; models may wait for it too
   bool recorded = false;
   std::mutex mu;                  // taken before a session's and a model's
   ~spp_pool_s() {
-    if (recorded) hipEventSynchronize(done);
-    if (done) hipEventDestroy(done);
+    if (recorded) hipEventSynchronize(done->ev);
     if (summary) hipFree(summary);
   }
 };
@@ -124,11 +123,11 @@ int32_t take_seq(spp_pool_s& p) {
 // what was enqueued since as its new end.
 spp_status order_after(spp_pool_s& p, hipStream_t st) {
   hipSetDevice(p.device);
-  if (p.recorded) HIPCHK(hipStreamWaitEvent(st, p.done, 0));
+  if (p.recorded) HIPCHK(hipStreamWaitEvent(st, p.done->ev, 0));
   return SPP_OK;
 }
 spp_status note_work(spp_pool_s& p, hipStream_t st) {
-  HIPCHK(hipEventRecord(p.done, st));
+  HIPCHK(hipEventRecord(p.done->ev, st));
   p.recorded = true;
   return SPP_OK;
 }
@@ -220,7 +219,7 @@ spp_status copy_session(spp_pool_s& p, const std::vector<int32_t>& pages, int n,
   Model& m = *s.m;
   std::lock_guard<std::mutex> mk(m.mu);
   if (const spp_status rc = order_after(p, st); rc != SPP_OK) return rc;
-  if (m.step_recorded) HIPCHK(hipStreamWaitEvent(st, m.step_done, 0));
+  if (const spp_status rc = after_steps(m, st); rc != SPP_OK) return rc;
   const int count = pages_for(p, n);
   for (int at = 0; at < count; at += kPageBatch) {
     PageList l;
@@ -230,9 +229,11 @@ spp_status copy_session(spp_pool_s& p, const std::vector<int32_t>& pages, int n,
     HIPCHK(k::page_session(p.v, l, c, s.kv, s.cap_stride, c0, (int)std::min<int64_t>(n - c0, (int64_t)c << p.v.shift),
                            to_pages, st));
   }
-  HIPCHK(hipEventRecord(m.step_done, st));
-  m.step_recorded = true;
-  return note_work(p, st);
+  // the model's next step waits for the pool's work up to then, which holds this copy and what
+  // the model waited for so far (later work of the pool too, until a step has run)
+  if (const spp_status rc = note_work(p, st); rc != SPP_OK) return rc;
+  m.copied = p.done;
+  return SPP_OK;
 }
 
 // The cells of a decode step's rows: row r is the new token of seqs[r], at its length.
@@ -351,7 +352,8 @@ spp_status spp_pool_create(const spp_pool_config* cfg, void* pages, size_t bytes
     std::vector<int32_t> numbers(cfg->max_seqs);
     for (int32_t i = 0; i < cfg->max_seqs; ++i) numbers[i] = i;
     p->free_seqs = Lowest(std::greater<int32_t>(), std::move(numbers));
-    if (hipEventCreateWithFlags(&p->done, hipEventDisableTiming) != hipSuccess ||
+    p->done = std::make_shared<Event>();
+    if (hipEventCreateWithFlags(&p->done->ev, hipEventDisableTiming) != hipSuccess ||
         hipMalloc((void**)&p->summary, sizeof(ScanResult) * cfg->max_seqs) != hipSuccess)
       return fail(SPP_E_NOMEM, "pool resources");
     *out = p.release();
@@ -608,7 +610,7 @@ spp_status spp_seq_summaries(spp_pool_t p, int32_t n, const int32_t* seqs, spp_s
       hi = std::max(hi, (int)seqs[i]);
     }
     std::vector<ScanResult> r(hi - lo + 1);
-    HIPCHK(hipEventSynchronize(p->done));
+    HIPCHK(hipEventSynchronize(p->done->ev));
     HIPCHK(hipMemcpy(r.data(), p->summary + lo, r.size() * sizeof(ScanResult), hipMemcpyDeviceToHost));
     for (int i = 0; i < n; ++i) fill_summary(r[seqs[i] - lo], p->seqs[seqs[i]].summary_at, out + i);
     return SPP_OK;

@@ -282,7 +282,7 @@ spp_status run_step(Model& m, const SegReq* segs, int nseg, bool logits, hipStre
   if (cache) cache->fill(m.params_host + off_cache, static_cast<char*>(m.params_dev.p) + off_cache);
 
   // ---- order after the previous step of this model, whatever stream it ran on
-  if (m.step_recorded) HIPCHK(hipStreamWaitEvent(st, m.step_done, 0));
+  if ((rc = after_steps(m, st)) != SPP_OK) return rc;
   const StepView dp = step_view(static_cast<const StepParams*>(m.params_dev.p), hp);
   HIPCHK(hipMemcpyAsync(m.params_dev.p, m.params_host, bytes, hipMemcpyHostToDevice, st));
   HIPCHK(hipEventRecord(m.params_free, st));
@@ -378,9 +378,7 @@ spp_status run_step(Model& m, const SegReq* segs, int nseg, bool logits, hipStre
       LAUNCH(KC_SCAN, k::scan(s, nseg, job, st));
     }
   }
-  HIPCHK(hipEventRecord(m.step_done, st));
-  m.step_recorded = true;
-  return SPP_OK;
+  return note_step(m, st);
 }
 
 spp_status check_tokens(const Model& m, const int32_t* t, int n) {
@@ -1243,11 +1241,11 @@ spp_status spp_shift(spp_session_t s, int32_t delta, void* stream) {
     std::lock_guard<std::mutex> mk(m.mu);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     // ordered after the model's last step on whatever stream it ran, and before the next
-    if (m.step_recorded) HIPCHK(hipStreamWaitEvent(st, m.step_done, 0));
+    spp_status rc = after_steps(m, st);
+    if (rc != SPP_OK) return rc;
     const hipError_t e = k::shift_cells(m.s, s->kv, s->cap_stride, n_new, delta, st);
     if (e != hipSuccess) return fail(SPP_E_HIP, "shift: %s", hipGetErrorString(e));
-    HIPCHK(hipEventRecord(m.step_done, st));
-    m.step_recorded = true;
+    if ((rc = note_step(m, st)) != SPP_OK) return rc;
   }
   s->n_s = n_new;
   return SPP_OK;

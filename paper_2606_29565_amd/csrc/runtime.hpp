@@ -32,6 +32,17 @@ struct DevBuf {
   size_t bytes = 0;
 };
 
+// An event that lives as long as one of those who wait for it.
+struct Event {
+  hipEvent_t ev = nullptr;
+  Event() = default;
+  Event(const Event&) = delete;
+  Event& operator=(const Event&) = delete;
+  ~Event() {
+    if (ev) hipEventDestroy(ev);
+  }
+};
+
 // Per-kernel timing for spp_profile_preposition (dispatch events, see LaunchRecorder).
 using Prof = LaunchRecorder;
 
@@ -78,6 +89,7 @@ struct Model {
   hipEvent_t step_done = nullptr;    // the last step has finished with the work buffers
   hipEvent_t chunk_end[2] = {};      // ends of the last two layer chunks of a yielding pass
   bool step_recorded = false;
+  std::shared_ptr<Event> copied;      // a pool has copied a session's cells since (null: none has)
   std::mutex mu;       // one step at a time per model (work buffers)
   std::mutex gate_mu;  // one gate scan at a time per model (gate buffers)
 };
@@ -142,6 +154,22 @@ struct StepCache {
   virtual hipError_t attention(int layer, const float* q, void* part, void* out, void* out_lo,
                                hipStream_t st) = 0;
 };
+
+// What touches the cells of a model's sessions is one line: `st` continues after all of it, and
+// note_step marks what was enqueued since as its new end.  (Copies of a pool mark it with the
+// event that the pool records anyway: a second record in a row costs the device 4 us.)  The
+// caller holds m.mu.
+inline spp_status after_steps(Model& m, hipStream_t st) {
+  if (m.step_recorded) HIPCHK(hipStreamWaitEvent(st, m.step_done, 0));
+  if (m.copied) HIPCHK(hipStreamWaitEvent(st, m.copied->ev, 0));
+  return SPP_OK;
+}
+inline spp_status note_step(Model& m, hipStream_t st) {
+  HIPCHK(hipEventRecord(m.step_done, st));
+  m.step_recorded = true;
+  m.copied.reset();
+  return SPP_OK;
+}
 
 spp_status run_step(Model& m, const SegReq* segs, int nseg, bool logits, hipStream_t st, Prof* prof,
                     YieldCtl* y = nullptr, StepCache* cache = nullptr);

@@ -5,14 +5,18 @@
 //      page counts with the tables, on two streams in turn;
 //   2. calls that are refused leave everything as it was;
 //   3. several threads share a pool and a model;
-//   4. the checks of the stand-alone calls.
+//   4. the checks of the stand-alone calls;
+//   5. a model's steps come after the copies of its sessions' cells, whatever streams and pools.
 // Prints "OK" and exits 0 when every check holds.
 #include <algorithm>
+#include <atomic>
+#include <chrono>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
 #include <map>
+#include <memory>
 #include <random>
 #include <set>
 #include <thread>
@@ -528,6 +532,59 @@ void threads() {
   CHECK(spp_pool_info(pool.p, &i) == SPP_OK && i.used_pages == 0 && i.n_seqs == 0);
 }
 
+// Copies on two streams by two pools, then a step of the model on a third: what is enqueued behind
+// the step sees all of it done.  A pool or the model may end first.
+void copies_then_steps() {
+  hipStream_t st[3];
+  for (hipStream_t& s : st) hipStreamCreate(&s);
+  for (int it = 0; it < 8; ++it) {
+    auto pool = std::make_unique<Pool>(16, 8, 2), other = std::make_unique<Pool>(32, 8, 2);
+    auto model = std::make_unique<Model>(1);
+    auto sess = std::make_unique<Sess>(model->m, 100);
+    sess->fill(std::vector<uint16_t>(40, 5));
+    int32_t q = -1, r = -1;
+    CHECK(spp_seq_create(pool->p, 0, &q) == SPP_OK && spp_seq_create(other->p, 0, &r) == SPP_OK);
+    int first = 0, second = 0;
+    bool seen = false, again = false;
+    const auto late = [](int* done) {
+      std::this_thread::sleep_for(std::chrono::milliseconds(5));
+      *done = 1;
+    };
+    stub::enqueue(st[0], [&] { late(&first); });
+    CHECK(spp_seq_import(pool->p, q, sess->s, st[0]) == SPP_OK);
+    if (it & 1) {  // the second pool's copy comes after the first's
+      CHECK(spp_seq_import(other->p, r, sess->s, st[1]) == SPP_OK);
+      stub::enqueue(st[1], [&] { again = first; });
+    }
+    stub::enqueue(st[1], [&] { late(&second); });
+    CHECK(spp_seq_export(it & 2 ? other->p : pool->p, it & 2 ? r : q, sess->s, st[1]) == SPP_OK);
+    if (it & 2 && !(it & 1)) CHECK(spp_session_restore(sess->s, 40) == SPP_OK);  // (r was empty)
+    const int32_t tok = 7;
+    if (it & 4)
+      CHECK(spp_shift(sess->s, 1, st[2]) == SPP_OK);
+    else
+      CHECK(spp_kv_append_delta(sess->s, &tok, 1, st[2]) == SPP_OK);
+    const bool empty = it & 2 && !(it & 1);  // (an export of no cells copies nothing)
+    stub::enqueue(st[2], [&] { seen = first && (empty || second); });
+    hipDeviceSynchronize();
+    CHECK(seen && again == (bool)(it & 1));
+    // once more behind that step, on the first stream
+    bool last = false;
+    stub::enqueue(st[2], [&] { late(&second); last = true; });
+    CHECK(spp_shift(sess->s, 1, st[2]) == SPP_OK);
+    CHECK(spp_seq_import(pool->p, q, sess->s, st[0]) == SPP_OK);
+    bool behind = false;
+    stub::enqueue(st[0], [&] { behind = last; });
+    hipDeviceSynchronize();
+    CHECK(behind);
+    sess.reset();
+    if (it & 1) model.reset();
+    pool.reset();
+    other.reset();
+  }
+  for (hipStream_t s : st) hipStreamDestroy(s);
+}
+
 }  // namespace
 
 int main() {
@@ -536,6 +593,7 @@ int main() {
   random_calls(2, 16, 14);
   random_calls(3, 32, 300);
   threads();
+  copies_then_steps();
   CHECK(stub::live_allocations() == 0);
   stub::shutdown();
   if (g_fail) return 1;
