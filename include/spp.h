@@ -561,13 +561,13 @@ typedef struct {
   spp_pool_t pool;
   int32_t layer;
   int32_t n_seqs;            /* 0..65535 (0: nothing is done)                             */
-  int32_t n_q_heads;         /* a multiple of the pool's n_kv_heads                       */
+  int32_t n_q_heads;         /* a multiple of the pool's n_kv_heads, at most 65535        */
   int32_t io_dtype;          /* spp_dtype of q and out                                    */
   const void* q;             /* device, [n_seqs] rows of [n_q_heads][head_dim]            */
   int64_t q_stride;          /* elements between rows, a multiple of 8; q 16-byte aligned */
   const int32_t* table;      /* device, [n_seqs] rows of max_pages page numbers           */
   int64_t table_stride;      /* entries between rows, >= max_pages                        */
-  int32_t max_pages;         /* >= 1; max_pages*page_cells < 2^31                         */
+  int32_t max_pages;         /* >= 1; max_pages*page_cells <= 2^30                        */
   const int32_t* lengths;    /* device, [n_seqs]                                          */
   float scale;               /* finite; 0 stands for 1 / sqrt(head_dim)                   */
   void* out;                 /* device, rows as q's                                       */
