@@ -81,8 +81,8 @@ __device__ __forceinline__ T wave_reduce(T v, T none, F op) {
 // An instruction for every token of 32 rows of 128256 takes the chip 0.1 us: what counts is the
 // instructions each token costs.  So
 //  - the few tokens with a penalty or bias are adjusted one at a time: a thread goes over those
-//    of its tokens that were counted, reads their logits again, leaves the results where their
-//    counts were, and takes them from there;
+//    of its tokens that were counted and picks each from its registers (read again from memory,
+//    with the results left where the counts were, 0.5 us longer for the 64 rows below);
 //  - a slice of whole units has a path without a look at the row's ends;
 //  - the reductions start from the wave's largest value (no running maximum, the index only where
 //    it is), by data-parallel moves.
@@ -185,18 +185,14 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
     }
     for (uint32_t todo = touched; todo; todo &= todo - 1) {
       const int f = __ffs(todo) - 1, at = 4 * (f / 4 * kTpb + tid) + f % 4;
-      const uint32_t b = biased ? bias_at[at] : 0u;
-      cnt[at] = __float_as_uint(adjust_one(r.src[v0 + at], pen, cnt[at], b, b ? r.bias[b - 1] : 0.f));
+      const uint32_t c = cnt[at], b = biased ? bias_at[at] : 0u;
+      float y = x[0][0];
+#pragma unroll
+      for (int k = 1; k < 4 * UNITS; ++k) y = f == k ? x[k / 4][k % 4] : y;
+      y = adjust_one(y, pen, c, b, b ? r.bias[b - 1] : 0.f);
+#pragma unroll
+      for (int k = 0; k < 4 * UNITS; ++k) x[k / 4][k % 4] = f == k ? y : x[k / 4][k % 4];
     }
-    if (touched)
-#pragma unroll
-      for (int u = 0; u < UNITS; ++u) {
-        const uint4 q = reinterpret_cast<const uint4*>(cnt)[u * kTpb + tid];
-        const uint32_t qs[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if ((touched >> (4 * u + e)) & 1u) x[u][e] = __uint_as_float(qs[e]);
-      }
   }
 
   // Masked and stored; then x holds the allowed values, -inf elsewhere.
