@@ -14,7 +14,7 @@
 // Measured (with the launch that merges the slices' reductions): 64 rows of 128256 23.8 us,
 // 2.8 TB/s; without lists and reductions 32 rows take 6.3 us, a copy of them 6.0.  One row is
 // launches and latency: 9.6 us.
-#include "reduce.hpp"
+#include "common.hpp"
 #include "paged.hpp"
 
 namespace spp {
@@ -73,6 +73,23 @@ __device__ __forceinline__ T wave_reduce(T v, T none, F op) {
   return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
+// The reductions over a part of a row travel as four words: the largest value (NaN left out), the
+// second largest, the first one's index as bits (the lowest; kNone without one), and the sum of
+// exp(value - largest), NaN if a value is not finite.
+constexpr int kNone = 0x7FFFFFFF;
+// What the sum of a part with largest value m counts in that of a whole with largest value `all`.
+__device__ __forceinline__ float part_weight(float m, float all) {
+  return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - all) * 1.44269504f);
+}
+__device__ __forceinline__ void part_merge(float4& a, const float4& b) {
+  const float m = fmaxf(a.x, b.x);
+  a.y = fmaxf(fmaxf(a.y, b.y), fminf(a.x, b.x));
+  const int ia = a.x == m ? __float_as_int(a.z) : kNone, ib = b.x == m ? __float_as_int(b.z) : kNone;
+  a.z = __int_as_float(min(ia, ib));
+  a.w = a.w * part_weight(a.x, m) + b.w * part_weight(b.x, m);
+  a.x = m;
+}
+
 // Grid (slices, rows), UNITS * 1024 tokens a slice.  A row's tokens are cut into units of four
 // at 16-byte boundaries of src (unit u holds tokens 4u - a .. 4u - a + 3, a the elements that
 // src starts past such a boundary), so that all whole units are 16-byte accesses whatever the
@@ -90,11 +107,11 @@ __device__ __forceinline__ T wave_reduce(T v, T none, F op) {
 // adjusts all its tokens wherever one lane needs it 32.3; a list of the touched tokens made by
 // the counting 30.4; their logits kept in LDS 27.0; without the last two of these points 26.3.
 template <int UNITS, int R>
-__global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs, ScanPartial* parts) {
+__global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs, float4* parts) {
   constexpr int S = UNITS * 4 * kTpb;
   __shared__ __align__(16) uint32_t cnt[S];    // occurrences past the prompt; bit 31: in the prompt
   __shared__ __align__(16) uint32_t bias_at[S];  // last bias entry of the token, plus one
-  __shared__ ScanPartial red[4];
+  __shared__ float4 red[4];
   const spp_adjust r = jobs.row[blockIdx.y];
   const Penalties pen{r.repetition, r.frequency, r.presence};
   const int tid = threadIdx.x;
@@ -239,7 +256,7 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
   }
   if (!parts) return;
 
-  // The slice's partial, from the largest value on: the thread's two largest (v_max and v_med
+  // The wave's part, from the largest value on: the thread's two largest (v_max and v_med
   // take NaN for none), the wave's largest, its index where a thread holds it, and the sum of
   // exponentials against it.  Of what is not finite, NaN and +inf show in that sum, -inf in `low`.
   float v1 = -INFINITY, v2 = -INFINITY;
@@ -251,23 +268,22 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
       v2 = __builtin_amdgcn_fmed3f(y, v1, v2);
       v1 = fmaxf(v1, y);
     }
-  Acc acc;
-  acc.m = wave_reduce(v1, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
-  acc.s = 0.f;
+  const float m = wave_reduce(v1, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
+  float sum = 0.f;
   const int base = v0 + 4 * tid;
-  int at = 0x7FFFFFFF;  // of the thread's value equal to the wave's largest, the lowest index
-  if (acc.m > -INFINITY) {
+  int at = kNone;  // of the thread's value equal to the wave's largest, the lowest index
+  if (m > -INFINITY) {
     int off = -1;
 #pragma unroll
     for (int u = UNITS - 1; u >= 0; --u)
 #pragma unroll
-      for (int e = 3; e >= 0; --e) off = x[u][e] == acc.m ? 4 * kTpb * u + e : off;
+      for (int e = 3; e >= 0; --e) off = x[u][e] == m ? 4 * kTpb * u + e : off;
     at = off >= 0 ? base + off : at;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc.s += __builtin_amdgcn_exp2f((x[u][e] - acc.m) * 1.44269504f);
-    acc.s = wave_reduce(acc.s, 0.f, [](float p, float q) { return p + q; });
+      for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((x[u][e] - m) * 1.44269504f);
+    sum = wave_reduce(sum, 0.f, [](float p, float q) { return p + q; });
   } else if (live) {  // nothing above -inf: the first allowed -inf
 #pragma unroll
     for (int u = UNITS - 1; u >= 0; --u)
@@ -275,37 +291,49 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
       for (int e = 3; e >= 0; --e)
         if ((live >> (4 * u + e)) & 1u && x[u][e] == x[u][e]) at = base + 4 * kTpb * u + e;
   }
-  const int first = wave_reduce(at, 0x7FFFFFFF, [](int p, int q) { return min(p, q); });
+  const int first = wave_reduce(at, kNone, [](int p, int q) { return min(p, q); });
   // the second largest: among the others' largest and the holder's second
   const float next = wave_reduce(at == first ? v2 : v1, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
-  acc.t = Top2{acc.m, next, first};
-  acc.nonfinite = __any(low == -INFINITY) || !(acc.s < INFINITY) || (acc.m == -INFINITY && __any(live != 0)) ? 1u : 0u;
-  if ((tid & 63) == 0) red[tid >> 6] = to_partial(acc);
+  const bool bad = __any(low == -INFINITY) || !(sum < INFINITY) || (m == -INFINITY && __any(live != 0));
+  const float4 mine = make_float4(m, next, __int_as_float(first), bad ? __builtin_nanf("") : sum);
+  if ((tid & 63) == 0) red[tid >> 6] = mine;
   __syncthreads();
   if (tid == 0) {
-    Acc all = from_partial(red[0]);
-    for (int k = 1; k < kTpb / 64; ++k) acc_merge<true>(all, from_partial(red[k]));
-    parts[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = to_partial(all);
+    float4 all = red[0];
+    for (int k = 1; k < kTpb / 64; ++k) part_merge(all, red[k]);
+    parts[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = all;
   }
 }
 
-// Grid (rows), one wave each: the slices' partials merged in a fixed order.
-__global__ __launch_bounds__(64) void adjust_merge_kernel(int nb, const ScanPartial* parts,
-                                                          spp_summary* out) {
-  Acc a;
-  acc_init(a);
-  for (int b = threadIdx.x; b < nb; b += 64) acc_merge<true>(a, from_partial(parts[(int64_t)blockIdx.x * nb + b]));
-  a = wave_acc<true>(a);
+// Grid (rows), one wave each: the slices' parts merged in a fixed order, lanes' own first, then
+// across the wave as above (merging pairs of lanes by shuffles took 1.0 to 1.4 us longer).
+__global__ __launch_bounds__(64) void adjust_merge_kernel(int nb, const float4* parts, spp_summary* out) {
+  parts += (int64_t)blockIdx.x * nb;
+  constexpr int AHEAD = 4;
+  float4 a = make_float4(-INFINITY, -INFINITY, __int_as_float(kNone), 0.f);
+  for (int b0 = threadIdx.x; b0 - (int)threadIdx.x < nb; b0 += AHEAD * 64) {
+    float4 p[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) p[u] = parts[min(b0 + u * 64, nb - 1)];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (b0 + u * 64 < nb) part_merge(a, p[u]);
+  }
+  const float m = wave_reduce(a.x, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
+  const float sum = wave_reduce(a.w * part_weight(a.x, m), 0.f, [](float p, float q) { return p + q; });
+  const int at = a.x == m ? __float_as_int(a.z) : kNone;
+  const int first = wave_reduce(at, kNone, [](int p, int q) { return min(p, q); });
+  const float next = wave_reduce(at == first ? a.y : a.x, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
   if (threadIdx.x) return;
-  const bool none = a.t.i1 == 0x7FFFFFFF;
+  const bool none = first == kNone, bad = sum != sum;
   spp_summary s;
-  s.argmax = none ? -1 : a.t.i1;
-  s.top1 = a.t.v1;
-  s.top2 = a.t.v2;
-  s.gap = a.t.v1 - a.t.v2;
-  s.lse = a.nonfinite || none ? __builtin_nanf("") : a.m + __logf(a.s);
+  s.argmax = none ? -1 : first;
+  s.top1 = m;
+  s.top2 = next;
+  s.gap = m - next;
+  s.lse = bad || none ? __builtin_nanf("") : m + __logf(sum);
   s.position = 0;
-  s.flags = (a.nonfinite ? 1u : 0u) | (none && !a.nonfinite ? 8u : 0u);
+  s.flags = (bad ? 1u : 0u) | (none && !bad ? 8u : 0u);
   out[blockIdx.x] = s;
 }
 
@@ -322,11 +350,11 @@ int slices(int units, int vocab) { return (vocab + 3 + units * 4 * kTpb - 1) / (
 namespace k {
 
 size_t adjust_work_bytes(int n, int vocab) {
-  return (size_t)n * slices(slice_units(n, vocab), vocab) * sizeof(ScanPartial);
+  return (size_t)n * slices(slice_units(n, vocab), vocab) * sizeof(float4);
 }
 
 template <int R>
-void launch_rows(int units, int nb, int m, int vocab, const spp_adjust* rows, ScanPartial* parts, hipStream_t st) {
+void launch_rows(int units, int nb, int m, int vocab, const spp_adjust* rows, float4* parts, hipStream_t st) {
   AdjustBatch<R> b{};
   for (int i = 0; i < m; ++i) b.row[i] = rows[i];
   if (units == 1)
@@ -340,14 +368,14 @@ hipError_t adjust_logits(int n, int vocab, const spp_adjust* rows, spp_summary* 
   const int units = slice_units(n, vocab), nb = slices(units, vocab);
   for (int r0 = 0; r0 < n; r0 += kManyRows) {
     const int m = n - r0 < kManyRows ? n - r0 : kManyRows;
-    ScanPartial* parts = summaries ? static_cast<ScanPartial*>(work) + (int64_t)r0 * nb : nullptr;
+    float4* parts = summaries ? static_cast<float4*>(work) + (int64_t)r0 * nb : nullptr;
     if (m <= kFewRows)
       launch_rows<kFewRows>(units, nb, m, vocab, rows + r0, parts, st);
     else
       launch_rows<kManyRows>(units, nb, m, vocab, rows + r0, parts, st);
   }
   if (summaries)
-    SPP_LAUNCH(adjust_merge_kernel, dim3(n), dim3(64), 0, st, nb, static_cast<const ScanPartial*>(work),
+    SPP_LAUNCH(adjust_merge_kernel, dim3(n), dim3(64), 0, st, nb, static_cast<const float4*>(work),
                summaries);
   return hipGetLastError();
 }
