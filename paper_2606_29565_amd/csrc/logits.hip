@@ -11,9 +11,8 @@
 // vocabulary) and counts those of its slice in LDS with integer atomics, whose order does not
 // matter.  The largest index of a bias entry is kept the same way, so the last entry of a token
 // counts.  Nothing of the vocabulary's size besides the logits is written, cleared or read again.
-// Measured (with the launch that merges the slices' reductions): 64 rows of 128256 23.8 us,
-// 2.8 TB/s; without lists and reductions 32 rows take 6.3 us, a copy of them 6.0.  One row is
-// launches and latency: 9.6 us.
+// Measured (with the launch that merges the slices' reductions): 64 rows of 128256 19.8 us,
+// 3.3 TB/s.  One row is launches and latency: 7.1 us from a graph, 10.2 through the binding.
 #include "common.hpp"
 #include "paged.hpp"
 
@@ -103,9 +102,10 @@ __device__ __forceinline__ void part_merge(float4& a, const float4& b) {
 //  - a slice of whole units has a path without a look at the row's ends;
 //  - the reductions start from the wave's largest value (no running maximum, the index only where
 //    it is), by data-parallel moves.
-// 64 rows of 128256 with 2000 tokens and 100 biases, with the summaries: 23.8 us.  A wave that
-// adjusts all its tokens wherever one lane needs it 32.3; a list of the touched tokens made by
-// the counting 30.4; their logits kept in LDS 27.0; without the last two of these points 26.3.
+// 64 rows of 128256 with 2000 tokens and 100 biases, with the summaries: 19.8 us.  Before the
+// stores' and the merge's own steps (then 23.1): a wave that adjusts all its tokens wherever one
+// lane needs it 32.3; a list of the touched tokens made by the counting 30.4; their logits kept
+// in LDS 27.0; without the last two of these points 26.3.
 template <int UNITS, int R>
 __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs, float4* parts) {
   constexpr int S = UNITS * 4 * kTpb;
@@ -341,8 +341,8 @@ __global__ __launch_bounds__(64) void adjust_merge_kernel(int nb, const float4* 
 
 // Tokens of a slice: 1024 while that makes under 2048 workgroups, else 2048, which halves how
 // often a history is read and the instructions of a workgroup beside its tokens' own (64 rows of
-// 128256 with 2000 tokens each: 23.8 us; with slices of 4096, half as many waves to a CU, 25.1;
-// 17 rows of 152063 with 700: 12.2 and 12.3).
+// 128256 with 2000 tokens each: 20.7 us, with slices of 1024 23.1, with slices of 4096, half as
+// many waves to a CU, 22.5; 17 rows of 152063 with 700: 10.1, 10.4 and 10.9).
 int slice_units(int n, int vocab) { return (int64_t)vocab * n <= 2048 * 1024 ? 1 : 2; }
 // Slices of a row, whatever its alignment.
 int slices(int units, int vocab) { return (vocab + 3 + units * 4 * kTpb - 1) / (units * 4 * kTpb); }
@@ -368,8 +368,11 @@ void launch_rows(int units, int nb, int m, int vocab, const spp_adjust* rows, fl
 hipError_t adjust_logits(int n, int vocab, const spp_adjust* rows, spp_summary* summaries, void* work,
                          hipStream_t st) {
   const int units = slice_units(n, vocab), nb = slices(units, vocab);
-  for (int r0 = 0; r0 < n; r0 += kManyRows) {
-    const int m = n - r0 < kManyRows ? n - r0 : kManyRows;
+  // launches of like size: what is left over a multiple of kManyRows would not fill the chip (64
+  // rows of 128256: 20.7 us as 48 and 16, 20.1 as 32 and 32)
+  const int launches = (n - 1) / kManyRows + 1, step = (n - 1) / launches + 1;
+  for (int r0 = 0; r0 < n; r0 += step) {
+    const int m = n - r0 < step ? n - r0 : step;
     float4* parts = summaries ? static_cast<float4*>(work) + (int64_t)r0 * nb : nullptr;
     if (m <= kFewRows)
       launch_rows<kFewRows>(units, nb, m, vocab, rows + r0, parts, st);
