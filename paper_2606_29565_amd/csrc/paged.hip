@@ -437,8 +437,10 @@ __global__ __launch_bounds__(256) void page_copy_kernel(PageView v, PageList l) 
 // Grid (pages of the list, fastest, times layers * 2 * kv heads): one head's keys or values of one
 // page, to or from the session's buffer, in 16-byte units.  Of the last page only the live
 // cells move.  (Neighbouring workgroups take neighbouring pages, so that the pieces of a V^T row
-// are read close in time: 8100 cells of 4 layers of the 8B shape, 265 MB, into pages of 64 in 55.9 us,
-// 4.7 TB/s; heads fastest 64.5.  Several pages to a workgroup: no shorter.)
+// are read close in time: 8100 cells of 4 layers of the 8B shape, 265 MB, into pages of 64 in 55.9 us;
+// heads fastest 64.5.  Several pages to a workgroup: no shorter.  The loads pass the L2 by, where
+// lines read once would only make room among the stores': 46.1 us, 5.8 TB/s, and 41.0 the other
+// way, 42.8 before.  Stores that pass it too: both ways together 97.5 us for 94.9.)
 template <typename T, bool TO_PAGES>
 __global__ __launch_bounds__(256) void page_session_kernel(PageView v, PageList l, int n_pages, T* kv, int64_t cap,
                                                            int64_t c0, int cells) {
@@ -459,7 +461,7 @@ __global__ __launch_bounds__(256) void page_session_kernel(PageView v, PageList 
     for (int u0 = threadIdx.x; u0 < n; u0 += 4 * 256) {
       u32x4 w[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) w[k] = src[min(u0 + k * 256, n - 1)];
+      for (int k = 0; k < 4; ++k) w[k] = __builtin_nontemporal_load(src + min(u0 + k * 256, n - 1));
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
@@ -482,7 +484,8 @@ __global__ __launch_bounds__(256) void page_session_kernel(PageView v, PageList 
       s[k] = sess + at + (ok[k] ? d * cap + c * E : 0);
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const u32x4*>(TO_PAGES ? s[k] : p[k]);
+    for (int k = 0; k < 4; ++k)
+      w[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(TO_PAGES ? s[k] : p[k]));
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
