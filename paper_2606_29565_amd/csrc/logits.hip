@@ -54,24 +54,6 @@ __device__ __forceinline__ uint32_t mask_bits(const uint32_t (&w)[2], int t) {
   return b & 0xFu;
 }
 
-// A reduction over the wave in a fixed order, the result in every lane: within rows of 16 lanes,
-// then across them, by data-parallel moves (`none` comes in where a lane has no source).
-template <typename T, typename F>
-__device__ __forceinline__ T wave_reduce(T v, T none, F op) {
-  static_assert(sizeof(T) == 4, "one register");
-  const int n = __builtin_bit_cast(int, none);
-#define SPP_STEP(CTRL, ROWS)                                                              \
-  v = op(v, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(n, __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, false)))
-  SPP_STEP(0x111, 0xF);  // row_shr 1, 2, 4, 8: lane 15 of a row has its row's
-  SPP_STEP(0x112, 0xF);
-  SPP_STEP(0x114, 0xF);
-  SPP_STEP(0x118, 0xF);
-  SPP_STEP(0x142, 0xA);  // lane 15 of rows 0 and 2 to rows 1 and 3
-  SPP_STEP(0x143, 0xC);  // lane 31 to rows 2 and 3: lane 63 has all
-#undef SPP_STEP
-  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
-}
-
 // The reductions over a part of a row travel as four words: the largest value (NaN left out), the
 // second largest, the first one's index as bits (the lowest; kNone without one), and the sum of
 // exp(value - largest), NaN if a value is not finite.

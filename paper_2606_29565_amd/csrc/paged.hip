@@ -126,14 +126,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PageView v, 
   const int k_begin = r0 + wave * share, k_end = min(r1, k_begin + share);
   const bool solo = range >= len;  // (an empty sequence: range 0, this writes its zeros)
 
+  // (a row past the last repeats that: its sums are this lane's alone and go nowhere)
   uint4 qh[NC], ql[NC];
+  const int64_t q_at = (int64_t)seq * a.q_stride + (int64_t)(q0 + min(i, nh - 1)) * DH + g * E;
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    qh[c] = ql[c] = make_uint4(0, 0, 0, 0);
-    if (i < nh)
-      query_frag(a.q, a.q_bf16, (int64_t)seq * a.q_stride + (int64_t)(q0 + i) * DH + c * KT + g * E, qh[c], ql[c],
-                 T{});
-  }
+  for (int c = 0; c < NC; ++c) query_frag(a.q, a.q_bf16, q_at + c * KT, qh[c], ql[c], T{});
   float m = -INFINITY, l = 0.f;
   f32x4 acc[ND];
 #pragma unroll
@@ -318,8 +315,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PageView v, 
 // Grid (query heads, sequences), 256 threads: the ranges of one head joined.  Thread s first
 // takes range s's factor; then DH / 4 threads cover the row and the groups of so many threads
 // take the ranges in turn, four of a thread's loads in flight; the groups' sums are added in
-// order.  (One thread a column and every range in a row took 20.7 us for 64 ranges of 32 heads of
-// 128; this takes 4.2.)
+// order.  Latency bounds it: no load waits for another.  (64 ranges of 32 heads of 128: one thread a
+// column and every range in a row 20.7 us, the groups 4.2; with the length, the factors and
+// the sums loaded one after the other and reductions by shuffles, 0.7 us longer than this.)
 template <int DH>
 __global__ __launch_bounds__(kMaxSplits) void paged_join_kernel(PagedAttn a, int shift, int splits, int unit,
                                                                 const float* o_part, const float2* ml_part) {
@@ -327,35 +325,42 @@ __global__ __launch_bounds__(kMaxSplits) void paged_join_kernel(PagedAttn a, int
   __shared__ float f_lds[kMaxSplits], w_max[4], w_sum[4];
   __shared__ float4 o_lds[GRPS][COLS];
   const int h = blockIdx.x, seq = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int col = tid % COLS, grp = tid / COLS;
+  const int64_t at = ((int64_t)seq * a.n_q + h) * splits;
+  // The length, the factors and the first sums are on their way together: of a range that the
+  // length does not reach, whatever the workspace holds is loaded and left out.
+  const float4* op = reinterpret_cast<const float4*>(o_part + at * DH) + col;
+  float2 ml = ml_part[at + min(tid, splits - 1)];
+  float4 v[4];
+  auto sums = [&](int s0) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = op[(int64_t)min(s0 + u * GRPS, splits - 1) * COLS];
+  };
+  sums(grp);
   const int len = live_cells(a, shift, seq);
   const int range = range_cells(len, splits, unit);
   if (range >= len) return;  // one range: its workgroup has written the output
   const int n = (len + range - 1) / range;
-  const int64_t at = ((int64_t)seq * a.n_q + h) * splits;
-  const float2 ml = tid < n ? ml_part[at + tid] : make_float2(-INFINITY, 0.f);
-  float M = wave_max(ml.x);
+  ml = tid < n ? ml : make_float2(-INFINITY, 0.f);
+  float M = wave_reduce(ml.x, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
   if (lane == 0) w_max[wave] = M;
   __syncthreads();
   M = fmaxf(fmaxf(w_max[0], w_max[1]), fmaxf(w_max[2], w_max[3]));
   const float f = __builtin_amdgcn_exp2f(ml.x - (M == -INFINITY ? 0.f : M));
   f_lds[tid] = f;
-  const float part = wave_sum(f * ml.y);
+  const float part = wave_reduce(f * ml.y, 0.f, [](float p, float q) { return p + q; });
   if (lane == 0) w_sum[wave] = part;
   __syncthreads();
   const float L = w_sum[0] + w_sum[1] + w_sum[2] + w_sum[3];
-  const int col = tid % COLS, grp = tid / COLS;
-  const float4* op = reinterpret_cast<const float4*>(o_part + at * DH) + col;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s0 = grp; s0 < n; s0 += 4 * GRPS) {
-    float4 v[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = op[(int64_t)min(s0 + u * GRPS, n - 1) * COLS];
+  for (int s0 = grp; s0 - grp < n; s0 += 4 * GRPS) {
 #pragma unroll
     for (int u = 0; u < 4; ++u)
       if (s0 + u * GRPS < n) {
         const float w = f_lds[s0 + u * GRPS];
         o = make_float4(o.x + w * v[u].x, o.y + w * v[u].y, o.z + w * v[u].z, o.w + w * v[u].w);
       }
+    if (s0 - grp + 4 * GRPS < n) sums(s0 + 4 * GRPS);
   }
   o_lds[grp][col] = o;
   __syncthreads();
