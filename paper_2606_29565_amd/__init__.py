@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import math
+import operator
 import os
 from typing import Dict, List, Optional, Sequence, Tuple
 
@@ -250,6 +251,12 @@ class YieldFlag:
 
     def is_set(self) -> bool:
         return self._word.value != 0
+
+
+def _unconverted(name: str):
+    """The function as called with ctypes objects of its types (and int32 as int): without the
+    conversion of every argument, 0.07 us each, for calls made in numbers."""
+    return lib()[name]
 
 
 def check(rc: int, where: str) -> int:
@@ -590,7 +597,7 @@ def gate_batch(readies: Sequence[Ready], taus: Sequence[float], bitmaps, stream=
     return [(outs[i], toks[i]) for i in range(n)]
 
 
-_ShortTable = ctypes.c_int32 * 64
+_ShortTable = ctypes.c_int32 * 65  # 64 pages and their number
 
 
 class PagePool:
@@ -603,7 +610,7 @@ class PagePool:
                                    SPP_DTYPE_BF16 if bf16 else SPP_DTYPE_F32, page_cells, n_pages,
                                    max_seqs)
         self.handle = None
-        self._lib = lib()
+        self._free, self._table = _unconverted("spp_seq_free"), _unconverted("spp_seq_table")
         import torch
         if pages is None:
             nbytes = lib().spp_pool_bytes(ctypes.byref(self.cfg))
@@ -648,7 +655,7 @@ class PagePool:
         return q.value
 
     def free(self, seq: int) -> None:
-        rc = self._lib.spp_seq_free(self.handle, seq)
+        rc = self._free(self.handle, operator.index(seq))
         if rc < 0:
             raise SppError(rc, "spp_seq_free")
 
@@ -659,12 +666,14 @@ class PagePool:
 
     def table(self, seq: int) -> List[int]:
         """The sequence's page numbers."""
-        n, t = ctypes.c_int32(), _ShortTable()
-        if self._lib.spp_seq_table(self.handle, seq, t, len(t), ctypes.byref(n)) < 0:  # a longer one?
-            check(self._lib.spp_seq_table(self.handle, seq, None, 0, ctypes.byref(n)), "spp_seq_table")
+        t, seq = _ShortTable(), operator.index(seq)
+        if self._table(self.handle, seq, t, 64, ctypes.byref(t, 256)) < 0:  # a longer one?
+            n = ctypes.c_int32()
+            check(self._table(self.handle, seq, None, 0, ctypes.byref(n)), "spp_seq_table")
             t = (ctypes.c_int32 * max(1, n.value))()
-            check(self._lib.spp_seq_table(self.handle, seq, t, n.value, ctypes.byref(n)), "spp_seq_table")
-        return t[:n.value]
+            check(self._table(self.handle, seq, t, len(t), ctypes.byref(n)), "spp_seq_table")
+            return t[:n.value]
+        return t[:t[64]]
 
     def fork(self, seq: int, n: int = 1) -> List[int]:
         """n sequences that share the pages of `seq` until they are written (spp_seq_fork)."""
@@ -756,9 +765,9 @@ class PagedAttention:
                                  lengths.data_ptr(), scale, dummy, row)
         nbytes = lib().spp_paged_attention_work_bytes(ctypes.byref(self._a))
         self._work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=table.device)
-        self._ref = ctypes.byref(self._a)
-        self._wp = ctypes.c_void_p(self._work.data_ptr())
-        self._nb = self._work.numel()
+        self._call = _unconverted("spp_paged_attention")
+        self._args = (ctypes.byref(self._a), ctypes.c_void_p(self._work.data_ptr()),
+                      ctypes.c_size_t(self._work.numel()))
 
     def __call__(self, q, out, stream=None):
         if q.dtype != self._dtype or out.dtype != self._dtype or q.shape != self._shape or \
@@ -769,7 +778,7 @@ class PagedAttention:
         a = self._a
         a.q, a.q_stride = q.data_ptr(), self._row if q.is_contiguous() else _row_stride(q, "q")
         a.out, a.out_stride = out.data_ptr(), self._row if out.is_contiguous() else _row_stride(out, "out")
-        rc = lib().spp_paged_attention(self._ref, self._wp, self._nb, ctypes.c_void_p(_stream_of(stream, self._dev)))
+        rc = self._call(*self._args, ctypes.c_void_p(_stream_of(stream, self._dev)))
         if rc < 0:
             raise SppError(rc, "spp_paged_attention")
         return out
@@ -850,14 +859,15 @@ class LogitsAdjust:
             nbytes = lib().spp_adjust_logits_work_bytes(n, vocab)
             self._work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self._out.device)
         self._args = (n, vocab, self._rows, ctypes.c_void_p(_ptr(self._out)),
-                      ctypes.c_void_p(_ptr(self._work) if nbytes else 0), nbytes)
+                      ctypes.c_void_p(_ptr(self._work) if nbytes else 0), ctypes.c_size_t(nbytes))
+        self._call = _unconverted("spp_adjust_logits")
 
     def __call__(self, stream=None):
         if not self.n:
             return None
         if self._current_device() != self._dev:
             raise ValueError(f"the rows are on device {self._dev}, which is not the current one")
-        rc = lib().spp_adjust_logits(*self._args, ctypes.c_void_p(_stream_of(stream, self._dev)))
+        rc = self._call(*self._args, ctypes.c_void_p(_stream_of(stream, self._dev)))
         if rc < 0:
             raise SppError(rc, "spp_adjust_logits")
         return self._summ
