@@ -190,23 +190,31 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-// A reduction over the wave in a fixed order, the result in every lane: within rows of 16 lanes,
-// then across them, by data-parallel moves (`none` comes in where a lane has no source).
-template <typename T, typename F>
-__device__ __forceinline__ T wave_reduce(T v, T none, F op) {
-  static_assert(sizeof(T) == 4, "one register");
-  const int n = __builtin_bit_cast(int, none);
-#define SPP_STEP(CTRL, ROWS)                                                              \
-  v = op(v, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(n, __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, false)))
-  SPP_STEP(0x111, 0xF);  // row_shr 1, 2, 4, 8: lane 15 of a row has its row's
-  SPP_STEP(0x112, 0xF);
-  SPP_STEP(0x114, 0xF);
-  SPP_STEP(0x118, 0xF);
-  SPP_STEP(0x142, 0xA);  // lane 15 of rows 0 and 2 to rows 1 and 3
-  SPP_STEP(0x143, 0xC);  // lane 31 to rows 2 and 3: lane 63 has all
-#undef SPP_STEP
-  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+// Reductions over the wave in a fixed order, the result in every lane: within rows of 16 lanes (lane
+// 15 of a row has its row's), then lane 15 of rows 0 and 2 to rows 1 and 3, then lane 31 to rows 2
+// and 3 (lane 63 has all), by data-parallel moves that are an operand of the operation itself: a
+// lane without a source keeps its value.  Two wait states come before the use of a result by
+// such a move, and one before readlane.  NaN is left out by the maximum.
+#define SPP_WAVE_STEP(OP, MOVE, ROWS) "s_nop 1\n\t" OP "_dpp %0, %0, %0 " MOVE " row_mask:" ROWS " bank_mask:0xf\n\t"
+#define SPP_WAVE_REDUCE(OP, V)                                                                             \
+  asm(SPP_WAVE_STEP(OP, "row_shr:1", "0xf") SPP_WAVE_STEP(OP, "row_shr:2", "0xf")                          \
+          SPP_WAVE_STEP(OP, "row_shr:4", "0xf") SPP_WAVE_STEP(OP, "row_shr:8", "0xf")                      \
+              SPP_WAVE_STEP(OP, "row_bcast:15", "0xa") SPP_WAVE_STEP(OP, "row_bcast:31", "0xc") "s_nop 1"  \
+      : "+v"(V))
+__device__ __forceinline__ float wave_max_all(float v) {
+  SPP_WAVE_REDUCE("v_max_f32", v);
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
+__device__ __forceinline__ int wave_min_all(int v) {
+  SPP_WAVE_REDUCE("v_min_i32", v);
+  return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ __forceinline__ float wave_sum_all(float v) {
+  SPP_WAVE_REDUCE("v_add_f32", v);
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+#undef SPP_WAVE_REDUCE
+#undef SPP_WAVE_STEP
 
 // Top-2 of a distribution: the largest value with its lowest index, and the second largest
 // value (equal to the first where that occurs twice).  NaN is never a candidate (the callers

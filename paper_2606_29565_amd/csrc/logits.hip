@@ -11,8 +11,8 @@
 // vocabulary) and counts those of its slice in LDS with integer atomics, whose order does not
 // matter.  The largest index of a bias entry is kept the same way, so the last entry of a token
 // counts.  Nothing of the vocabulary's size besides the logits is written, cleared or read again.
-// Measured (with the launch that merges the slices' reductions): 64 rows of 128256 19.8 us,
-// 3.3 TB/s.  One row is launches and latency: 7.1 us from a graph, 10.2 through the binding.
+// Measured (with the launch that merges the slices' reductions): 64 rows of 128256 19.2 us,
+// 3.4 TB/s.  One row is launches and latency: 6.9 us from a graph, 8 through the binding.
 #include "common.hpp"
 #include "paged.hpp"
 
@@ -84,7 +84,7 @@ __device__ __forceinline__ void part_merge(float4& a, const float4& b) {
 //  - a slice of whole units has a path without a look at the row's ends;
 //  - the reductions start from the wave's largest value (no running maximum, the index only where
 //    it is), by data-parallel moves.
-// 64 rows of 128256 with 2000 tokens and 100 biases, with the summaries: 19.8 us.  Before the
+// 64 rows of 128256 with 2000 tokens and 100 biases, with the summaries: 19.2 us.  Before the
 // stores' and the merge's own steps (then 23.1): a wave that adjusts all its tokens wherever one
 // lane needs it 32.3; a list of the touched tokens made by the counting 30.4; their logits kept
 // in LDS 27.0; without the last two of these points 26.3.
@@ -120,20 +120,29 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
   // first tokens of the row's first and last whole units (no whole unit: t_hi < t_lo)
   const int t_lo = a ? 4 - a : 0, t_hi = ((V + a) & ~3) - 4 - a;
   float x[UNITS][4];
-  if (t_lo <= t_hi)
+  const bool whole = v0 >= t_lo && v0 + S - 4 <= t_hi;  // the slice has no end of the row
+  if (whole) {
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-      const int t = min(max(v0 + 4 * (u * kTpb + tid), t_lo), t_hi);
-      const float4 q = *reinterpret_cast<const float4*>(r.src + t);
+      const float4 q = *reinterpret_cast<const float4*>(r.src + v0 + 4 * (u * kTpb + tid));
       x[u][0] = q.x; x[u][1] = q.y; x[u][2] = q.z; x[u][3] = q.w;
     }
-  // the row's first and last unit, where they are not whole
+  } else {
+    if (t_lo <= t_hi)
 #pragma unroll
-  for (int u = 0; u < UNITS; ++u) {
-    const int t = v0 + 4 * (u * kTpb + tid);
-    if ((t < t_lo || t > t_hi) && t + 3 >= 0 && t < V)
+      for (int u = 0; u < UNITS; ++u) {
+        const int t = min(max(v0 + 4 * (u * kTpb + tid), t_lo), t_hi);
+        const float4 q = *reinterpret_cast<const float4*>(r.src + t);
+        x[u][0] = q.x; x[u][1] = q.y; x[u][2] = q.z; x[u][3] = q.w;
+      }
+    // the row's first and last unit, where they are not whole
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[u][e] = r.src[min(max(t + e, 0), V - 1)];
+    for (int u = 0; u < UNITS; ++u) {
+      const int t = v0 + 4 * (u * kTpb + tid);
+      if ((t < t_lo || t > t_hi) && t + 3 >= 0 && t < V)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[u][e] = r.src[min(max(t + e, 0), V - 1)];
+    }
   }
   uint32_t w[UNITS][2];
   if (masked)
@@ -155,17 +164,20 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
     }
     __syncthreads();
     // (a slice's tokens below 0 or from V on are none of the row's: entries there are skipped)
-    const int lo = max(v0, 0), hi = min(v0 + S, V);
-    for (int i0 = tid; i0 - tid < n_tokens; i0 += AHEAD * kTpb) {
+    const int lo = max(v0, 0), hi = max(lo, min(v0 + S, V));  // (the last slice may be behind the row)
+    for (int i0 = 0; i0 < n_tokens; i0 += AHEAD * kTpb) {
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u)
-        if (i0 + u * kTpb < n_tokens && tok[u] >= lo && tok[u] < hi) {
-          if (i0 + u * kTpb < r.n_prompt)
-            atomicOr(cnt + (tok[u] - v0), 0x80000000u);
+      for (int u = 0; u < AHEAD; ++u) {
+        const uint32_t off = (uint32_t)tok[u] - (uint32_t)lo;
+        if (tid < n_tokens - i0 - u * kTpb && off < (uint32_t)(hi - lo)) {
+          uint32_t* c = cnt + (lo - v0) + off;
+          if (tid < r.n_prompt - i0 - u * kTpb)
+            atomicOr(c, 0x80000000u);
           else
-            atomicAdd(cnt + (tok[u] - v0), 1u);
+            atomicAdd(c, 1u);
         }
-      if (i0 - tid + AHEAD * kTpb < n_tokens) tokens_at(i0 + AHEAD * kTpb);
+      }
+      if (i0 + AHEAD * kTpb < n_tokens) tokens_at(i0 + AHEAD * kTpb + tid);
     }
     for (int i = tid; i - tid < r.n_bias; i += kTpb) {
       if (i < r.n_bias && bt >= lo && bt < hi) atomicMax(bias_at + (bt - v0), (uint32_t)i + 1);
@@ -199,7 +211,7 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
   // the next (64 rows of 128256: 22.9 us so, 20.7 past it; loads past it too 21.8).
   uint32_t live = kAll;   // a bit per value: in the row and allowed
   float low = INFINITY;   // the smallest allowed value
-  if (pair && v0 >= t_lo && v0 + S - 4 <= t_hi) {  // the slice is whole units
+  if (pair && whole) {
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
       const int t = v0 + 4 * (u * kTpb + tid);
@@ -248,11 +260,11 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
   for (int u = 0; u < UNITS; ++u)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float y = fmaxf(x[u][e], -INFINITY);  // (NaN -> -inf)
+      const float y = fmaxf(x[u][e], -INFINITY);  // (NaN, a signalling one too, -> -inf)
       v2 = __builtin_amdgcn_fmed3f(y, v1, v2);
       v1 = fmaxf(v1, y);
     }
-  const float m = wave_reduce(v1, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
+  const float m = wave_max_all(v1);
   float sum = 0.f;
   const int base = v0 + 4 * tid;
   int at = kNone;  // of the thread's value equal to the wave's largest, the lowest index
@@ -267,7 +279,7 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
     for (int u = 0; u < UNITS; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((x[u][e] - m) * 1.44269504f);
-    sum = wave_reduce(sum, 0.f, [](float p, float q) { return p + q; });
+    sum = wave_sum_all(sum);
   } else if (live) {  // nothing above -inf: the first allowed -inf
 #pragma unroll
     for (int u = UNITS - 1; u >= 0; --u)
@@ -275,9 +287,9 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
       for (int e = 3; e >= 0; --e)
         if ((live >> (4 * u + e)) & 1u && x[u][e] == x[u][e]) at = base + 4 * kTpb * u + e;
   }
-  const int first = wave_reduce(at, kNone, [](int p, int q) { return min(p, q); });
+  const int first = wave_min_all(at);
   // the second largest: among the others' largest and the holder's second
-  const float next = wave_reduce(at == first ? v2 : v1, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
+  const float next = wave_max_all(at == first ? v2 : v1);
   const bool bad = __any(low == -INFINITY) || !(sum < INFINITY) || (m == -INFINITY && __any(live != 0));
   const float4 mine = make_float4(m, next, __int_as_float(first), bad ? __builtin_nanf("") : sum);
   if ((tid & 63) == 0) red[tid >> 6] = mine;
@@ -303,11 +315,11 @@ __global__ __launch_bounds__(64) void adjust_merge_kernel(int nb, const float4* 
     for (int u = 0; u < AHEAD; ++u)
       if (b0 + u * 64 < nb) part_merge(a, p[u]);
   }
-  const float m = wave_reduce(a.x, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
-  const float sum = wave_reduce(a.w * part_weight(a.x, m), 0.f, [](float p, float q) { return p + q; });
+  const float m = wave_max_all(a.x);
+  const float sum = wave_sum_all(a.w * part_weight(a.x, m));
   const int at = a.x == m ? __float_as_int(a.z) : kNone;
-  const int first = wave_reduce(at, kNone, [](int p, int q) { return min(p, q); });
-  const float next = wave_reduce(at == first ? a.y : a.x, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
+  const int first = wave_min_all(at);
+  const float next = wave_max_all(at == first ? a.y : a.x);
   if (threadIdx.x) return;
   const bool none = first == kNone, bad = sum != sum;
   spp_summary s;

@@ -342,13 +342,13 @@ __global__ __launch_bounds__(kMaxSplits) void paged_join_kernel(PagedAttn a, int
   if (range >= len) return;  // one range: its workgroup has written the output
   const int n = (len + range - 1) / range;
   ml = tid < n ? ml : make_float2(-INFINITY, 0.f);
-  float M = wave_reduce(ml.x, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
+  float M = wave_max_all(ml.x);
   if (lane == 0) w_max[wave] = M;
   __syncthreads();
   M = fmaxf(fmaxf(w_max[0], w_max[1]), fmaxf(w_max[2], w_max[3]));
   const float f = __builtin_amdgcn_exp2f(ml.x - (M == -INFINITY ? 0.f : M));
   f_lds[tid] = f;
-  const float part = wave_reduce(f * ml.y, 0.f, [](float p, float q) { return p + q; });
+  const float part = wave_sum_all(f * ml.y);
   if (lane == 0) w_sum[wave] = part;
   __syncthreads();
   const float L = w_sum[0] + w_sum[1] + w_sum[2] + w_sum[3];

@@ -72,7 +72,7 @@ def _check_row(y, ok, s, i):
 
 @pytest.mark.parametrize("V,n,offset", [(1, 1, 0), (2, 3, 1), (31, 2, 3), (1023, 5, 2), (1024, 1, 0), (1025, 33, 1),
                                         (4096, 4, 0), (50021, 40, 3), (128256, 1, 0), (152063, 9, 0),
-                                        (128256, 64, 0)])
+                                        (128256, 64, 0), (1022, 6, 0), (129022, 17, 0)])
 def test_rows_match_their_steps_bit_for_bit(V, n, offset):
     """(`offset`: elements past a 16-byte boundary, src and dst unlike each other for odd rows.)"""
     import torch
@@ -150,6 +150,8 @@ def test_nonfinite_logits_ties_and_masked_values():
     plans.append((h, ok))                                   # ... and allowed
     h2 = np.full(V, -np.inf, np.float32); h2[20] = np.nan
     plans.append((h2, ok))                                  # nothing finite is allowed
+    k = base.copy(); k.view(np.uint32)[[4, 4998]] = 0x7FA00000, 0xFFA00001
+    plans.append((k, None))                                 # signalling NaN, one beside the largest
     src = torch.stack([torch.from_numpy(p[0]) for p in plans]).cuda()
     rows = [spp.AdjustRow(src[i], src[i], allowed=None if p[1] is None else _bitmap(torch, p[1]), fill=-3.4028235e38)
             for i, p in enumerate(plans)]                   # in place
