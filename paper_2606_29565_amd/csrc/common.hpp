@@ -194,7 +194,8 @@ __device__ __forceinline__ float wave_max(float v) {
 // 15 of a row has its row's), then lane 15 of rows 0 and 2 to rows 1 and 3, then lane 31 to rows 2
 // and 3 (lane 63 has all), by data-parallel moves that are an operand of the operation itself: a
 // lane without a source keeps its value.  Two wait states come before the use of a result by
-// such a move, and one before readlane.  NaN is left out by the maximum.
+// such a move, and one before readlane (a value straight from a matrix instruction would need
+// more).  NaN is left out by the maximum.
 #define SPP_WAVE_STEP(OP, MOVE, ROWS) "s_nop 1\n\t" OP "_dpp %0, %0, %0 " MOVE " row_mask:" ROWS " bank_mask:0xf\n\t"
 #define SPP_WAVE_REDUCE(OP, V)                                                                             \
   asm(SPP_WAVE_STEP(OP, "row_shr:1", "0xf") SPP_WAVE_STEP(OP, "row_shr:2", "0xf")                          \
