@@ -747,6 +747,8 @@ class PagedAttention:
                  io_bf16: bool = True, scale: float = 0.0):
         import torch
         self._dev = dev = pool.device
+        if not pool.handle:
+            raise ValueError("the pool is closed")
         if table.get_device() != dev or lengths.get_device() != dev:
             raise ValueError("table and lengths are on the pool's device")
         if table.dtype != torch.int32 or lengths.dtype != torch.int32 or table.dim() != 2 or \

@@ -458,3 +458,31 @@ def test_refusals_on_the_device():
     with pytest.raises(ValueError):
         att(x, torch.empty_like(x))
     refused(spp.SPP_E_INVALID_ARG, spp.decode_batch, pool, b.model, [a], [1], d[:1])
+    with pytest.raises(ValueError):
+        spp.PagedAttention(pool, 0, 4, table, lens)
+
+
+def test_tables_of_any_length_and_numbers_of_any_kind():
+    import numpy as np
+    import paper_2606_29565_amd as spp
+    pool = spp.PagePool(1, 1, 64, True, 16, 150, max_seqs=4)
+    for n in (0, 1, 63, 64, 65):                   # pages
+        q = pool.create(16 * n)
+        assert pool.table(q) == pool.table(np.int64(q)) == list(range(n))
+        pool.free(np.int32(q))
+        for f in (pool.table, pool.free):
+            with pytest.raises(spp.SppError):
+                f(q)                               # given back
+    q = pool.create(16 * 150)
+    assert pool.table(q) == list(range(150)) and pool.info().used_pages == 150
+    for f in (pool.table, pool.free):
+        for bad in ("0", None, 0.0):
+            with pytest.raises(TypeError):
+                f(bad)
+        for bad in (-1, 3, 4):
+            with pytest.raises(spp.SppError):
+                f(bad)
+    pool.close()
+    for f in (pool.table, pool.free):
+        with pytest.raises(spp.SppError):
+            f(q)
