@@ -301,6 +301,48 @@ def test_import_and_export_of_a_session(bf16, page, n):
     pool.close()
 
 
+def test_a_session_changes_after_its_copy_on_another_stream():
+    """A copy that starts late on one stream, then a shift of the same cells on another, and back."""
+    import torch
+    import paper_2606_29565_amd as spp
+    shape = synth.Shape("pages", 2, 256, 4, 2, 64, 512, 2048, 1e4, "bf16")
+    b = build_model(shape, 3)
+    n = 4000
+    sess = spp.Session(b.model, n + 8)
+    fill_synthetic_kv(b, sess, 5, n)
+    sess.restore(n)
+    pool, pages, _ = _pool(torch, spp, 2, 2, 64, True, 64, 200)
+    first, second, third = (pool.create() for _ in range(3))
+    pool.import_session(first, sess)
+    want = [[c.clone() for c in _cells(torch, spp, pool, pages, first, l, n)] for l in range(2)]
+    torch.cuda.synchronize()
+    late, other = torch.cuda.Stream(), torch.cuda.Stream()
+    a = torch.randn(4096, 4096, device="cuda")
+
+    def delay():
+        with torch.cuda.stream(late):
+            x = a
+            for _ in range(30):
+                x = torch.tanh(x @ a)
+        return x
+
+    torch.cuda.synchronize()
+    busy = delay()
+    pool.import_session(second, sess, stream=late)
+    sess.shift(1, stream=other)                            # waits for the copy
+    pool.export_session(first, sess, stream=other)
+    busy = delay()
+    pool.compact(stream=late)
+    pool.import_session(third, sess, stream=late)          # waits for the export
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(busy).all()) and sess.info().n_committed == n
+    for seq in (second, third):
+        for l in range(2):
+            got = _cells(torch, spp, pool, pages, seq, l, n)
+            assert all(torch.equal(x, y) for x, y in zip(got, want[l])), (seq, l)
+    pool.close()
+
+
 # ---- the decode step ------------------------------------------------------------------------
 
 
