@@ -428,8 +428,10 @@ spp_status spp_gate_batch_noalloc(int32_t n, const spp_ready_t* ready, const flo
  * the call's stream and ordered after that of the pool's earlier calls on whatever stream,
  * so a page freed and taken again is not written while earlier work reads it.  A pool's
  * calls may come from several threads: they are serialized.  Work that a caller enqueues on
- * the pages by itself (spp_paged_attention too) is the caller's to order.  A pool's calls are
- * not for capture into a graph (spp_paged_attention is). */
+ * the pages by itself (spp_paged_attention too) is the caller's to order: on the stream of a
+ * spp_seq_reserve it follows the pool's earlier calls, and later calls have to be put behind
+ * it (their stream, or an event).  A pool's calls are not for capture into a graph
+ * (spp_paged_attention is). */
 typedef struct spp_pool_s* spp_pool_t;
 
 typedef struct {
@@ -479,7 +481,9 @@ spp_status spp_pool_destroy(spp_pool_t pool);
 spp_status spp_pool_info(spp_pool_t pool, spp_pool_info_t* out);
 
 /* A sequence of n_cells cells with pages of its own, whose contents the caller has written
- * or will write (0: an empty one).  Pages are taken lowest number first, here and below.
+ * or will write (0: an empty one).  No stream waits here: earlier work of the pool may still
+ * use these pages, and a caller that cannot rule it out starts with 0 cells, reserves and
+ * commits.  Pages are taken lowest number first, here and below.
  * SPP_E_CAPACITY when the pages or the sequence numbers run out (then nothing changes, as
  * for every call below). */
 spp_status spp_seq_create(spp_pool_t pool, int32_t n_cells, int32_t* seq_out);
@@ -500,7 +504,8 @@ spp_status spp_seq_fork(spp_pool_t pool, int32_t src, int32_t n, int32_t* seqs_o
  * last cell shares with another sequence is copied to a page of their own (one launch for
  * all), and pages are added to their tables.  Lengths do not change.  spp_decode_batch does
  * this for its one cell; a caller that writes cells itself reserves, writes and then calls
- * spp_seq_commit.  Asynchronous on `stream`.  SPP_E_CAPACITY when the pages run out. */
+ * spp_seq_commit.  Asynchronous on `stream`, on which what is enqueued next follows the
+ * pool's earlier work, also where nothing is copied.  SPP_E_CAPACITY when the pages run out. */
 spp_status spp_seq_reserve(spp_pool_t pool, int32_t n, const int32_t* seqs, int32_t cells,
                            void* stream);
 /* Declares the next `cells` reserved cells written: n_cells <- n_cells + cells.

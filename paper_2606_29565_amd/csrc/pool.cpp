@@ -133,9 +133,9 @@ spp_status note_work(spp_pool_s& p, hipStream_t st) {
 }
 
 // Copies pages: (source, destination) pairs, no page both; batches travel as launch arguments.
+// `st` already continues the pool's line.
 spp_status copy_pages(spp_pool_s& p, const std::vector<std::pair<int32_t, int32_t>>& moves, hipStream_t st) {
   if (moves.empty()) return SPP_OK;
-  if (const spp_status rc = order_after(p, st); rc != SPP_OK) return rc;
   for (size_t at = 0; at < moves.size(); at += kPageBatch) {
     PageList l;
     const int n = (int)std::min<size_t>(kPageBatch, moves.size() - at);
@@ -149,7 +149,8 @@ spp_status copy_pages(spp_pool_s& p, const std::vector<std::pair<int32_t, int32_
 }
 
 // Makes the next `cells` cells of the sequences writable (spp_seq_reserve).  Nothing changes
-// unless the pages suffice.
+// unless the pages suffice.  `st` continues after the pool's work also where nothing is copied:
+// earlier work may still read a page that is handed out here.
 spp_status reserve(spp_pool_s& p, int32_t n, const int32_t* seqs, int32_t cells, hipStream_t st) {
   int64_t need = 0;
   // a shared page is copied by each of its writers but the last reference's
@@ -178,6 +179,7 @@ spp_status reserve(spp_pool_s& p, int32_t n, const int32_t* seqs, int32_t cells,
   moves.reserve(n);  // (what can throw comes before the first change)
   moved.reserve(n);
   for (int i = 0; i < n; ++i) p.seqs[seqs[i]].pages.reserve(pages_for(p, (int64_t)p.seqs[seqs[i]].n + cells));
+  if (const spp_status rc = order_after(p, st); rc != SPP_OK) return rc;
   for (int i = 0; i < n; ++i) {
     Seq& s = p.seqs[seqs[i]];
     if (s.n % p.cfg.page_cells) {
@@ -554,7 +556,10 @@ spp_status spp_pool_compact(spp_pool_t p, void* stream, int32_t* n_moved) {
     std::vector<int32_t> rest;
     rest.reserve(p->cfg.n_pages);  // (giving pages back never allocates)
     for (int32_t pg = used; pg < p->cfg.n_pages; ++pg) rest.push_back(pg);
-    if (const spp_status rc = copy_pages(*p, moves, static_cast<hipStream_t>(stream)); rc != SPP_OK) return rc;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (!moves.empty())
+      if (const spp_status rc = order_after(*p, st); rc != SPP_OK) return rc;
+    if (const spp_status rc = copy_pages(*p, moves, st); rc != SPP_OK) return rc;
     for (Seq& s : p->seqs)
       for (int32_t& pg : s.pages) pg = to[pg];
     for (const auto& mv : moves) std::swap(p->refs[mv.first], p->refs[mv.second]);
@@ -576,9 +581,8 @@ spp_status spp_decode_batch(spp_pool_t p, spp_model_t m, int32_t n, const int32_
     for (int i = 0; i < n; ++i)
       if (!dists[i]) return fail(SPP_E_INVALID_ARG, "null dist %d", i);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if ((rc = reserve(*p, n, seqs, 1, st)) != SPP_OK) return rc;
+    if ((rc = reserve(*p, n, seqs, 1, st)) != SPP_OK) return rc;  // (st follows the pool's work from here)
     std::lock_guard<std::mutex> mk(m->mu);
-    if ((rc = order_after(*p, st)) != SPP_OK) return rc;
     const int per = std::min({(int)k::kScanMax, (int)m->cfg.max_sessions, (int)m->cfg.max_tokens});
     for (int at = 0; at < n; at += per) {
       const int c = std::min(per, n - at);

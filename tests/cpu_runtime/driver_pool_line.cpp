@@ -1,0 +1,161 @@
+// Scenarios for the order of a pool's device work (pool.cpp) over host stand-ins for HIP and the
+// kernels, run under AddressSanitizer and ThreadSanitizer by tests/test_pool_line.py, one to a
+// process: the name of the scenario is the argument.  Prints "OK" and exits 0 when every check
+// holds.  The stand-ins of the paged kernels are here: a copy moves its bytes when its stream
+// comes to it, and one may be told to fail.
+#include <atomic>
+#include <chrono>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <map>
+#include <string>
+#include <thread>
+#include <vector>
+
+#include <hip/hip_runtime.h>
+
+#include "paged.hpp"
+#include "spp.h"
+
+namespace spp {
+namespace k {
+
+int paged_splits(const PageView&, int, int, int) { return 1; }
+size_t paged_work_bytes(const PageView&, int, int, int) { return 0; }
+hipError_t paged_attention(const PageView&, int, const PagedAttn&, void*, hipStream_t) { return hipSuccess; }
+
+hipError_t page_copy(const PageView& v, const PageList& l, int n, hipStream_t st) {
+  stub::enqueue(st, [=] {
+    for (int i = 0; i < n; ++i) std::memcpy(v.base + l.b[i] * v.page(), v.base + l.a[i] * v.page(), v.page());
+  });
+  return hipSuccess;
+}
+
+hipError_t page_session(const PageView& v, const PageList& l, int n, void* kv, int64_t, int64_t, int, bool to_pages,
+                        hipStream_t st) {
+  stub::enqueue(st, [=] {  // (a byte of each page stands for its cells)
+    for (int i = 0; i < n; ++i) {
+      char *p = v.base + l.a[i] * v.page(), *s = static_cast<char*>(kv);
+      if (to_pages) *p = *s; else *s = *p;
+    }
+  });
+  return hipSuccess;
+}
+
+hipError_t paged_epilogue(const Shape&, const StepView&, int, int, const PageView&, const int32_t*, int64_t,
+                          const float*, int, const float*, const float2*, float*, hipStream_t) {
+  return hipSuccess;
+}
+size_t adjust_work_bytes(int n, int) { return (size_t)n * 16; }
+hipError_t adjust_logits(int, int, const spp_adjust*, spp_summary*, void*, hipStream_t) { return hipSuccess; }
+
+}  // namespace k
+}  // namespace spp
+
+namespace {
+
+std::atomic<int> g_fail{0};
+#define CHECK(c)                                                                     \
+  do {                                                                               \
+    if (!(c)) {                                                                      \
+      std::fprintf(stderr, "%s:%d: check failed: %s (%s)\n", __FILE__, __LINE__, #c, \
+                   spp_last_error());                                                \
+      ++g_fail;                                                                      \
+    }                                                                                \
+  } while (0)
+
+constexpr int kLayers = 2, kD = 64, kDh = 64, kV = 512, kPage = 16;
+
+struct Pool {
+  spp_pool_config cfg{};
+  spp_page_layout lay{};
+  char* pages = nullptr;
+  spp_pool_t p = nullptr;
+  Pool(int n_pages, int max_seqs) {
+    cfg.n_layers = kLayers;
+    cfg.n_kv_heads = 1;
+    cfg.head_dim = kDh;
+    cfg.dtype = SPP_DTYPE_BF16;
+    cfg.page_cells = kPage;
+    cfg.n_pages = n_pages;
+    cfg.max_seqs = max_seqs;
+    hipMalloc((void**)&pages, spp_pool_bytes(&cfg));
+    CHECK(spp_pool_page_layout(&cfg, &lay) == SPP_OK);
+    CHECK(spp_pool_create(&cfg, pages, spp_pool_bytes(&cfg), &p) == SPP_OK);
+  }
+  ~Pool() {
+    spp_pool_destroy(p);
+    hipFree(pages);
+  }
+  int create(int cells) {
+    int32_t q = -1;
+    CHECK(spp_seq_create(p, cells, &q) == SPP_OK);
+    return q;
+  }
+  std::vector<int32_t> table(int seq) {
+    int32_t n = 0;
+    CHECK(spp_seq_table(p, seq, nullptr, 0, &n) == SPP_OK);
+    std::vector<int32_t> t(n);
+    CHECK(spp_seq_table(p, seq, t.data(), n, &n) == SPP_OK);
+    return t;
+  }
+  char* page(int i) { return pages + i * lay.page_stride; }
+  void fill(int i, int tag) { std::memset(page(i), tag, lay.page_stride); }
+  bool holds(int i, int tag) {
+    for (int64_t b = 0; b < lay.page_stride; ++b)
+      if (page(i)[b] != (char)tag) return false;
+    return true;
+  }
+};
+
+struct Streams {
+  hipStream_t st[2];
+  Streams() {
+    for (hipStream_t& s : st) hipStreamCreate(&s);
+  }
+  ~Streams() {
+    for (hipStream_t s : st) hipStreamDestroy(s);
+  }
+  hipStream_t operator[](int i) const { return st[i]; }
+};
+
+// Work that keeps a stream for a while.
+void busy(hipStream_t st) {
+  stub::enqueue(st, [] { std::this_thread::sleep_for(std::chrono::milliseconds(30)); });
+}
+
+// A page that a compaction is still reading is free on the host: a reserve that copies nothing may
+// hand it out, and what its caller then writes on the reserve's stream comes after that read.
+void reserve_orders() {
+  Streams st;
+  Pool pool(8, 4);
+  const int a = pool.create(kPage), b = pool.create(kPage), c = pool.create(0);
+  pool.fill(0, 1);
+  pool.fill(1, 2);
+  CHECK(spp_seq_free(pool.p, a) == SPP_OK);
+  busy(st[0]);
+  int32_t moved = 0;
+  CHECK(spp_pool_compact(pool.p, st[0], &moved) == SPP_OK && moved == 1);
+  CHECK(spp_seq_reserve(pool.p, 1, &c, 1, st[1]) == SPP_OK);
+  CHECK(pool.table(b) == std::vector<int32_t>{0} && pool.table(c) == std::vector<int32_t>{1});
+  stub::enqueue(st[1], [&] { pool.fill(1, 9); });
+  hipDeviceSynchronize();
+  CHECK(pool.holds(0, 2) && pool.holds(1, 9));
+}
+
+}  // namespace
+
+int main(int argc, char** argv) {
+  const std::map<std::string, void (*)()> scenarios = {
+      {"reserve_orders", reserve_orders},
+  };
+  const auto it = argc > 1 ? scenarios.find(argv[1]) : scenarios.end();
+  if (it == scenarios.end()) return 2;
+  it->second();
+  CHECK(stub::live_allocations() == 0);
+  stub::shutdown();
+  if (g_fail) return 1;
+  std::puts("OK");
+  return 0;
+}
