@@ -131,12 +131,17 @@ spp_status note_work(spp_pool_s& p, hipStream_t st) {
   p.recorded = true;
   return SPP_OK;
 }
+// The same at the end of work that came to rc: launches before a failed one are in the line too.
+spp_status end_work(spp_pool_s& p, hipStream_t st, spp_status rc) {
+  const spp_status noted = note_work(p, st);
+  return rc != SPP_OK ? rc : noted;
+}
 
 // Copies pages: (source, destination) pairs, no page both; batches travel as launch arguments.
 // `st` already continues the pool's line.
 spp_status copy_pages(spp_pool_s& p, const std::vector<std::pair<int32_t, int32_t>>& moves, hipStream_t st) {
   if (moves.empty()) return SPP_OK;
-  for (size_t at = 0; at < moves.size(); at += kPageBatch) {
+  const auto copy = [&](size_t at) -> spp_status {
     PageList l;
     const int n = (int)std::min<size_t>(kPageBatch, moves.size() - at);
     for (int i = 0; i < n; ++i) {
@@ -144,8 +149,11 @@ spp_status copy_pages(spp_pool_s& p, const std::vector<std::pair<int32_t, int32_
       l.b[i] = moves[at + i].second;
     }
     HIPCHK(k::page_copy(p.v, l, n, st));
-  }
-  return note_work(p, st);
+    return SPP_OK;
+  };
+  spp_status rc = SPP_OK;
+  for (size_t at = 0; at < moves.size() && rc == SPP_OK; at += kPageBatch) rc = copy(at);
+  return end_work(p, st, rc);
 }
 
 // Makes the next `cells` cells of the sequences writable (spp_seq_reserve).  Nothing changes
@@ -223,19 +231,22 @@ spp_status copy_session(spp_pool_s& p, const std::vector<int32_t>& pages, int n,
   if (const spp_status rc = order_after(p, st); rc != SPP_OK) return rc;
   if (const spp_status rc = after_steps(m, st); rc != SPP_OK) return rc;
   const int count = pages_for(p, n);
-  for (int at = 0; at < count; at += kPageBatch) {
+  const auto copy = [&](int at) -> spp_status {
     PageList l;
     const int c = std::min(kPageBatch, count - at);
     std::copy_n(pages.begin() + at, c, l.a);
     const int64_t c0 = (int64_t)at << p.v.shift;
     HIPCHK(k::page_session(p.v, l, c, s.kv, s.cap_stride, c0, (int)std::min<int64_t>(n - c0, (int64_t)c << p.v.shift),
                            to_pages, st));
-  }
+    return SPP_OK;
+  };
+  spp_status rc = SPP_OK;
+  for (int at = 0; at < count && rc == SPP_OK; at += kPageBatch) rc = copy(at);
+  rc = end_work(p, st, rc);
   // the model's next step waits for the pool's work up to then, which holds this copy and what
   // the model waited for so far (later work of the pool too, until a step has run)
-  if (const spp_status rc = note_work(p, st); rc != SPP_OK) return rc;
   m.copied = p.done;
-  return SPP_OK;
+  return rc;
 }
 
 // The cells of a decode step's rows: row r is the new token of seqs[r], at its length.
@@ -597,8 +608,7 @@ spp_status spp_decode_batch(spp_pool_t p, spp_model_t m, int32_t n, const int32_
         s.summary_at = ++s.n;
       }
     }
-    const spp_status noted = note_work(*p, st);
-    return rc != SPP_OK ? rc : noted;
+    return end_work(*p, st, rc);
   });
 }
 

@@ -18,6 +18,11 @@
 #include "paged.hpp"
 #include "spp.h"
 
+namespace {
+int g_launches_left = -1;  // copies that still start (-1: all)
+bool launch_fails() { return g_launches_left == 0 || (g_launches_left > 0 && g_launches_left-- == 0); }
+}  // namespace
+
 namespace spp {
 namespace k {
 
@@ -26,6 +31,7 @@ size_t paged_work_bytes(const PageView&, int, int, int) { return 0; }
 hipError_t paged_attention(const PageView&, int, const PagedAttn&, void*, hipStream_t) { return hipSuccess; }
 
 hipError_t page_copy(const PageView& v, const PageList& l, int n, hipStream_t st) {
+  if (launch_fails()) return hipErrorInvalidValue;
   stub::enqueue(st, [=] {
     for (int i = 0; i < n; ++i) std::memcpy(v.base + l.b[i] * v.page(), v.base + l.a[i] * v.page(), v.page());
   });
@@ -34,6 +40,7 @@ hipError_t page_copy(const PageView& v, const PageList& l, int n, hipStream_t st
 
 hipError_t page_session(const PageView& v, const PageList& l, int n, void* kv, int64_t, int64_t, int, bool to_pages,
                         hipStream_t st) {
+  if (launch_fails()) return hipErrorInvalidValue;
   stub::enqueue(st, [=] {  // (a byte of each page stands for its cells)
     for (int i = 0; i < n; ++i) {
       char *p = v.base + l.a[i] * v.page(), *s = static_cast<char*>(kv);
@@ -144,11 +151,114 @@ void reserve_orders() {
   CHECK(pool.holds(0, 2) && pool.holds(1, 9));
 }
 
+// A copy on write of more pages than one launch lists, whose second launch fails: the first one's
+// target pages are free again, and who takes them comes after it.
+void failed_page_copy() {
+  constexpr int kForks = 300;
+  Streams st;
+  Pool pool(2 + 2 * kForks, kForks + 2);
+  const int a = pool.create(5), d = pool.create(0);
+  pool.fill(0, 7);
+  std::vector<int32_t> forks(kForks);
+  CHECK(spp_seq_fork(pool.p, a, kForks, forks.data()) == SPP_OK);
+  busy(st[0]);
+  g_launches_left = 1;
+  CHECK(spp_seq_reserve(pool.p, kForks, forks.data(), 1, st[0]) == SPP_E_HIP);
+  g_launches_left = -1;
+  spp_pool_info_t i;
+  CHECK(spp_pool_info(pool.p, &i) == SPP_OK && i.used_pages == 1 && i.shared_pages == 1);
+  for (int32_t f : forks) CHECK(pool.table(f) == std::vector<int32_t>{0});
+  CHECK(spp_seq_reserve(pool.p, 1, &d, 1, st[1]) == SPP_OK && pool.table(d) == std::vector<int32_t>{1});
+  stub::enqueue(st[1], [&] { pool.fill(1, 9); });
+  hipDeviceSynchronize();
+  CHECK(pool.holds(0, 7) && pool.holds(1, 9));
+}
+
+struct Model {
+  std::vector<void*> bufs;
+  std::vector<const void*> layers;
+  spp_model_t m = nullptr;
+  spp_session_t s = nullptr;
+  void* kv = nullptr;
+  void* dev(size_t n) {
+    void* p = nullptr;
+    hipMalloc(&p, n);
+    bufs.push_back(p);
+    return p;
+  }
+  explicit Model(int cells) {  // and a session of it with so many cells
+    spp_weights w{};
+    w.embed = dev((size_t)kV * kD * 2);
+    w.final_norm = dev(kD * 2);
+    w.lm_head = dev((size_t)kV * kD * 2);
+    layers.assign(kLayers, dev((size_t)kD * kD * 2));  // (one buffer is every matrix: all are 64 x 64)
+    for (const void* const** p : {&w.attn_norm, &w.wq, &w.wk, &w.wv, &w.wo, &w.mlp_norm, &w.w_gate, &w.w_up, &w.w_down})
+      *p = layers.data();
+    spp_model_config c{};
+    c.n_layers = kLayers;
+    c.d_model = kD;
+    c.n_q_heads = c.n_kv_heads = 1;
+    c.head_dim = kDh;
+    c.ffn_dim = kD;
+    c.vocab = kV;
+    c.rms_eps = 1e-5f;
+    c.rope_base = 1e4;
+    c.dtype = SPP_DTYPE_BF16;
+    c.max_tokens = 16;
+    c.max_sessions = 1;
+    CHECK(spp_model_create(&c, &w, &m) == SPP_OK);
+    kv = dev(spp_session_kv_bytes(m, cells + 64));
+    const spp_session_config sc{cells + 64, 0};
+    CHECK(spp_session_create(m, &sc, kv, spp_session_kv_bytes(m, cells + 64), &s) == SPP_OK);
+    CHECK(spp_session_restore(s, cells) == SPP_OK);
+  }
+  ~Model() {
+    spp_session_destroy(s);
+    spp_model_destroy(m);
+    for (void* p : bufs) hipFree(p);
+  }
+};
+
+// An import and an export of more pages than one launch lists, whose second launch fails: what
+// the first launch reads and writes is used by the model's next step, and by the pool's next
+// work, after it.
+void failed_session_copy() {
+  for (int it = 0; it < 4; ++it) {
+    Streams st;
+    Pool pool(300, 4);
+    Model model(257 * kPage);
+    const int q = pool.create(it & 1 ? 257 * kPage : 0), c = pool.create(0);
+    bool first = false, seen = false;
+    busy(st[0]);
+    stub::enqueue(st[0], [&] { first = true; });
+    g_launches_left = 1;
+    CHECK((it & 1 ? spp_seq_export : spp_seq_import)(pool.p, q, model.s, st[0]) == SPP_E_HIP);
+    g_launches_left = -1;
+    const int32_t tok = 3;
+    if (it & 2)
+      CHECK(spp_kv_append_delta(model.s, &tok, 1, st[1]) == SPP_OK);
+    else
+      CHECK(spp_seq_reserve(pool.p, 1, &c, 1, st[1]) == SPP_OK);
+    stub::enqueue(st[1], [&] { seen = first; });
+    hipDeviceSynchronize();
+    CHECK(seen);
+    spp_seq_info_t i;  // what a failed copy leaves is no state
+    spp_session_info_t si;
+    CHECK(spp_seq_info(pool.p, q, &i) == SPP_OK && spp_session_info(model.s, &si) == SPP_OK);
+    if (it & 1)
+      CHECK(si.n_committed == (it & 2 ? 1 : 0) && i.n_cells == 257 * kPage);
+    else
+      CHECK(i.n_cells == 0);
+  }
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
   const std::map<std::string, void (*)()> scenarios = {
       {"reserve_orders", reserve_orders},
+      {"failed_page_copy", failed_page_copy},
+      {"failed_session_copy", failed_session_copy},
   };
   const auto it = argc > 1 ? scenarios.find(argv[1]) : scenarios.end();
   if (it == scenarios.end()) return 2;
