@@ -186,7 +186,12 @@ spp_status reserve(spp_pool_s& p, int32_t n, const int32_t* seqs, int32_t cells,
   std::vector<int32_t*> moved;  // the table entries of the moves
   moves.reserve(n);  // (what can throw comes before the first change)
   moved.reserve(n);
-  for (int i = 0; i < n; ++i) p.seqs[seqs[i]].pages.reserve(pages_for(p, (int64_t)p.seqs[seqs[i]].n + cells));
+  std::vector<size_t> had(n);   // pages of the tables before
+  for (int i = 0; i < n; ++i) {
+    Seq& s = p.seqs[seqs[i]];
+    had[i] = s.pages.size();
+    s.pages.reserve(pages_for(p, (int64_t)s.n + cells));
+  }
   if (const spp_status rc = order_after(p, st); rc != SPP_OK) return rc;
   for (int i = 0; i < n; ++i) {
     Seq& s = p.seqs[seqs[i]];
@@ -204,12 +209,14 @@ spp_status reserve(spp_pool_s& p, int32_t n, const int32_t* seqs, int32_t cells,
     while ((int)s.pages.size() < want) s.pages.push_back(take_page(p));
   }
   const spp_status rc = copy_pages(p, moves, st);
-  if (rc != SPP_OK)  // the pages stay shared (each still has the reference of another)
+  if (rc != SPP_OK) {  // the pages stay shared (each still has the reference of another), the tables as they were
     for (size_t i = 0; i < moves.size(); ++i) {
       drop_page(p, moves[i].second);
       if (p.refs[moves[i].first]++ == 1) ++p.n_shared;
       *moved[i] = moves[i].first;
     }
+    for (int i = 0; i < n; ++i) drop_pages_from(p, p.seqs[seqs[i]], had[i]);
+  }
   return rc;
 }
 

@@ -174,6 +174,31 @@ void failed_page_copy() {
   CHECK(pool.holds(0, 7) && pool.holds(1, 9));
 }
 
+// A reserve that fails gives back the pages it added to the tables too, shared ones copied or not.
+void failed_reserve_changes_nothing() {
+  Streams st;
+  Pool pool(20, 6);
+  const int a = pool.create(5), b = pool.create(kPage), c = pool.create(0), e = pool.create(3);
+  int32_t f = -1;
+  CHECK(spp_seq_fork(pool.p, a, 1, &f) == SPP_OK);
+  CHECK(spp_seq_reserve(pool.p, 1, &e, 2 * kPage, st[0]) == SPP_OK);  // (an earlier reserve stays)
+  spp_pool_info_t was, now;
+  CHECK(spp_pool_info(pool.p, &was) == SPP_OK);
+  std::map<int, std::vector<int32_t>> tables;
+  for (int q : {a, b, c, e, f}) tables[q] = pool.table(q);
+  const int32_t all[] = {b, f, c, e, a};
+  for (int cells : {1, kPage, 3 * kPage}) {
+    g_launches_left = 0;
+    CHECK(spp_seq_reserve(pool.p, 5, all, cells, st[1]) == SPP_E_HIP);
+    g_launches_left = -1;
+    CHECK(spp_pool_info(pool.p, &now) == SPP_OK && std::memcmp(&was, &now, sizeof now) == 0);
+    for (int q : {a, b, c, e, f}) CHECK(pool.table(q) == tables[q]);
+  }
+  CHECK(spp_seq_reserve(pool.p, 5, all, kPage, st[1]) == SPP_OK);
+  CHECK(spp_pool_info(pool.p, &now) == SPP_OK && now.shared_pages == 0);
+  hipDeviceSynchronize();
+}
+
 struct Model {
   std::vector<void*> bufs;
   std::vector<const void*> layers;
@@ -259,6 +284,7 @@ int main(int argc, char** argv) {
       {"reserve_orders", reserve_orders},
       {"failed_page_copy", failed_page_copy},
       {"failed_session_copy", failed_session_copy},
+      {"failed_reserve_changes_nothing", failed_reserve_changes_nothing},
   };
   const auto it = argc > 1 ? scenarios.find(argv[1]) : scenarios.end();
   if (it == scenarios.end()) return 2;

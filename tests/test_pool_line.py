@@ -12,7 +12,8 @@ STUB = os.path.join(ROOT, "tests", "cpu_runtime")
 CSRC = os.path.join(ROOT, "paper_2606_29565_amd", "csrc")
 SANITIZERS = {"asan": ["-fsanitize=address,undefined", "-fno-omit-frame-pointer"],
               "tsan": ["-fsanitize=thread"]}
-SCENARIOS = ["reserve_orders", "failed_page_copy", "failed_session_copy"]
+SCENARIOS = ["reserve_orders", "failed_page_copy", "failed_session_copy",
+             "failed_reserve_changes_nothing"]
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not available")
 
