@@ -37,11 +37,14 @@ struct spp_pool_s {
   Lowest free_seqs;           // sequence numbers, lowest first
   int n_seqs = 0, n_shared = 0;
   ScanResult* summary = nullptr;  // device, one slot per sequence
-  std::shared_ptr<Event> done;    // the pool's device work so far; models may wait for it too
+  // The pool's device work so far is events[done].  An event that a model has to wait for
+  // (Model::copied) is not recorded again while it has: two would do for one model.
+  std::shared_ptr<Event> events[4];
+  int done = 0;
   bool recorded = false;
   std::mutex mu;                  // taken before a session's and a model's
   ~spp_pool_s() {
-    if (recorded) hipEventSynchronize(done->ev);
+    if (recorded) hipEventSynchronize(events[done]->ev);
     if (summary) hipFree(summary);
   }
 };
@@ -123,11 +126,17 @@ int32_t take_seq(spp_pool_s& p) {
 // what was enqueued since as its new end.
 spp_status order_after(spp_pool_s& p, hipStream_t st) {
   hipSetDevice(p.device);
-  if (p.recorded) HIPCHK(hipStreamWaitEvent(st, p.done->ev, 0));
+  if (p.recorded) HIPCHK(hipStreamWaitEvent(st, p.events[p.done]->ev, 0));
   return SPP_OK;
 }
 spp_status note_work(spp_pool_s& p, hipStream_t st) {
-  HIPCHK(hipEventRecord(p.done->ev, st));
+  // an event of the pool's alone, the last one if it is (each held by a model: the last one, and
+  // that model waits for what follows too)
+  constexpr int n = sizeof(p.events) / sizeof(p.events[0]);
+  int at = p.done;
+  for (int i = 0; i < n && p.events[at].use_count() > 1; ++i) at = (at + 1) % n;
+  HIPCHK(hipEventRecord(p.events[at]->ev, st));
+  p.done = at;
   p.recorded = true;
   return SPP_OK;
 }
@@ -250,9 +259,9 @@ spp_status copy_session(spp_pool_s& p, const std::vector<int32_t>& pages, int n,
   spp_status rc = SPP_OK;
   for (int at = 0; at < count && rc == SPP_OK; at += kPageBatch) rc = copy(at);
   rc = end_work(p, st, rc);
-  // the model's next step waits for the pool's work up to then, which holds this copy and what
-  // the model waited for so far (later work of the pool too, until a step has run)
-  m.copied = p.done;
+  // the model's next step waits for the pool's work up to here, which holds this copy and what
+  // the model waited for so far
+  m.copied = p.events[p.done];
   return rc;
 }
 
@@ -372,9 +381,12 @@ spp_status spp_pool_create(const spp_pool_config* cfg, void* pages, size_t bytes
     std::vector<int32_t> numbers(cfg->max_seqs);
     for (int32_t i = 0; i < cfg->max_seqs; ++i) numbers[i] = i;
     p->free_seqs = Lowest(std::greater<int32_t>(), std::move(numbers));
-    p->done = std::make_shared<Event>();
-    if (hipEventCreateWithFlags(&p->done->ev, hipEventDisableTiming) != hipSuccess ||
-        hipMalloc((void**)&p->summary, sizeof(ScanResult) * cfg->max_seqs) != hipSuccess)
+    for (auto& e : p->events) {
+      e = std::make_shared<Event>();
+      if (hipEventCreateWithFlags(&e->ev, hipEventDisableTiming) != hipSuccess)
+        return fail(SPP_E_NOMEM, "pool resources");
+    }
+    if (hipMalloc((void**)&p->summary, sizeof(ScanResult) * cfg->max_seqs) != hipSuccess)
       return fail(SPP_E_NOMEM, "pool resources");
     *out = p.release();
     return SPP_OK;
@@ -631,7 +643,7 @@ spp_status spp_seq_summaries(spp_pool_t p, int32_t n, const int32_t* seqs, spp_s
       hi = std::max(hi, (int)seqs[i]);
     }
     std::vector<ScanResult> r(hi - lo + 1);
-    HIPCHK(hipEventSynchronize(p->done->ev));
+    HIPCHK(hipEventSynchronize(p->events[p->done]->ev));
     HIPCHK(hipMemcpy(r.data(), p->summary + lo, r.size() * sizeof(ScanResult), hipMemcpyDeviceToHost));
     for (int i = 0; i < n; ++i) fill_summary(r[seqs[i] - lo], p->seqs[seqs[i]].summary_at, out + i);
     return SPP_OK;

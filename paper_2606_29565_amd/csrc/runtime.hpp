@@ -157,8 +157,8 @@ struct StepCache {
 
 // What touches the cells of a model's sessions is one line: `st` continues after all of it, and
 // note_step marks what was enqueued since as its new end.  (Copies of a pool mark it with the
-// event that the pool records anyway: a second record in a row costs the device 4 us.)  The
-// caller holds m.mu.
+// event that the pool records anyway, and does not record again while it is `copied`: a second
+// record in a row costs the device 4 us.)  The caller holds m.mu.
 inline spp_status after_steps(Model& m, hipStream_t st) {
   if (m.step_recorded) HIPCHK(hipStreamWaitEvent(st, m.step_done, 0));
   if (m.copied) HIPCHK(hipStreamWaitEvent(st, m.copied->ev, 0));

@@ -277,6 +277,45 @@ void failed_session_copy() {
   }
 }
 
+// A model's step waits for the copies of its sessions' cells, and for nothing that the pool does
+// after them: later work of the pool that waits for that step (here for what follows it on its
+// stream) gets to see it.  Two pools take turns at the model, so that every copy has one before it.
+void later_work_holds_no_step() {
+  Streams st;
+  Pool pool(16, 6), other(16, 6);
+  Model model(20);
+  for (int it = 0; it < 12; ++it) {
+    Pool& p = it % 3 == 2 ? other : pool;
+    const int low = p.create(kPage), q = p.create(0);
+    std::atomic<bool> copied{false}, stepped{false};
+    bool in_order = false, seen = false;
+    busy(st[0]);
+    stub::enqueue(st[0], [&] { copied = true; });
+    CHECK(spp_seq_import(p.p, q, model.s, st[0]) == SPP_OK);
+    if (it & 1) CHECK(spp_seq_export(p.p, q, model.s, st[0]) == SPP_OK);
+    CHECK(spp_seq_free(p.p, low) == SPP_OK);
+    stub::enqueue(st[0], [&] {
+      for (int ms = 0; ms < 3000 && !stepped; ++ms) std::this_thread::sleep_for(std::chrono::milliseconds(1));
+      seen = stepped;
+    });
+    int32_t moved = 0;
+    CHECK(spp_pool_compact(p.p, st[0], &moved) == SPP_OK && moved == 1);
+    const int32_t tok = 3;
+    if (it & 2)
+      CHECK(spp_shift(model.s, 1, st[1]) == SPP_OK);
+    else
+      CHECK(spp_kv_append_delta(model.s, &tok, 1, st[1]) == SPP_OK);
+    stub::enqueue(st[1], [&] {
+      in_order = copied;
+      stepped = true;
+    });
+    hipDeviceSynchronize();
+    CHECK(in_order && seen);
+    CHECK(spp_seq_free(p.p, q) == SPP_OK && spp_session_restore(model.s, 20) == SPP_OK);
+    if (g_fail) return;
+  }
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
@@ -285,6 +324,7 @@ int main(int argc, char** argv) {
       {"failed_page_copy", failed_page_copy},
       {"failed_session_copy", failed_session_copy},
       {"failed_reserve_changes_nothing", failed_reserve_changes_nothing},
+      {"later_work_holds_no_step", later_work_holds_no_step},
   };
   const auto it = argc > 1 ? scenarios.find(argv[1]) : scenarios.end();
   if (it == scenarios.end()) return 2;

@@ -13,7 +13,7 @@ CSRC = os.path.join(ROOT, "paper_2606_29565_amd", "csrc")
 SANITIZERS = {"asan": ["-fsanitize=address,undefined", "-fno-omit-frame-pointer"],
               "tsan": ["-fsanitize=thread"]}
 SCENARIOS = ["reserve_orders", "failed_page_copy", "failed_session_copy",
-             "failed_reserve_changes_nothing"]
+             "failed_reserve_changes_nothing", "later_work_holds_no_step"]
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not available")
 
