@@ -578,8 +578,10 @@ typedef struct {
   void* out;                 /* device, rows as q's                                       */
   int64_t out_stride;        /* as q_stride                                               */
 } spp_paged_attn;
-/* Bytes of workspace the call needs (0 for bad arguments, or none needed; it depends on
- * n_seqs, n_q_heads, max_pages and the pool). */
+/* Bytes of workspace that suffice for the call, and for those with fewer sequences or a smaller
+ * max_pages (0 for bad arguments, or none needed): a workspace made for the largest batch
+ * serves it as sequences finish, which may need more than the largest itself.  The size depends on
+ * n_seqs, n_q_heads, max_pages and the pool. */
 size_t spp_paged_attention_work_bytes(const spp_paged_attn* a);
 /* Only launches kernels (one or two) on `stream`: it may be captured into a graph, whose
  * replays read the table and the lengths as they are then.  The workspace (device, 16-byte
@@ -615,7 +617,8 @@ typedef struct {
                                    -FLT_MAX, to gate the adjusted logits                  */
 } spp_adjust;
 
-/* Bytes of workspace spp_adjust_logits needs for n rows with summaries. */
+/* Bytes of workspace that suffice for n rows with summaries, and for fewer (which may need more
+ * than n rows themselves). */
 size_t spp_adjust_logits_work_bytes(int32_t n, int32_t vocab);
 /* Penalties for repeated tokens, biases and an allowed set (a grammar's next tokens) on n
  * rows of logits -- those of a resume or a decode step -- with the reductions a greedy step

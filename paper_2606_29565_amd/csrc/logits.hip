@@ -337,7 +337,7 @@ __global__ __launch_bounds__(64) void adjust_merge_kernel(int nb, const float4* 
 // often a history is read and the instructions of a workgroup beside its tokens' own (64 rows of
 // 128256 with 2000 tokens each: 20.7 us, with slices of 1024 23.1, with slices of 4096, half as
 // many waves to a CU, 22.5; 17 rows of 152063 with 700: 10.1, 10.4 and 10.9).
-int slice_units(int n, int vocab) { return (int64_t)vocab * n <= 2048 * 1024 ? 1 : 2; }
+int slice_units(int n, int vocab) { return (int64_t)vocab * n <= kShortSliceTokens ? 1 : 2; }
 // Slices of a row, whatever its alignment.
 int slices(int units, int vocab) { return (vocab + 3 + units * 4 * kTpb - 1) / (units * 4 * kTpb); }
 

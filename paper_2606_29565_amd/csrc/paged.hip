@@ -556,7 +556,7 @@ int paged_splits(const PageView& v, int n, int n_q, int max_pages) {
   const int unit = (v.elem == 2 ? step_keys<bf16_t>() : step_keys<float>()) * kWaves;
   const int64_t most = (((int64_t)max_pages << v.shift) + unit - 1) / unit, wgs = (int64_t)n * v.n_kv * tiles;
   if (most <= (wgs >= 128 ? 4 : 2)) return 1;
-  const int64_t want = std::max<int64_t>(std::min<int64_t>(4, most / 8), 1024 / wgs);
+  const int64_t want = std::max<int64_t>(std::min<int64_t>(4, most / 8), kSplitWorkgroups / wgs);
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, (int64_t)kMaxSplits}));
 }
 

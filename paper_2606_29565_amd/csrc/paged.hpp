@@ -39,10 +39,17 @@ struct PageList {
   int32_t a[kPageBatch], b[kPageBatch];
 };
 
+// Workgroups of an attention call that its ranges make up to: as many sequences or more get no
+// more ranges each for being fewer.
+constexpr int kSplitWorkgroups = 1024;
+// Tokens of all rows up to which adjusted logits are cut into the shorter slices.
+constexpr int kShortSliceTokens = 2048 * 1024;
+
 namespace k {
 
 // Key ranges per sequence and kv head of a call: a rule on n, the heads and the table's width.
 int paged_splits(const PageView& v, int n, int n_q, int max_pages);
+// Workspace of this very call (of fewer sequences it may be more, see kSplitWorkgroups).
 size_t paged_work_bytes(const PageView& v, int n, int n_q, int max_pages);
 hipError_t paged_attention(const PageView& v, int layer, const PagedAttn& a, void* work,
                            hipStream_t st);
@@ -62,6 +69,7 @@ hipError_t paged_epilogue(const Shape& s, const StepView& sv, int n_rows, int la
                           const float* partials, int splits, const float* ss, const float2* rope,
                           float* q_out, hipStream_t st);
 
+// Workspace of this very call (of fewer rows it may be more, see kShortSliceTokens).
 size_t adjust_work_bytes(int n, int vocab);
 hipError_t adjust_logits(int n, int vocab, const spp_adjust* rows, spp_summary* summaries,
                          void* work, hipStream_t st);

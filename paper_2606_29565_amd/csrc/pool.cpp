@@ -652,7 +652,12 @@ spp_status spp_seq_summaries(spp_pool_t p, int32_t n, const int32_t* seqs, spp_s
 
 size_t spp_paged_attention_work_bytes(const spp_paged_attn* a) {
   if (check_attn(a) != SPP_OK || a->n_seqs == 0) return 0;
-  return k::paged_work_bytes(a->pool->v, a->n_seqs, a->n_q_heads, a->max_pages);
+  // fewer sequences may take more ranges each: the most that any number of them up to n_seqs takes
+  // (what one takes never falls with max_pages)
+  size_t most = k::paged_work_bytes(a->pool->v, a->n_seqs, a->n_q_heads, a->max_pages);
+  for (int n = std::min(a->n_seqs, kSplitWorkgroups); n >= 1; --n)
+    most = std::max(most, k::paged_work_bytes(a->pool->v, n, a->n_q_heads, a->max_pages));
+  return most;
 }
 
 spp_status spp_paged_attention(const spp_paged_attn* a, void* work, size_t work_bytes, void* stream) {
@@ -673,7 +678,9 @@ spp_status spp_paged_attention(const spp_paged_attn* a, void* work, size_t work_
 
 size_t spp_adjust_logits_work_bytes(int32_t n, int32_t vocab) {
   if (n < 1 || vocab < 1 || vocab > (1 << 24)) return 0;
-  return k::adjust_work_bytes(n, vocab);
+  // the most rows that are cut into the shorter slices may take more than n rows
+  const int few = std::min(n, kShortSliceTokens / vocab);
+  return std::max(k::adjust_work_bytes(n, vocab), few ? k::adjust_work_bytes(few, vocab) : 0);
 }
 
 spp_status spp_adjust_logits(int32_t n, int32_t vocab, const spp_adjust* rows, spp_summary* summaries, void* work,

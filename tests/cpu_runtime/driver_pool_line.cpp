@@ -27,7 +27,9 @@ namespace spp {
 namespace k {
 
 int paged_splits(const PageView&, int, int, int) { return 1; }
-size_t paged_work_bytes(const PageView&, int, int, int) { return 0; }
+size_t paged_work_bytes(const PageView&, int n, int n_q, int max_pages) {  // (falls, as a rule on n may)
+  return n >= 16 && max_pages < 100 ? 0 : (size_t)n_q * max_pages * (n >= 5 ? n : 2 * n);
+}
 hipError_t paged_attention(const PageView&, int, const PagedAttn&, void*, hipStream_t) { return hipSuccess; }
 
 hipError_t page_copy(const PageView& v, const PageList& l, int n, hipStream_t st) {
@@ -277,6 +279,33 @@ void failed_session_copy() {
   }
 }
 
+// A workspace for a call serves every smaller one, whatever the rule does with their number; a
+// call is held to what itself needs.
+void workspace_of_smaller_calls() {
+  Pool pool(4, 4);
+  std::vector<int32_t> tab(4096, 0), len(64, 1);
+  alignas(16) static char io[64 * 4 * kDh * 2], work[1 << 16];
+  const auto call = [&](int n, int max_pages) {
+    return spp_paged_attn{pool.p, 0, n, 4, SPP_DTYPE_BF16, io, 4 * kDh, tab.data(), max_pages, max_pages, len.data(),
+                          0.f, io, 4 * kDh};
+  };
+  for (int max_pages : {1, 60}) {
+    size_t most = 0;
+    for (int n = 1; n <= 40; ++n) {
+      const spp_paged_attn a = call(n, max_pages), less = call(n, max_pages / 2 + 1);
+      const size_t bytes = spp_paged_attention_work_bytes(&a);
+      CHECK(bytes >= most && bytes >= spp_paged_attention_work_bytes(&less));
+      most = bytes;
+    }
+    CHECK(most == (size_t)4 * max_pages * 15);
+    for (int n = 1; n <= 40; ++n) {
+      const spp_paged_attn a = call(n, max_pages);
+      CHECK(spp_paged_attention(&a, work, most, nullptr) == SPP_OK);
+      CHECK(spp_paged_attention(&a, nullptr, 0, nullptr) == (n >= 16 ? SPP_OK : SPP_E_INVALID_ARG));
+    }
+  }
+}
+
 // A model's step waits for the copies of its sessions' cells, and for nothing that the pool does
 // after them: later work of the pool that waits for that step (here for what follows it on its
 // stream) gets to see it.  Two pools take turns at the model, so that every copy has one before it.
@@ -324,6 +353,7 @@ int main(int argc, char** argv) {
       {"failed_page_copy", failed_page_copy},
       {"failed_session_copy", failed_session_copy},
       {"failed_reserve_changes_nothing", failed_reserve_changes_nothing},
+      {"workspace_of_smaller_calls", workspace_of_smaller_calls},
       {"later_work_holds_no_step", later_work_holds_no_step},
   };
   const auto it = argc > 1 ? scenarios.find(argv[1]) : scenarios.end();

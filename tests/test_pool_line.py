@@ -13,7 +13,8 @@ CSRC = os.path.join(ROOT, "paper_2606_29565_amd", "csrc")
 SANITIZERS = {"asan": ["-fsanitize=address,undefined", "-fno-omit-frame-pointer"],
               "tsan": ["-fsanitize=thread"]}
 SCENARIOS = ["reserve_orders", "failed_page_copy", "failed_session_copy",
-             "failed_reserve_changes_nothing", "later_work_holds_no_step"]
+             "failed_reserve_changes_nothing", "later_work_holds_no_step",
+             "workspace_of_smaller_calls"]
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not available")
 
