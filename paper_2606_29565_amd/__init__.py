@@ -720,11 +720,18 @@ class PagePool:
 
 def decode_batch(pool: PagePool, model: Model, seqs: Sequence[int], tokens: Sequence[int], dists,
                  stream=None) -> None:
-    """One decode step: tokens[i] appended to seqs[i], its logits to dists[i] (spp_decode_batch)."""
+    """One decode step: tokens[i] appended to seqs[i], its logits to dists[i] (spp_decode_batch):
+    contiguous fp32 tensors of at least the vocabulary on the pool's device, or their pointers."""
     arr, n = _host_i32(seqs)
     toks, nt = _host_i32(tokens)
     if nt != n or len(dists) != n:
         raise ValueError("sequences, tokens and dists differ in number")
+    import torch
+    for i, d in enumerate(dists):
+        if isinstance(d, torch.Tensor) and (d.dtype != torch.float32 or not d.is_contiguous() or
+                                            d.numel() < model.vocab or d.get_device() != pool.device):
+            raise ValueError(f"dist {i} is a contiguous float32 tensor of at least {model.vocab} "
+                             f"elements on the pool's device")
     ptrs = (ctypes.c_void_p * max(1, n))(*[_ptr(d) for d in dists])
     check(lib().spp_decode_batch(pool.handle, model.handle, n, arr, toks, ptrs,
                                  ctypes.c_void_p(_stream_of(stream, pool.device))), "spp_decode_batch")
