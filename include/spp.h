@@ -558,8 +558,10 @@ spp_status spp_seq_summaries(spp_pool_t pool, int32_t n, const int32_t* seqs, sp
  * table[i][j / page_cells].  A table entry outside [0, n_pages) takes its cells out (a page
  * given up from the middle); lengths beyond max_pages*page_cells are cut to it, negative
  * ones are zero.  A sequence with no cell left gets zeros.  What lies in a page behind a sequence's
- * last cell, or in a page that is not listed, has no influence, NaN included (an infinite or
- * NaN element of a live cell gives NaN where it is used).
+ * last cell, or in a page that is not listed, has no influence, NaN included.  Of a live cell, a
+ * NaN of K makes the rows of the query heads that read it NaN, one of V its dimension of them; an
+ * infinity of V makes its dimension infinite or NaN, and one of K makes infinite or NaN scores.  A
+ * score of +inf or NaN makes its row NaN, one of -inf has no weight (a row of these alone gets zeros).
  * The products of bf16 cells run on bf16 matrix cores with q (unless it is bf16) and p in
  * two bf16 parts and fp32 sums: about 16 significant bits of both. */
 typedef struct {

@@ -1,5 +1,5 @@
 """Attention over paged caches where its rules change or reach their ends: workspaces of smaller
-calls.  The bound of a result is that of test_gpu_paged.py."""
+calls, infinities and NaN in live cells.  The bound of a result is that of test_gpu_paged.py."""
 import ctypes
 import math
 
@@ -44,3 +44,73 @@ def test_a_workspace_of_the_largest_batch_serves_smaller_ones():
         diff = (out[:m].double().cpu() - want[:m]).abs()
         assert bool((diff <= _bound(A, vmax, dh, 1000, True, True, want[:m])).all()), (m, float(diff.max()))
         assert bool((out[m:] == 7).all())
+
+
+@pytest.mark.parametrize("bf16,io_bf16,page,cells", [(True, True, 16, 100), (False, False, 32, 77), (True, True, 64, 3000),
+                                                     (False, True, 16, 2500), (True, False, 64, 3000)])
+def test_infinities_and_nan_in_live_cells(bf16, io_bf16, page, cells):
+    """Of a live cell: a NaN of K makes the rows that use it NaN, one of V its dimension; an infinity
+    of K makes scores of +inf (a NaN row) and -inf (no weight), one of V its dimension not finite.
+    A row whose scores all are -inf is zero.  Nothing else changes a bit.  (fp32 queries over
+    bf16 cells go through two parts, whose second is zero here: their infinite scores are NaN.)"""
+    import torch
+    import paper_2606_29565_amd as spp
+    nq, nkv, dh, at, dim = 8, 2, 64, cells // 3, 37
+    width = -(-cells // page)
+    pool, pages, g = _pool(torch, spp, 1, nkv, dh, bf16, page, 2 * width)
+    table = torch.randperm(2 * width, generator=g, device="cuda").view(2, width).int()
+    lens = torch.full((2,), cells, dtype=torch.int32, device="cuda")
+    q = torch.empty(2, nq, dh, device="cuda").normal_(0, 1.5, generator=g).bfloat16().to(
+        torch.bfloat16 if io_bf16 else torch.float32)
+    q[:, :, dim] = torch.tensor([2.0, -2.0] * (nq // 2), device="cuda")
+    neg, pos = slice(1, nq // nkv, 2), slice(0, nq // nkv, 2)       # heads of kv head 0 by the sign
+    att = spp.PagedAttention(pool, 0, nq, table, lens, io_bf16=io_bf16)
+    run = lambda: att(q, torch.full_like(q, 7.0)).clone()  # noqa: E731
+    keys = pages[:, 0, 0].view(-1, nkv, page, dh)
+    vals = pages[:, 0, 1].view(-1, nkv, dh, page)
+    pg, c = int(table[0, at // page]), at % page
+    plain, clean = run(), pages.clone()
+    split = bf16 and not io_bf16
+
+    keys[pg, 0, c, dim] = float("nan")
+    got = run()
+    assert bool(got[0, :nq // nkv].isnan().all())
+    assert torch.equal(got[0, nq // nkv:], plain[0, nq // nkv:]) and torch.equal(got[1], plain[1])
+    pages.copy_(clean)
+
+    for value in (float("nan"), float("inf"), -float("inf")):
+        vals[pg, 0, dim, c] = value
+        got = run()
+        assert not bool(got[0, :nq // nkv, dim].isfinite().any())
+        if math.isnan(value):
+            assert bool(got[0, :nq // nkv, dim].isnan().all())
+        got[0, :nq // nkv, dim] = plain[0, :nq // nkv, dim]
+        assert torch.equal(got, plain)
+        pages.copy_(clean)
+
+    keys[pg, 0, c, dim] = float("inf")
+    got = run()
+    assert bool(got[0, pos].isnan().all())
+    assert torch.equal(got[0, nq // nkv:], plain[0, nq // nkv:]) and torch.equal(got[1], plain[1])
+    if split:
+        assert bool(got[0, neg].isnan().all())
+    else:                                                            # the cell is left out
+        want, A, vmax = _reference_without(torch, pages, nq, nkv, dh, page, table, cells, q, at)
+        diff = (got[0, neg].double().cpu() - want[neg]).abs()
+        assert bool((diff <= _bound(A, vmax, dh, cells, bf16, io_bf16, want[neg])).all()), float(diff.max())
+        keys[table[0].long(), 0, :, dim] = float("inf")
+        got = run()
+        assert bool((got[0, neg] == 0).all()) and bool(got[0, pos].isnan().all())
+        assert torch.equal(got[0, nq // nkv:], plain[0, nq // nkv:]) and torch.equal(got[1], plain[1])
+
+
+def _reference_without(torch, pages, nq, nkv, dh, page, table, cells, q, gone):
+    """The formula for sequence 0 without cell `gone`: its cells moved together into pages of their own."""
+    P = pages[table[0].long()].cpu()
+    keep = [j for j in range(cells) if j != gone]
+    K = P[:, 0, 0].view(-1, nkv, page, dh).transpose(1, 2).reshape(-1, nkv, dh)[keep]
+    V = P[:, 0, 1].view(-1, nkv, dh, page).permute(0, 3, 1, 2).reshape(-1, nkv, dh)[keep]
+    one = torch.stack([K.permute(1, 0, 2).reshape(-1), V.permute(1, 2, 0).reshape(-1)])[None, None]
+    out, A, vmax = _reference(torch, one, 0, nq, nkv, dh, cells - 1, torch.zeros(1, 1, dtype=torch.int64).numpy(),
+                              [cells - 1], q[:1], 1 / math.sqrt(dh))
+    return out[0], A, vmax
