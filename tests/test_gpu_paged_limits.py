@@ -1,5 +1,6 @@
 """Attention over paged caches where its rules change or reach their ends: workspaces of smaller
-calls, infinities and NaN in live cells.  The bound of a result is that of test_gpu_paged.py."""
+calls, infinities and NaN in live cells, the most ranges, the decode step over several of them.
+The bound of a result is that of test_gpu_paged.py."""
 import ctypes
 import math
 
@@ -114,3 +115,77 @@ def _reference_without(torch, pages, nq, nkv, dh, page, table, cells, q, gone):
     out, A, vmax = _reference(torch, one, 0, nq, nkv, dh, cells - 1, torch.zeros(1, 1, dtype=torch.int64).numpy(),
                               [cells - 1], q[:1], 1 / math.sqrt(dh))
     return out[0], A, vmax
+
+
+@pytest.mark.parametrize("nq,dh,bf16,io_bf16,page,lengths", [
+    (4, 64, False, False, 16, [32768 + 129, 100]),    # ranges of 128 cells: the most ranges, one of them longer
+    (3, 128, False, True, 128, [129, 32768 * 2 + 1]),
+    (5, 64, True, True, 64, [65536 + 257, 513]),      # ranges of 256
+    (2, 128, True, False, 256, [300, 65536 + 257]),
+    (4, 128, True, True, 32, [65536, 65537, 0]),
+])
+def test_as_many_ranges_as_there_are(nq, dh, bf16, io_bf16, page, lengths):
+    """More cells than 256 ranges of one step hold: every thread of a join has a range, ranges are
+    of several steps, and the other sequences of the call take a few ranges or one."""
+    import torch
+    import paper_2606_29565_amd as spp
+    n, width = len(lengths), -(-max(lengths) // page)
+    pool, pages, g = _pool(torch, spp, 1, 1, dh, bf16, page, n * width, seed=nq)
+    table = torch.randperm(n * width, generator=g, device="cuda").view(n, width).int()
+    lens = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    q = torch.empty(n, nq, dh, device="cuda").normal_(0, 1.5, generator=g).to(
+        torch.bfloat16 if io_bf16 else torch.float32)
+    att = spp.PagedAttention(pool, 0, nq, table, lens, io_bf16=io_bf16)
+    att._work.fill_(255)
+    # as many ranges as the join has threads: each leaves dh sums, a maximum and a sum
+    assert att._work.numel() == n * nq * 256 * (dh + 2) * 4
+    out = att(q, torch.full_like(q, 7.0))
+    want, A, vmax = _reference(torch, pages, 0, nq, 1, dh, page, table.cpu().numpy(), lengths, q, 1 / math.sqrt(dh))
+    diff = (out.double().cpu() - want).abs()
+    for i, m in enumerate(lengths):
+        assert bool((diff[i] <= _bound(A, vmax, dh, m, bf16, io_bf16, want[i])).all()), (m, float(diff[i].max()))
+    assert torch.equal(out, att(q, torch.empty_like(q)))
+
+
+@pytest.mark.parametrize("fmt,max_sessions,page,heads", [("bf16", 4, 64, (4, 2, 64)), ("f32", 4, 16, (4, 2, 64)),
+                                                         ("bf16", 1, 16, (2, 1, 128)), ("mxfp4", 3, 32, (4, 2, 64))])
+def test_a_decode_step_over_several_ranges(fmt, max_sessions, page, heads):
+    """Sequences of 1 to 1300 cells decoded together: the step joins its ranges (of 256 cells, 128 in
+    fp32) and hands the attention on in its model's form.  Every distribution against the oracle's, where
+    256 values less (the first, or the last of 1300 cells) are 0.2 and 0.14, one value less 5e-3."""
+    import torch
+    import oracle
+    import paper_2606_29565_amd as spp
+    import synth
+    from gpu_util import build_model, log, max_abs
+    nq, nkv, dh = heads
+    bf16, steps = fmt != "f32", 2
+    shape = synth.Shape("paged-long-" + fmt, 2, 256, nq, nkv, dh, 512, 2048, 1e4, "bf16" if bf16 else "f32",
+                        wfmt="mxfp4" if fmt == "mxfp4" else "dtype")
+    b = build_model(shape, 31, max_sessions=max_sessions, max_tokens=64)
+    lengths = [1300, 1, 640, 255, 900]
+    text = synth.cpu_tokens(max(lengths), 31, 1, shape.vocab)
+    pool, _, _ = _pool(torch, spp, 2, nkv, dh, bf16, page, sum(-(-(m + steps) // page) for m in lengths), max_seqs=8)
+    seqs, w = [], oracle.Weights(shape, 31)
+    sess = spp.Session(b.model, max(lengths) + 8)
+    sess.append_delta(text.tolist())
+    for m in lengths:                                  # (a prefix's cells do not depend on what follows)
+        sess.restore(m)
+        seqs.append(pool.create())
+        pool.import_session(seqs[-1], sess)
+    toks = synth.cpu_tokens(len(lengths) * steps, 32, 2, shape.vocab).reshape(-1, steps)
+    kv = oracle.KVState(shape, max(lengths) + steps)
+    oracle.forward(w, kv, 0, text, logits=False)
+    want = {}                                          # longest first: the cells overwritten are past the next ones'
+    for i in sorted(range(len(lengths)), key=lambda i: -lengths[i]):
+        for t in range(steps):
+            want[i, t] = oracle.forward(w, kv, lengths[i] + t, toks[i, t:t + 1])
+    dists = [torch.empty(shape.vocab, dtype=torch.float32, device="cuda") for _ in seqs]
+    worst = 0.0
+    for t in range(steps):
+        spp.decode_batch(pool, b.model, seqs, toks[:, t].tolist(), dists)
+        for i, d in enumerate(dists):
+            worst = max(worst, max_abs(d.cpu().numpy(), want[i, t]))
+        assert [s.position for s in pool.summaries(seqs)] == [m + t + 1 for m in lengths]
+    log(f"paged decode {fmt} {heads} to {max(lengths)} cells: max |logit - oracle| {worst:.2e}")
+    assert worst <= (5e-2 if bf16 else 1e-4)
