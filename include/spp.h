@@ -508,8 +508,8 @@ spp_status spp_seq_fork(spp_pool_t pool, int32_t src, int32_t n, int32_t* seqs_o
  * pool's earlier work, also where nothing is copied.  SPP_E_CAPACITY when the pages run out. */
 spp_status spp_seq_reserve(spp_pool_t pool, int32_t n, const int32_t* seqs, int32_t cells,
                            void* stream);
-/* Declares the next `cells` reserved cells written: n_cells <- n_cells + cells.
- * SPP_E_STATE if they were not reserved. */
+/* Declares the next `cells` cells written: n_cells <- n_cells + cells.  SPP_E_STATE unless
+ * pages of the sequence's own hold them, as after spp_seq_reserve. */
 spp_status spp_seq_commit(spp_pool_t pool, int32_t seq, int32_t cells);
 /* Discards cells: n_cells <- min(n_cells, n), and gives up the pages past them. */
 spp_status spp_seq_truncate(spp_pool_t pool, int32_t seq, int32_t n);
@@ -517,7 +517,7 @@ spp_status spp_seq_truncate(spp_pool_t pool, int32_t seq, int32_t n);
 /* The sequence becomes a copy of the session's committed cells (its former cells are given
  * up): every layer's cells [0, n_s) into pages of its own.  The session is only read.  Asynchronous
  * on `stream`, ordered after the device work of the session's model as well, and before its
- * next (as spp_seq_export).
+ * next (as spp_seq_export); the session's buffer stays until the copy has run.
  * SPP_E_INVALID_ARG unless the session's model has the pool's layers, kv heads, head_dim and
  * dtype and lives on its device; SPP_E_CAPACITY when the pages run out. */
 spp_status spp_seq_import(spp_pool_t pool, int32_t seq, spp_session_t session, void* stream);
@@ -602,7 +602,9 @@ spp_status spp_paged_attention(const spp_paged_attn* a, void* work, size_t work_
  *   y = y + bias[i]                                if bias_tokens[i] = v (the last such i)
  *   y = fill                                       if the allowed set lacks v
  * every operation in fp32 with its own rounding.  Entries of tokens and bias_tokens
- * outside [0, vocab) are skipped. */
+ * outside [0, vocab) are skipped: a row may keep one array of tokens, filled with -1 behind a
+ * history that grows in place.  Every part of a row reads the whole list, so its length counts,
+ * skipped entries too. */
 typedef struct {
   const float* src;             /* device, [vocab]                                        */
   float* dst;                   /* device, [vocab]; may be src                            */

@@ -796,7 +796,8 @@ class PagedAttention:
 @dataclasses.dataclass
 class AdjustRow:
     """One row of adjusted logits (spp_adjust): src and dst fp32 device tensors of the
-    vocabulary, tokens / bias_tokens int32, bias fp32, allowed a bitmap of int32 words."""
+    vocabulary, tokens / bias_tokens int32, bias fp32, allowed a bitmap of int32 words.  Entries
+    of tokens outside the vocabulary are skipped."""
     src: object
     dst: object
     tokens: object = None
@@ -835,7 +836,11 @@ class LogitsAdjust:
     """spp_adjust_logits with its rows marshalled once: each call() adjusts them and returns
     their AdjustSummaries (None with summaries=False), which the next call overwrites.  The
     workspace is held here: one call at a time, and the object lives until its calls have
-    finished."""
+    finished.
+
+    A decode keeps one object over its steps: the rows' tensors are fixed, what they hold is read
+    at each call.  A history that grows is a tensor with room for it, -1 behind its tokens; an
+    object made anew takes the host some 10 us a row."""
 
     def __init__(self, vocab: int, rows: Sequence[AdjustRow], summaries: bool = True):
         import torch

@@ -7,12 +7,14 @@
 // Bound by memory: a row's logits are read and written once (8 bytes a token).  What each
 // token needs to know of the history -- whether it occurs, and how often past the prompt -- is
 // gathered per workgroup: it owns a slice of the vocabulary, reads the whole list of tokens
-// (from L2 after the first workgroup; a history is a few KB against 8 bytes per token of the
-// vocabulary) and counts those of its slice in LDS with integer atomics, whose order does not
-// matter.  The largest index of a bias entry is kept the same way, so the last entry of a token
+// (from L2 after the first workgroup) and counts those of its slice in LDS with integer atomics,
+// whose order does not matter.  That suits histories of some thousand tokens, a few KB; long ones
+// outweigh the logits: 64 rows of 128256 take, from a graph, 20.0 us with 2000 tokens each, 28.7 with
+// 8000 and 55 with 32768, one row 7.2 with 6000 and 14.4 with 32768.  The largest index of a bias entry is kept the same way, so the last entry of a token
 // counts.  Nothing of the vocabulary's size besides the logits is written, cleared or read again.
-// Measured (with the launch that merges the slices' reductions): 64 rows of 128256 19.2 us,
-// 3.4 TB/s.  One row is launches and latency: 6.9 us from a graph, 8 through the binding.
+// Measured (with the launch that merges the slices' reductions): 64 rows of 128256 with 2000 tokens
+// 19.3 us through the binding, 3.4 TB/s.  One row is launches and latency: 7.2 us from a graph, 8
+// through the binding.
 #include "common.hpp"
 #include "paged.hpp"
 
@@ -84,7 +86,7 @@ __device__ __forceinline__ void part_merge(float4& a, const float4& b) {
 //  - a slice of whole units has a path without a look at the row's ends;
 //  - the reductions start from the wave's largest value (no running maximum, the index only where
 //    it is), by data-parallel moves.
-// 64 rows of 128256 with 2000 tokens and 100 biases, with the summaries: 19.2 us.  Before the
+// 64 rows of 128256 with 2000 tokens and 100 biases, with the summaries: 19.3 us.  Before the
 // stores' and the merge's own steps (then 23.1): a wave that adjusts all its tokens wherever one
 // lane needs it 32.3; a list of the touched tokens made by the counting 30.4; their logits kept
 // in LDS 27.0; without the last two of these points 26.3.
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(kTpb) void adjust_kernel(int V, AdjustBatch<R> jobs
 
   // Masked and stored; then x holds the allowed values, -inf elsewhere.  The stores pass the L2 by:
   // nothing here reads them, and lines that wait there are written back between this launch and
-  // the next (64 rows of 128256: 22.9 us so, 20.7 past it; loads past it too 21.8).
+  // the next (64 rows of 128256 when this was chosen: 22.9 us so, 20.7 past it; loads past it too 21.8).
   uint32_t live = kAll;   // a bit per value: in the row and allowed
   float low = INFINITY;   // the smallest allowed value
   if (pair && whole) {
@@ -334,9 +336,9 @@ __global__ __launch_bounds__(64) void adjust_merge_kernel(int nb, const float4* 
 }
 
 // Tokens of a slice: 1024 while that makes under 2048 workgroups, else 2048, which halves how
-// often a history is read and the instructions of a workgroup beside its tokens' own (64 rows of
-// 128256 with 2000 tokens each: 20.7 us, with slices of 1024 23.1, with slices of 4096, half as
-// many waves to a CU, 22.5; 17 rows of 152063 with 700: 10.1, 10.4 and 10.9).
+// often a history is read and the instructions of a workgroup beside its tokens' own (from a
+// graph, 64 rows of 128256 with 2000 tokens each: 20.0 us, with slices of 1024 22.7, with slices of
+// 4096, half as many waves to a CU, 20.0; 17 rows of 152063 with 700: 9.9, 10.7 and 10.7).
 int slice_units(int n, int vocab) { return (int64_t)vocab * n <= kShortSliceTokens ? 1 : 2; }
 // Slices of a row, whatever its alignment.
 int slices(int units, int vocab) { return (vocab + 3 + units * 4 * kTpb - 1) / (units * 4 * kTpb); }
@@ -363,7 +365,7 @@ hipError_t adjust_logits(int n, int vocab, const spp_adjust* rows, spp_summary* 
                          hipStream_t st) {
   const int units = slice_units(n, vocab), nb = slices(units, vocab);
   // launches of like size: what is left over a multiple of kManyRows would not fill the chip (64
-  // rows of 128256: 20.7 us as 48 and 16, 20.1 as 32 and 32)
+  // rows of 128256 from a graph: 20.4 us as 48 and 16, 20.0 as 32 and 32)
   const int launches = (n - 1) / kManyRows + 1, step = (n - 1) / launches + 1;
   for (int r0 = 0; r0 < n; r0 += step) {
     const int m = n - r0 < step ? n - r0 : step;

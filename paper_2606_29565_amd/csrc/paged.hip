@@ -25,7 +25,7 @@
 // of U[1024, 8192] cells, 8 heads of 128, 1.14 GB, against 220, and 289 against 259 with
 // loads that bypass the L2.)
 // The next trip's keys are loaded once this trip's scores are formed, its values once this
-// trip's sums are: one register set of each (236 of the 256 that two waves a SIMD have), and
+// trip's sums are: one register set of each (236, with fp32 queries 252, of the 256 that two waves a SIMD have), and
 // always one of the two in flight.
 #include <algorithm>
 #include <cmath>
