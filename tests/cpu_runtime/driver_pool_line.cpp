@@ -345,6 +345,43 @@ void later_work_holds_no_step() {
   }
 }
 
+// More models wait for copies of one pool than it has events: each still comes after its own copy,
+// with the pool's later work in between or not, and when it has waited its event is the pool's again.
+void more_models_than_events() {
+  constexpr int kModels = 6;
+  Streams st;
+  Pool pool(64, 8);
+  Model models[kModels] = {Model(20), Model(20), Model(20), Model(20), Model(20), Model(20)};
+  for (int round = 0; round < 4; ++round) {
+    std::atomic<bool> copied[kModels] = {};
+    bool after[kModels] = {};
+    std::vector<int> seqs;
+    for (int i = 0; i < kModels; ++i) {
+      seqs.push_back(pool.create(0));
+      stub::enqueue(st[0], [&, i] {
+        std::this_thread::sleep_for(std::chrono::milliseconds(3));
+        copied[i] = true;
+      });
+      CHECK(spp_seq_import(pool.p, seqs[i], models[i].s, st[0]) == SPP_OK);
+      int32_t f = -1;
+      if (i & 1) {
+        CHECK(spp_seq_fork(pool.p, seqs[i], 1, &f) == SPP_OK && spp_seq_reserve(pool.p, 1, &f, 1, st[0]) == SPP_OK);
+        CHECK(spp_seq_free(pool.p, f) == SPP_OK);
+      }
+    }
+    for (int i = 0; i < kModels; ++i) {
+      if (round == 1 && i % 2) continue;  // (these keep waiting for theirs)
+      CHECK(spp_shift(models[i].s, 1, st[1]) == SPP_OK);
+      stub::enqueue(st[1], [&, i] { after[i] = copied[i]; });
+    }
+    hipDeviceSynchronize();
+    for (int i = 0; i < kModels; ++i) {
+      CHECK(after[i] || (round == 1 && i % 2));
+      CHECK(spp_seq_free(pool.p, seqs[i]) == SPP_OK && spp_session_restore(models[i].s, 20) == SPP_OK);
+    }
+  }
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
@@ -355,6 +392,7 @@ int main(int argc, char** argv) {
       {"failed_reserve_changes_nothing", failed_reserve_changes_nothing},
       {"workspace_of_smaller_calls", workspace_of_smaller_calls},
       {"later_work_holds_no_step", later_work_holds_no_step},
+      {"more_models_than_events", more_models_than_events},
   };
   const auto it = argc > 1 ? scenarios.find(argv[1]) : scenarios.end();
   if (it == scenarios.end()) return 2;

@@ -14,7 +14,7 @@ SANITIZERS = {"asan": ["-fsanitize=address,undefined", "-fno-omit-frame-pointer"
               "tsan": ["-fsanitize=thread"]}
 SCENARIOS = ["reserve_orders", "failed_page_copy", "failed_session_copy",
              "failed_reserve_changes_nothing", "later_work_holds_no_step",
-             "workspace_of_smaller_calls"]
+             "more_models_than_events", "workspace_of_smaller_calls"]
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not available")
 
