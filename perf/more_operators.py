@@ -1,0 +1,570 @@
+"""The operators of a decode over caches held in 8 bits, measured one at a time.
+
+Three operators: quantising a cache as it is written (new cells of many sequences into pages and
+back, a session's cells into pages and back); attention of one new token per sequence over such
+pages; log probabilities of given tokens with the entropy and the top alternatives, by which
+continuations are compared.  With ``own`` false ``run`` computes them in elementary torch
+operations in 32 bits, with ``own`` true it makes the calls of the public binding.
+
+A cell's element is an 8-bit code, a signed integer ("i8") or a float of 4 exponent and 3 mantissa
+bits ("e4m3"), times the scale of its block: 16 cells of one head, keys and values apart.  The
+scale is the smallest power of two s with max |x| / s <= 127 (448 in e4m3) over the cells written, not below
+2^-100, and not below the scale of the cells that the block keeps, whose codes are rounded to a
+scale that grew.  Rounding is to the nearest, ties to even.
+
+A page holds, per layer, the codes of K as [kv head][cell][dim] and of V as [kv head][dim][cell],
+then the fp32 scales of K as [kv head][block] and of V likewise, and fills up to 128 bytes.  A session's
+buffer holds, per layer, K as [kv head][capacity][dim] and V as [kv head][dim][capacity], the
+capacity rounded up to 64 cells.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+# query heads, kv heads, head_dim, element type of what is written, read and asked
+HEADS = {
+    "tiny-f32": (4, 4, 64, "f32"),
+    "small": (4, 2, 64, "bf16"),
+    "8b": (32, 8, 128, "bf16"),
+    "32b": (64, 8, 128, "bf16"),
+    "thirds": (6, 2, 64, "bf16"),
+    "one-kv": (20, 1, 128, "bf16"),
+}
+DEV = "cuda"
+BLOCK = 16
+
+
+def listed():
+    return [
+        # short and empty sequences of the small model, pages dropped from the middle
+        {"name": "attn8_small_holes", "op": "attention", "code": "i8", "heads": "small", "n": 37, "cells": 700,
+         "page": 16, "ragged": True, "holes": 0.2},
+        # a decode step after a fall-through: one continuation of a streaming session
+        {"name": "attn8_8b_one", "op": "attention", "code": "i8", "heads": "8b", "n": 1, "cells": 8192,
+         "page": 64, "ragged": False, "holes": 0.0},
+        # 64 sequences of unequal lengths, as in the batched workload
+        {"name": "attn8_8b_ragged64", "op": "attention", "code": "i8", "heads": "8b", "n": 64, "cells": 8192,
+         "page": 64, "ragged": True, "holes": 0.0},
+        # a few continuations of a long history, the 32B heads, in floats
+        {"name": "attn8_32b_long", "op": "attention", "code": "e4m3", "heads": "32b", "n": 3, "cells": 32749,
+         "page": 128, "ragged": False, "holes": 0.0},
+        # one new token of the fp32 model of the smoke tests: launches and latency
+        {"name": "write_tiny_f32", "op": "write", "code": "i8", "heads": "tiny-f32", "n": 1, "before": 500,
+         "cells": 1, "page": 16},
+        # one new token of each of 64 sequences
+        {"name": "write_8b_step64", "op": "write", "code": "i8", "heads": "8b", "n": 64, "before": 4000,
+         "cells": 1, "page": 64},
+        # the cells of a few prompts of unequal lengths behind a shared beginning, in floats
+        {"name": "write_8b_prompts", "op": "write", "code": "e4m3", "heads": "8b", "n": 5, "before": 1000,
+         "cells": 4096, "page": 64},
+        # a session's cells into pages and into another session
+        {"name": "import8_8b", "op": "import", "code": "i8", "heads": "8b", "layers": 4, "cells": 8100,
+         "page": 64},
+        # one row of the tiny model's vocabulary, the token that was taken
+        {"name": "logp_tiny", "op": "logprobs", "vocab": 4096, "n": 1, "tokens": 1, "top": 0, "allowed": 1.0},
+        # one decode step with twenty alternatives
+        {"name": "logp_one", "op": "logprobs", "vocab": 128256, "n": 1, "tokens": 1, "top": 20, "allowed": 1.0},
+        # 64 continuations compared
+        {"name": "logp_64", "op": "logprobs", "vocab": 128256, "n": 64, "tokens": 4, "top": 8, "allowed": 1.0},
+        # an odd vocabulary, half of it masked, a fast-answer set's tokens and many alternatives
+        {"name": "logp_odd", "op": "logprobs", "vocab": 152063, "n": 17, "tokens": 64, "top": 50, "allowed": 0.5},
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(("attention", "attention", "write", "import", "logprobs", "logprobs"))
+    if op == "logprobs":
+        return {"op": op, "vocab": _log(rng, 2000, 160000), "n": _log(rng, 1, 52),
+                "tokens": rng.choice((1, _log(rng, 1, 100))), "top": rng.choice((0, _log(rng, 1, 64))),
+                "allowed": rng.choice((1.0, rng.uniform(0.05, 0.9)))}
+    page, code = rng.choice((16, 32, 64, 128, 256)), rng.choice(("i8", "e4m3"))
+    if op == "attention":
+        heads = rng.choice(sorted(set(HEADS) - {"tiny-f32"}))
+        n = _log(rng, 1, 64)
+        return {"op": op, "code": code, "heads": heads, "n": n,
+                "cells": min(_log(rng, 1, 32768), 262144 // n), "page": page,
+                "ragged": rng.random() < 0.6, "holes": rng.choice((0.0, 0.0, rng.uniform(0.0, 0.5)))}
+    if op == "import":
+        return {"op": op, "code": code, "heads": rng.choice(("tiny-f32", "small", "8b", "8b")),
+                "layers": rng.randint(1, 4), "cells": _log(rng, 1, 8192), "page": page}
+    n = _log(rng, 1, 64)
+    return {"op": op, "code": code, "heads": rng.choice(sorted(HEADS)), "n": n,
+            "before": rng.choice((0, _log(rng, 1, 2000))),
+            "cells": rng.choice((1, min(_log(rng, 1, 4096), 16384 // n))), "page": page}
+
+
+# ---- inputs -------------------------------------------------------------------------------
+
+
+def _gen(seed, stream):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1000003 * seed + stream)
+    return g
+
+
+def _dtype(case):
+    return torch.float32 if HEADS[case["heads"]][3] == "f32" else torch.bfloat16
+
+
+def _normal(shape, dtype, g, sigma=1.0):
+    """Normal values; a large tensor is a block of 2^22 + 1 of them over and over, which is
+    quick and lines up with no row."""
+    n = math.prod(shape)
+    block = torch.empty(min(n, (1 << 22) + 1), device=DEV).normal_(0.0, sigma, generator=g)
+    block = block.clamp(-127, 127).round().to(dtype) if dtype == torch.int8 else block.to(dtype)
+    if block.numel() == n:
+        return block.view(shape)
+    return block.repeat(-(-n // block.numel()))[:n].view(shape)
+
+
+def _half(case):
+    """Bytes of a layer's codes of K (or V) in a page."""
+    _, nkv, dh, _ = HEADS[case["heads"]]
+    return nkv * case["page"] * dh
+
+
+def _layer_bytes(case):
+    scales = 8 * HEADS[case["heads"]][1] * (case["page"] // BLOCK)
+    return 2 * _half(case) + -(-scales // 128) * 128
+
+
+def _views(case, pages):
+    """Codes of K [page, layer, head, cell, dim] and V [page, layer, head, dim, cell], scales of
+    both [page, layer, head, block], of a buffer of pages."""
+    _, nkv, dh, _ = HEADS[case["heads"]]
+    page, half, blocks = case["page"], _half(case), case["page"] // BLOCK
+    fmt = torch.int8 if case["code"] == "i8" else torch.float8_e4m3fn
+    head = pages.shape[:2]
+    sc = pages[:, :, 2 * half:2 * half + 8 * nkv * blocks].view(torch.float32).view(*head, 2, nkv, blocks)
+    return (pages[:, :, :half].view(fmt).view(*head, nkv, page, dh),
+            pages[:, :, half:2 * half].view(fmt).view(*head, nkv, dh, page), sc[:, :, 0], sc[:, :, 1])
+
+
+def _pages(case, count, layers, g):
+    """Pages as earlier writes left them: normal cells of differing sizes, quantised."""
+    pages = torch.zeros(count, layers, _layer_bytes(case), dtype=torch.uint8, device=DEV)
+    half = _half(case)
+    if case["code"] == "i8":
+        codes = _normal((count, layers, 2 * half), torch.int8, g, 32.0)
+    else:
+        codes = _normal((count, layers, 2 * half), torch.float8_e4m3fn, g, 80.0)
+    pages[:, :, :2 * half] = codes.view(torch.uint8)
+    ks, vs = _views(case, pages)[2:]
+    for s in (ks, vs):
+        s.copy_(torch.exp2(torch.randint(-7, -3, s.shape, generator=g, device=DEV).float()))
+    return pages
+
+
+def _lengths(case):
+    """Cells of each sequence: from the case alone, so that its work is known."""
+    n, cells = case["n"], case["cells"]
+    if not case["ragged"]:
+        return np.full(n, cells)
+    r = np.random.RandomState(cells + 31 * n + case["page"])  # down to an eighth; one in 16 is empty
+    lengths = r.randint(max(1, cells // 8), cells + 1, n)
+    lengths[r.rand(n) < 1 / 16] = 0
+    return lengths
+
+
+def _spans(case):
+    """First new cell and number of new cells of each sequence, from the case alone."""
+    r = np.random.RandomState(case["before"] + 31 * case["n"] + case["cells"])
+    first = r.randint(case["before"] // 2, case["before"] + 1, case["n"])
+    return first, r.randint(-(-case["cells"] // 2), case["cells"] + 1, case["n"])
+
+
+def _rows(counts):
+    return np.concatenate([[0], np.cumsum(counts)])
+
+
+def _i32(a):
+    return torch.from_numpy(np.asarray(a)).to(DEV, torch.int32)
+
+
+def _attention_inputs(case, seed):
+    nq, nkv, dh, _ = HEADS[case["heads"]]
+    n, cells, page = case["n"], case["cells"], case["page"]
+    g = _gen(seed, 1)
+    width = -(-cells // page)
+    count = n * width + 3
+    # the pages of a sequence lie anywhere, as they do after hours of serving
+    table = torch.randperm(count, generator=g, device=DEV)[:n * width].view(n, width).to(torch.int32)
+    if case["holes"]:
+        table[torch.rand(n, width, generator=g, device=DEV) < case["holes"]] = -1
+    return {"pages": _pages(case, count, 1, g), "table": table, "lengths": _i32(_lengths(case)),
+            "q": _normal((n, nq, dh), _dtype(case), g, 1.5)}
+
+
+def _write_inputs(case, seed):
+    _, nkv, dh, _ = HEADS[case["heads"]]
+    n, page, g = case["n"], case["page"], _gen(seed, 2)
+    first, counts = _spans(case)
+    width = -(-(case["before"] + case["cells"]) // page)
+    start = first - first % BLOCK  # the blocks that are written begin here
+    rows, back = _rows(counts), _rows(first + counts - start)
+    total = int(rows[-1])
+    # one head in eight has keys of several times the others' size
+    size = torch.where(torch.arange(nkv, device=DEV) % 8 == 1, 6.0, 1.0)[:, None]
+    make = lambda: (_normal((total, nkv, dh), torch.float32, g) * size).to(_dtype(case))  # noqa: E731
+    table = torch.randperm(n * width, generator=g, device=DEV).view(n, width).to(torch.int32)
+    empty = lambda: torch.empty(int(back[-1]), nkv, dh, dtype=_dtype(case), device=DEV)  # noqa: E731
+    return {"pages": _pages(case, n * width, 1, g), "table": table, "first": _i32(first), "rows": _i32(rows),
+            "start": _i32(start), "back": _i32(back), "k": make(), "v": make(), "k_back": empty(),
+            "v_back": empty()}
+
+
+def _import_inputs(case, seed):
+    _, nkv, dh, _ = HEADS[case["heads"]]
+    dt, g = _dtype(case), _gen(seed, 3)
+    cap = -(-case["cells"] // 64) * 64
+    shape = (case["layers"], 2, nkv * cap * dh)
+    return {"kv": _normal(shape, dt, g), "other": _normal(shape, dt, g),
+            "pages": _pages(case, -(-case["cells"] // case["page"]), case["layers"], g)}
+
+
+def _logprobs_inputs(case, seed):
+    n, V, g = case["n"], case["vocab"], _gen(seed, 4)
+    x = torch.empty(n, V, device=DEV).normal_(0.0, 2.0, generator=g)
+    if case["allowed"] < 1.0:  # what an adjusted row looks like behind a grammar
+        x[torch.rand(n, V, device=DEV, generator=g) >= case["allowed"]] = -math.inf
+    x[:, V // 3] = 9.0  # a token that stands out
+    tokens = torch.randint(0, V, (n, case["tokens"]), device=DEV, generator=g)
+    tokens[:, 0] = V // 3
+    return {"logits": x, "tokens": tokens.to(torch.int32)}
+
+
+INPUTS = {"attention": _attention_inputs, "write": _write_inputs, "import": _import_inputs,
+          "logprobs": _logprobs_inputs}
+
+
+def prepare(case, seed):
+    s = {"case": case, **INPUTS[case["op"]](case, seed)}
+    if own:
+        _handles(s)
+    return s
+
+
+def _handles(s):
+    """What a user's program makes once of the framework's objects."""
+    import paper_2606_29565_amd as spp
+
+    case = s["case"]
+    if case["op"] == "logprobs":
+        s["call"] = spp.LogProbs(case["vocab"], list(s["logits"]), tokens=s["tokens"], top=case["top"])
+        return
+    nq, nkv, dh, fmt = HEADS[case["heads"]]
+    layers = case.get("layers", 1)
+    s["pool"] = spp.PagePool(layers, nkv, dh, fmt == "bf16", case["page"], s["pages"].shape[0],
+                             max_seqs=4, pages=s["pages"], cells=case["code"])
+    if case["op"] == "attention":
+        s["call"] = spp.PagedAttention(s["pool"], 0, nq, s["table"], s["lengths"], io_bf16=fmt == "bf16")
+        s["o"] = torch.empty_like(s["q"])
+    elif case["op"] == "write":
+        most = case["cells"]
+        s["new"] = spp.PagedCells(s["pool"], 0, s["table"], s["first"], s["rows"], most, io_bf16=fmt == "bf16")
+        s["written"] = spp.PagedCells(s["pool"], 0, s["table"], s["start"], s["back"], most + BLOCK - 1,
+                                      io_bf16=fmt == "bf16")
+    else:
+        # the sessions of a model with these cells; the copies read nothing else of it
+        dt, d, ffn, vocab = _dtype(case), 64, 64, 64
+        shapes = {"wq": (nkv * dh, d), "wk": (nkv * dh, d), "wv": (nkv * dh, d), "wo": (d, nkv * dh),
+                  "w_gate": (ffn, d), "w_up": (ffn, d), "w_down": (d, ffn), "attn_norm": (d,),
+                  "mlp_norm": (d,)}
+        w = {k: [torch.zeros(v, dtype=dt, device=DEV)] * layers for k, v in shapes.items()}
+        w.update(embed=torch.zeros(vocab, d, dtype=dt, device=DEV),
+                 final_norm=torch.zeros(d, dtype=dt, device=DEV),
+                 lm_head=torch.zeros(vocab, d, dtype=dt, device=DEV))
+        s["model"] = spp.Model(layers, d, nkv, nkv, dh, ffn, vocab, 1e4, fmt == "bf16", w, max_tokens=1)
+        s["session"] = spp.Session(s["model"], case["cells"], kv=s["kv"])
+        s["session"].restore(case["cells"])
+        s["into"] = spp.Session(s["model"], case["cells"], kv=s["other"])
+
+
+# ---- one pass -------------------------------------------------------------------------------
+
+
+def run(s):
+    if own:
+        return {"attention": _own_attention, "write": _own_write, "import": _own_import,
+                "logprobs": _own_logprobs}[s["case"]["op"]](s)
+    return {"attention": _plain_attention, "write": _plain_write, "import": _plain_import,
+            "logprobs": _plain_logprobs}[s["case"]["op"]](s)
+
+
+def _own_attention(s):
+    s["call"](s["q"], s["o"])
+    return s["o"]
+
+
+def _own_write(s):
+    """New cells into the pages; then the blocks that they touched, as values."""
+    s["new"].write(s["k"], s["v"])
+    s["written"].read(s["k_back"], s["v_back"])
+    return {"k": s["k_back"], "v": s["v_back"]}
+
+
+def _own_import(s):
+    seq = s["pool"].create(0)
+    s["pool"].import_session(seq, s["session"])
+    s["pool"].export_session(seq, s["into"])
+    s["pool"].free(seq)
+    return {"other": s["other"]}
+
+
+def _own_logprobs(s):
+    r = s["call"]()
+    return {"logprobs": r.logprobs, "lse": r.lse, "entropy": r.entropy, "top_tokens": r.top_tokens,
+            "top_logprobs": r.top_logprobs}
+
+
+def _plain_scale(case, top):
+    """The smallest power of two s with top / s <= 127 (448), not below 2^-100."""
+    m, e = torch.frexp(top)
+    if case["code"] == "i8":
+        e = torch.where(m <= 127 / 128, e - 7, e - 6)
+    else:
+        e = torch.where(m <= 448 / 512, e - 9, e - 8)
+    return torch.ldexp(torch.ones_like(top), torch.where(top > 0, e, -100).clamp(min=-100))
+
+
+def _plain_codes(case, x):
+    return x.round().to(torch.int8) if case["code"] == "i8" else x.to(torch.float8_e4m3fn)
+
+
+def _plain_attention(s):
+    case = s["case"]
+    nq, nkv, dh, _ = HEADS[case["heads"]]
+    n, page = case["n"], case["page"]
+    width = s["table"].shape[1]
+    kc, vc, ks, vs = (t[:, 0] for t in _views(case, s["pages"]))
+    at = s["table"].clamp(min=0).long()
+    bits = torch.uint8  # (codes are gathered as bytes: not every type can be indexed)
+    K = kc.view(bits)[at].view(kc.dtype).float() * ks[at].repeat_interleave(BLOCK, 3)[..., None]
+    V = vc.view(bits)[at].view(vc.dtype).float() * vs[at].repeat_interleave(BLOCK, 3)[..., None, :]
+    K = K.permute(0, 2, 1, 3, 4).reshape(n, nkv, width * page, dh)
+    V = V.permute(0, 2, 1, 4, 3).reshape(n, nkv, width * page, dh)
+    live = torch.arange(width * page, device=DEV) < s["lengths"][:, None]
+    live = live & (s["table"] >= 0).repeat_interleave(page, dim=1)
+    q = s["q"].float().view(n, nkv, nq // nkv, dh)
+    scores = torch.matmul(q, K.transpose(2, 3).contiguous()) / math.sqrt(dh)
+    scores = scores.masked_fill(~live[:, None, None], -math.inf)
+    top = scores.amax(3, keepdim=True).clamp(min=-1e30)  # an empty row has no maximum
+    e = torch.exp(scores - top)
+    total = e.sum(3, keepdim=True)
+    out = torch.matmul(e, V) / torch.where(total > 0, total, torch.ones_like(total))
+    return out.view(n, nq, dh).to(s["q"].dtype)
+
+
+def _plain_write(s):
+    case = s["case"]
+    _, nkv, dh, _ = HEADS[case["heads"]]
+    n, page = case["n"], case["page"]
+    kc, vc, ks, vs = (t[:, 0] for t in _views(case, s["pages"]))
+    first, start = s["first"].long(), s["start"].long()
+    row0, end = s["rows"].long()[:-1], s["first"].long() + (s["rows"][1:] - s["rows"][:-1]).long()
+    blocks = (case["cells"] + BLOCK - 2) // BLOCK + 1  # the most that a sequence touches
+    at = start[:, None, None] + torch.arange(blocks * BLOCK, device=DEV).view(1, blocks, BLOCK)
+    new = (at >= first[:, None, None]) & (at < end[:, None, None])
+    kept = at < first[:, None, None]
+    touched = new.any(2)
+    b0 = torch.where(touched, at[:, :, 0], 0)
+    pg = torch.gather(s["table"].long(), 1, b0 // page)
+    blk, cell = b0 % page // BLOCK, b0[..., None] % page + torch.arange(BLOCK, device=DEV)
+    row = (at - first[:, None, None] + row0[:, None, None]).clamp(0, s["k"].shape[0] - 1)
+    bits, heads, dims = torch.uint8, torch.arange(nkv, device=DEV), torch.arange(dh, device=DEV)
+    # of both, [sequence, block, cell, head, dim]
+    kat = (pg[:, :, None, None, None], heads[:, None], cell[..., None, None], dims)
+    vat = (pg[:, :, None, None, None], heads[:, None], dims, cell[..., None, None])
+    back = (at < end[:, None, None]) & touched[..., None]
+
+    def put(rows, codes, index, scales):
+        x = rows.float()[row]
+        old = scales[pg, :, blk]  # [sequence, block, head]
+        top = torch.where(new[..., None, None], x.abs(), torch.zeros_like(x)).amax((2, 4))
+        scale = _plain_scale(case, top)
+        scale = torch.where(kept.any(2)[..., None], torch.maximum(scale, old), scale)
+        was = codes.view(bits)[index].view(codes.dtype).float() * old[:, :, None, :, None]
+        x = torch.where(new[..., None, None], x, torch.where(kept[..., None, None], was, torch.zeros_like(x)))
+        c = _plain_codes(case, x / scale[:, :, None, :, None])
+        codes.view(bits)[tuple(i.expand(c.shape)[touched] for i in index)] = c.view(bits)[touched]
+        scales[pg[touched], :, blk[touched]] = scale[touched]
+        return (c.float() * scale[:, :, None, :, None])[back].to(rows.dtype)
+
+    return {"k": put(s["k"], kc, kat, ks), "v": put(s["v"], vc, vat, vs)}
+
+
+def _plain_import(s):
+    case = s["case"]
+    _, nkv, dh, _ = HEADS[case["heads"]]
+    L, n, page = case["layers"], case["cells"], case["page"]
+    cap, count = s["kv"].shape[2] // (nkv * dh), -(-n // page)
+    kc, vc, ks, vs = _views(case, s["pages"])
+    K, V = s["kv"][:, 0].view(L, nkv, cap, dh), s["kv"][:, 1].view(L, nkv, dh, cap).transpose(2, 3)
+    K2, V2 = s["other"][:, 0].view(L, nkv, cap, dh), s["other"][:, 1].view(L, nkv, dh, cap).transpose(2, 3)
+
+    def put(x, codes, scales, other, turned):
+        cells = torch.zeros(L, nkv, count * page, dh, device=DEV)
+        cells[:, :, :n] = x[:, :, :n]
+        b = cells.view(L, nkv, -1, BLOCK, dh)
+        scale = _plain_scale(case, b.abs().amax((3, 4)))
+        c = _plain_codes(case, b / scale[..., None, None])
+        c = c.view(L, nkv, count, page, dh).permute(2, 0, 1, 3, 4)
+        codes.copy_(c.transpose(3, 4) if turned else c)
+        scales.copy_(scale.view(L, nkv, count, page // BLOCK).permute(2, 0, 1, 3))
+        held = codes.float().transpose(3, 4) if turned else codes.float()
+        held = held * scales.repeat_interleave(BLOCK, 3)[..., None]
+        other[:, :, :n] = held.permute(1, 2, 0, 3, 4).reshape(L, nkv, count * page, dh)[:, :, :n].to(other.dtype)
+
+    put(K, kc, ks, K2, False)
+    put(V, vc, vs, V2, True)
+    return {"other": s["other"]}
+
+
+def _plain_logprobs(s):
+    case, x = s["case"], s["logits"]
+    m = x.amax(1, keepdim=True)
+    e = torch.exp(x - m)
+    total = e.sum(1, keepdim=True)
+    lse = m + torch.log(total)
+    weighed = torch.where(e > 0, e * (x - m), torch.zeros_like(e))  # what is masked weighs nothing
+    entropy = torch.log(total) - weighed.sum(1, keepdim=True) / total
+    # in order of the value, the lower index first where two are the same
+    value, index = torch.sort(x, dim=1, descending=True, stable=True)
+    return {"logprobs": torch.gather(x, 1, s["tokens"].long()) - lse, "lse": lse[:, 0], "entropy": entropy[:, 0],
+            "top_tokens": index[:, :case["top"]].to(torch.int32), "top_logprobs": value[:, :case["top"]] - lse}
+
+
+# ---- what a pass cannot do without --------------------------------------------------------
+
+
+def work(case):
+    if case["op"] == "logprobs":
+        n, V = case["n"], case["vocab"]
+        return {"bytes": int(n * (4 * V + 8 * case["tokens"] + 8 * case["top"] + 8)), "flops": int(n * 5 * V)}
+    nq, nkv, dh, fmt = HEADS[case["heads"]]
+    elem = 4 if fmt == "f32" else 2
+    codes = 2 * nkv * (dh + 4 / BLOCK)  # a cell's codes and its share of the scales
+    if case["op"] == "attention":
+        cells = int(_lengths(case).sum()) * (1 - case["holes"])
+        return {"bytes": int(cells * codes + 2 * case["n"] * nq * dh * elem), "flops": int(4 * cells * nq * dh)}
+    given = 2 * nkv * dh * elem
+    if case["op"] == "write":  # rows read, codes written; then codes read, rows written
+        first, counts = _spans(case)
+        back = int((first % BLOCK + counts).sum())
+        return {"bytes": int(counts.sum() * (given + codes) + back * (given + codes)), "flops": 0}
+    # a session's cells read, codes written and read, the other session's cells written
+    return {"bytes": int(2 * case["cells"] * case["layers"] * (given + codes)), "flops": 0}
+
+
+# ---- the same from the definitions, in 64 bits --------------------------------------------
+
+
+def exact(case, seed):
+    s = INPUTS[case["op"]](case, seed)
+    return {"attention": _exact_attention, "write": _exact_write, "import": _exact_import,
+            "logprobs": _exact_logprobs}[case["op"]](case, s)
+
+
+def _exact_attention(case, s):
+    nq, nkv, dh, _ = HEADS[case["heads"]]
+    page, G = case["page"], nq // nkv
+    out = torch.zeros(case["n"], nq, dh, dtype=torch.float64, device=DEV)
+    table, lengths = s["table"].cpu().numpy(), s["lengths"].cpu().numpy()
+    kc, vc, ks, vs = _views(case, s["pages"])
+    kb, vb = kc[:, 0].view(torch.uint8), vc[:, 0].view(torch.uint8)
+    for i in range(case["n"]):
+        at = np.arange(int(lengths[i]))
+        at = at[table[i, at // page] >= 0]
+        if not at.size:
+            continue
+        pg = torch.from_numpy(table[i, at // page].astype(np.int64)).to(DEV)
+        cell = torch.from_numpy(at % page).to(DEV)
+        for h in range(nkv):
+            K = kb[pg, h, cell].view(kc.dtype).double() * ks[pg, 0, h, cell // BLOCK].double()[:, None]
+            V = vb[pg, h, :, cell].view(vc.dtype).double() * vs[pg, 0, h, cell // BLOCK].double()[:, None]
+            for j in range(h * G, (h + 1) * G):
+                z = (K * s["q"][i, j].double()).sum(1) / math.sqrt(dh)
+                p = torch.exp(z - z.max())
+                out[i, j] = (p[:, None] * V).sum(0) / p.sum()
+    return out
+
+
+def _exact_held(case, new, kept, kept_scale):
+    """What a block [cells, ..., dim] of one head comes back as: the kept cells, then the new ones."""
+    limit = 127.0 if case["code"] == "i8" else 448.0
+    need = float(new.abs().max()) / limit
+    scale = 2.0 ** -100
+    while scale < need:
+        scale *= 2.0
+    if kept.shape[0]:
+        scale = max(scale, kept_scale)
+    y = torch.cat([kept, new]) / scale
+    if case["code"] == "i8":
+        step = torch.ones_like(y)
+    else:  # 3 bits behind the leading one, which is 2^-6 at least
+        step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
+    return torch.round(y / step) * step * scale
+
+
+def _exact_write(case, s):
+    _, nkv, dh, _ = HEADS[case["heads"]]
+    first, counts = _spans(case)
+    if int(counts.sum()) * nkv > 300000:
+        return None  # (a block at a time: over 20 seconds)
+    rows, page, table = _rows(counts), case["page"], s["table"].cpu().numpy()
+    kc, vc, ks, vs = (t.cpu() for t in _views(case, s["pages"]))
+    given = {"k": s["k"].cpu().double(), "v": s["v"].cpu().double()}
+    out = {"k": [], "v": []}
+    for i in range(case["n"]):
+        lo, hi = int(first[i]), int(first[i] + counts[i])
+        for b in range(lo - lo % BLOCK, hi, BLOCK):
+            pg, c0 = int(table[i, b // page]), b % page
+            old, a, z = max(0, lo - b), max(b, lo), min(b + BLOCK, hi)
+            new = slice(int(rows[i]) + a - lo, int(rows[i]) + z - lo)
+            for name, codes, scales in (("k", kc, ks), ("v", vc, vs)):
+                heads = []
+                for h in range(nkv):
+                    block = codes[pg, 0, h, c0:c0 + old] if name == "k" else codes[pg, 0, h, :, c0:c0 + old].T
+                    sc = float(scales[pg, 0, h, c0 // BLOCK])
+                    heads.append(_exact_held(case, given[name][new, h], block.double() * sc, sc))
+                out[name].append(torch.stack(heads, 1))
+    return {name: torch.cat(v).to(DEV) for name, v in out.items()}
+
+
+def _exact_import(case, s):
+    _, nkv, dh, _ = HEADS[case["heads"]]
+    n, other = case["cells"], s["other"].cpu().double()
+    cap = s["kv"].shape[2] // (nkv * dh)
+    none = torch.empty(0, dh, dtype=torch.float64)
+    if n * nkv * case["layers"] > 300000:
+        return None  # (a block at a time: over 20 seconds)
+    for l in range(case["layers"]):
+        for h in range(nkv):
+            K, V = s["kv"][l, 0].view(nkv, cap, dh)[h].cpu().double(), s["kv"][l, 1].view(nkv, dh, cap)[h].T.cpu().double()
+            for b in range(0, n, BLOCK):
+                z = min(b + BLOCK, n)
+                other[l, 0].view(nkv, cap, dh)[h, b:z] = _exact_held(case, K[b:z], none, 0.0)
+                other[l, 1].view(nkv, dh, cap)[h, :, b:z] = _exact_held(case, V[b:z], none, 0.0).T
+    return {"other": other.to(DEV)}
+
+
+def _exact_logprobs(case, s):
+    x, tokens = s["logits"].cpu().double().numpy(), s["tokens"].cpu().numpy()
+    n, top = case["n"], case["top"]
+    out = {"logprobs": np.empty(tokens.shape), "lse": np.empty(n), "entropy": np.empty(n),
+           "top_tokens": np.empty((n, top), np.int32), "top_logprobs": np.empty((n, top))}
+    for i in range(n):
+        live = x[i][np.isfinite(x[i])]
+        p = np.exp(live - live.max())
+        lse = live.max() + math.log(p.sum())
+        order = np.lexsort((np.arange(x.shape[1]), -x[i]))[:top]
+        out["lse"][i], out["entropy"][i] = lse, -np.sum(p / p.sum() * (live - lse))
+        out["logprobs"][i], out["top_tokens"][i], out["top_logprobs"][i] = x[i][tokens[i]] - lse, order, x[i][order] - lse
+    return out
