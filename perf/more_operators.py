@@ -118,7 +118,11 @@ def _normal(shape, dtype, g, sigma=1.0):
     quick and lines up with no row."""
     n = math.prod(shape)
     block = torch.empty(min(n, (1 << 22) + 1), device=DEV).normal_(0.0, sigma, generator=g)
-    block = block.clamp(-127, 127).round().to(dtype) if dtype == torch.int8 else block.to(dtype)
+    if dtype == torch.int8:
+        block = block.clamp(-127, 127).round()
+    elif dtype == torch.float8_e4m3fn:
+        block = block.clamp(-448, 448)
+    block = block.to(dtype)
     if block.numel() == n:
         return block.view(shape)
     return block.repeat(-(-n // block.numel()))[:n].view(shape)
