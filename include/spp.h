@@ -71,6 +71,10 @@ typedef enum {
 
 typedef enum { SPP_DTYPE_F32 = 0, SPP_DTYPE_BF16 = 1 } spp_dtype;
 
+/* Cells of a pool in 8 bits an element: a code (a signed integer, or a float of 4 exponent and 3
+ * mantissa bits, largest 448) times the scale of its block.  See "caches of 8-bit codes". */
+typedef enum { SPP_CELLS_I8 = 8, SPP_CELLS_E4M3 = 9 } spp_cell_codes;
+
 /* Storage of the projection weights wq..w_down.  MXFP4 is the OCP microscaling format
  * (the 4-bit weight-only variant of the 70B-class headline model, Sec. 4): every weight
  * is a 4-bit e2m1 code (bit 3 sign, bits 2..1 exponent, bit 0 mantissa: magnitudes
@@ -437,7 +441,7 @@ typedef struct spp_pool_s* spp_pool_t;
 typedef struct {
   int32_t n_layers, n_kv_heads, head_dim;  /* of the models whose cells it holds; head_dim
                                               64 or 128                                  */
-  int32_t dtype;            /* spp_dtype of the cells                                     */
+  int32_t dtype;            /* spp_dtype of the cells, or their spp_cell_codes            */
   int32_t page_cells;       /* cells per page: 16, 32, 64, 128 or 256                     */
   int32_t n_pages;          /* pages in the caller's buffer, >= 1                         */
   int32_t max_seqs;         /* most sequences alive at once, 1..65536                     */
@@ -519,7 +523,9 @@ spp_status spp_seq_truncate(spp_pool_t pool, int32_t seq, int32_t n);
  * on `stream`, ordered after the device work of the session's model as well, and before its
  * next (as spp_seq_export); the session's buffer stays until the copy has run.
  * SPP_E_INVALID_ARG unless the session's model has the pool's layers, kv heads, head_dim and
- * dtype and lives on its device; SPP_E_CAPACITY when the pages run out. */
+ * dtype (any, where the pool's cells are 8-bit codes: they are quantised on the way in, and come
+ * back as values of the session's dtype) and lives on its device; SPP_E_CAPACITY when the pages run
+ * out. */
 spp_status spp_seq_import(spp_pool_t pool, int32_t seq, spp_session_t session, void* stream);
 /* The session's committed state becomes a copy of the sequence: its cells [0, n_cells) of
  * every layer are overwritten, n_s <- n_cells, its entry is dropped and its ready
@@ -538,8 +544,8 @@ spp_status spp_pool_compact(spp_pool_t pool, void* stream, int32_t* n_moved);
  * layer, into a page of the sequence's own (as spp_seq_reserve) -- and the fp32 logits after
  * it go to dists[i] (host array of device pointers, fp32[vocab] each); n_cells grows by one.
  * Every weight is read once for up to the model's max_sessions (and max_tokens) sequences;
- * more take further passes.  The model has the pool's layers, kv heads, head_dim and dtype
- * and lives on its device.  Asynchronous on `stream`.  SPP_E_INVALID_ARG for a null pointer,
+ * more take further passes.  The model has the pool's layers, kv heads, head_dim and dtype (any,
+ * where the pool's cells are 8-bit codes) and lives on its device.  Asynchronous on `stream`.  SPP_E_INVALID_ARG for a null pointer,
  * n < 1, a sequence that does not exist or is listed twice, a token outside [0, vocab);
  * SPP_E_CAPACITY when the pages run out or a sequence is SPP_MAX_CAPACITY cells long (then
  * nothing ran).  After SPP_E_HIP the sequences of finished passes have grown, the others not. */
@@ -563,7 +569,9 @@ spp_status spp_seq_summaries(spp_pool_t pool, int32_t n, const int32_t* seqs, sp
  * infinity of V makes its dimension infinite or NaN, and one of K makes infinite or NaN scores.  A
  * score of +inf or NaN makes its row NaN, one of -inf has no weight (a row of these alone gets zeros).
  * The products of bf16 cells run on bf16 matrix cores with q (unless it is bf16) and p in
- * two bf16 parts and fp32 sums: about 16 significant bits of both. */
+ * two bf16 parts and fp32 sums: about 16 significant bits of both.  8-bit codes are taken as they
+ * are, exactly, and likewise; their scales multiply scores and p_j in fp32.  A live cell whose scale
+ * is NaN makes the rows that read it NaN. */
 typedef struct {
   spp_pool_t pool;
   int32_t layer;
@@ -591,6 +599,72 @@ size_t spp_paged_attention_work_bytes(const spp_paged_attn* a);
  * SPP_E_INVALID_ARG for a null pointer or a value outside what the fields say. */
 spp_status spp_paged_attention(const spp_paged_attn* a, void* work, size_t work_bytes,
                                void* stream);
+
+/* ---- caches of 8-bit codes ----------------------------------------------------------- */
+
+/* A pool whose dtype is an spp_cell_codes holds every element in 8 bits: half a bf16 cell, so that
+ * attention reads half.  16 cells of one head (cells 16 b .. 16 b + 15 of a sequence) are a
+ * block, keys and values apart, and share an fp32 scale, a power of two:
+ *   s = the smallest with max |x| / s <= Q over the block's cells, at least 2^-100,
+ *   code = x / s rounded to the nearest, ties to even,   Q = 127 (I8) or 448 (E4M3).
+ * Cells appended to a block that holds cells already (a decode step, spp_paged_write) keep its s
+ * at least what it was; where it grows, the codes there are rounded to the new one.  So what a
+ * block holds depends on what was written and in which order, and the error of an element is at
+ * most s / 2 (I8) or 2^-4 of it and 2^-10 s (E4M3) as it is written, and after any growth less than s (I8), or
+ * the same relative to it and 2^-9 s (E4M3).  A block that is given an infinity or a NaN has
+ * the scale NaN and reads as NaN from then on, until it is written from its first cell;
+ * magnitudes of 2^127 and more may come back infinite.  Cells of a block past the last
+ * written one are undefined.  I8 keeps about twice as many bits of cells that are alike in size; E4M3
+ * keeps 4 bits of each element of a block whose elements differ by up to 2^14.
+ *
+ * All calls of a pool serve such pools too: import and export convert, decode steps append,
+ * forks, reserves and compaction copy pages with their scales. */
+
+/* Where the scale of (layer, head, block of a page) lives: byte offset from the buffer's start
+ * of K's = page*page_stride + layer*layer_stride + k_offset + (head*stride[0] + block*stride[1])
+ * * 4, of V's likewise (the other strides in spp_page_layout). */
+typedef struct {
+  int64_t k_offset, v_offset;   /* bytes           */
+  int64_t stride[2];            /* fp32 elements   */
+  int32_t block_cells;          /* 16              */
+} spp_scale_layout;
+/* SPP_E_INVALID_ARG for a bad configuration, a null pointer, or cells that are no codes. */
+spp_status spp_pool_scale_layout(const spp_pool_config* cfg, spp_scale_layout* out);
+
+/* Cells of one layer of many sequences as rows of the caller's: row rows[i] + j of k and v is cell
+ * first[i] + j of sequence i, for 0 <= j < rows[i + 1] - rows[i].  Tables as in
+ * spp_paged_attention.  A sequence with first[i] < 0 or rows[i] < 0, rows from n_rows on, rows of a
+ * sequence past max_cells and cells past its table are left out. */
+typedef struct {
+  spp_pool_t pool;           /* of 8-bit codes                                            */
+  int32_t layer;
+  int32_t n_seqs;            /* 0..65535 (0: nothing is done)                             */
+  const int32_t* table;      /* device, [n_seqs] rows of max_pages page numbers           */
+  int64_t table_stride;      /* entries between rows, >= max_pages                        */
+  int32_t max_pages;         /* >= 1; max_pages*page_cells <= 2^30                        */
+  const int32_t* first;      /* device, [n_seqs]                                          */
+  const int32_t* rows;       /* device, [n_seqs + 1]                                      */
+  int32_t n_rows;            /* rows of k and v, >= 0                                     */
+  int32_t max_cells;         /* most cells of a sequence, 1..2^24                         */
+  int32_t io_dtype;          /* spp_dtype of k and v                                      */
+  void* k;                   /* device, [n_rows] rows of [n_kv_heads][head_dim]           */
+  int64_t k_stride;          /* elements between rows, a multiple of 8; k 16-byte aligned */
+  void* v;                   /* as k                                                      */
+  int64_t v_stride;
+} spp_paged_cells;
+
+/* Quantises rows into cells (k and v are only read).  In the block of a sequence's first new cell, the cells
+ * before that one keep their values as described above; the cells past the last new one are undefined
+ * afterwards.  Cells whose page is not listed are left out.  No two sequences of a call write
+ * into the same block (a spp_seq_reserve gives them pages of their own).  Only launches a kernel on
+ * `stream` and may be captured into a graph, whose replays read tables, first, rows, k and v as they
+ * are then; it is the caller's to order against the pool's other work, as spp_paged_attention.
+ * SPP_E_INVALID_ARG for a null pointer or a value outside what the fields say. */
+spp_status spp_paged_write(const spp_paged_cells* a, void* stream);
+/* The cells' values, code times scale, into the rows (exact in bf16, but for what lies beyond its
+ * range).  Rows of cells whose page is not listed are zeros; rows that are no cell's stay as they
+ * are.  Otherwise as spp_paged_write. */
+spp_status spp_paged_read(const spp_paged_cells* a, void* stream);
 
 /* ---- adjusted logits ---------------------------------------------------------------- */
 

@@ -29,6 +29,7 @@ OUTCOME_NAMES = ["SERVED", "FALL_INVALID", "FALL_INELIGIBLE", "FALL_GAP", "FALL_
 # spp_mutation
 SPP_MUT_SHIFT, SPP_MUT_ROLLBACK, SPP_MUT_UPDATE = 0, 1, 2
 SPP_DTYPE_F32, SPP_DTYPE_BF16 = 0, 1
+SPP_CELLS_I8, SPP_CELLS_E4M3 = 8, 9  # spp_cell_codes
 SPP_W_Q, SPP_W_K, SPP_W_V, SPP_W_O, SPP_W_GATE, SPP_W_UP, SPP_W_DOWN = range(7)
 SPP_WFMT_DTYPE, SPP_WFMT_MXFP4 = 0, 1
 # largest session capacity in cells per layer (spp.h)
@@ -105,6 +106,11 @@ class spp_page_layout(ctypes.Structure):
                 ("v_stride", ctypes.c_int64 * 3), ("elem_bytes", ctypes.c_int32)]
 
 
+class spp_scale_layout(ctypes.Structure):
+    _fields_ = [("k_offset", ctypes.c_int64), ("v_offset", ctypes.c_int64),
+                ("stride", ctypes.c_int64 * 2), ("block_cells", ctypes.c_int32)]
+
+
 class spp_pool_info(ctypes.Structure):
     _fields_ = [("n_pages", ctypes.c_int32), ("used_pages", ctypes.c_int32),
                 ("shared_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
@@ -123,6 +129,15 @@ class spp_paged_attn(ctypes.Structure):
                 ("table_stride", ctypes.c_int64), ("max_pages", ctypes.c_int32),
                 ("lengths", ctypes.c_void_p), ("scale", ctypes.c_float), ("out", ctypes.c_void_p),
                 ("out_stride", ctypes.c_int64)]
+
+
+class spp_paged_cells(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("layer", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("max_pages", ctypes.c_int32), ("first", ctypes.c_void_p), ("rows", ctypes.c_void_p),
+                ("n_rows", ctypes.c_int32), ("max_cells", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("k", ctypes.c_void_p), ("k_stride", ctypes.c_int64),
+                ("v", ctypes.c_void_p), ("v_stride", ctypes.c_int64)]
 
 
 class spp_adjust(ctypes.Structure):
@@ -148,6 +163,7 @@ EXPORTS = ["spp_model_create", "spp_model_destroy", "spp_session_kv_bytes", "spp
            "spp_seq_reserve", "spp_seq_commit", "spp_seq_truncate", "spp_seq_import",
            "spp_seq_export", "spp_seq_summaries", "spp_decode_batch",
            "spp_paged_attention_work_bytes", "spp_paged_attention",
+           "spp_pool_scale_layout", "spp_paged_write", "spp_paged_read",
            "spp_adjust_logits_work_bytes", "spp_adjust_logits"]
 
 _lib = None
@@ -216,6 +232,9 @@ def lib() -> ctypes.CDLL:
         "spp_decode_batch": (st, [P, P, i32, P, P, P, P]),
         "spp_paged_attention_work_bytes": (sz, [ctypes.POINTER(spp_paged_attn)]),
         "spp_paged_attention": (st, [ctypes.POINTER(spp_paged_attn), P, sz, P]),
+        "spp_pool_scale_layout": (st, [ctypes.POINTER(spp_pool_config), ctypes.POINTER(spp_scale_layout)]),
+        "spp_paged_write": (st, [ctypes.POINTER(spp_paged_cells), P]),
+        "spp_paged_read": (st, [ctypes.POINTER(spp_paged_cells), P]),
         "spp_adjust_logits_work_bytes": (sz, [i32, i32]),
         "spp_adjust_logits": (st, [i32, i32, ctypes.POINTER(spp_adjust), P, P, sz, P]),
     }
@@ -600,14 +619,21 @@ def gate_batch(readies: Sequence[Ready], taus: Sequence[float], bitmaps, stream=
 _ShortTable = ctypes.c_int32 * 65  # 64 pages and their number
 
 
+CELL_CODES = {"i8": SPP_CELLS_I8, "e4m3": SPP_CELLS_E4M3}
+
+
 class PagePool:
     """Pages of a paged cache (spp_pool_*): sequences are numbers, the pages a device buffer
-    (`pages`: a contiguous tensor of at least the pool's bytes; else allocated here)."""
+    (`pages`: a contiguous tensor of at least the pool's bytes; else allocated here).  cells: "i8" or
+    "e4m3" for cells in 8 bits with a scale for each 16 of a head (spp_cell_codes), whatever bf16 says."""
 
     def __init__(self, n_layers: int, n_kv_heads: int, head_dim: int, bf16: bool, page_cells: int,
-                 n_pages: int, max_seqs: int = 64, pages=None, device="cuda"):
-        self.cfg = spp_pool_config(n_layers, n_kv_heads, head_dim,
-                                   SPP_DTYPE_BF16 if bf16 else SPP_DTYPE_F32, page_cells, n_pages,
+                 n_pages: int, max_seqs: int = 64, pages=None, device="cuda",
+                 cells: Optional[str] = None):
+        if cells is not None and cells not in CELL_CODES:
+            raise ValueError(f"cells: one of {sorted(CELL_CODES)} or None")
+        dtype = CELL_CODES[cells] if cells else SPP_DTYPE_BF16 if bf16 else SPP_DTYPE_F32
+        self.cfg = spp_pool_config(n_layers, n_kv_heads, head_dim, dtype, page_cells, n_pages,
                                    max_seqs)
         self.handle = None
         self._free, self._table = _unconverted("spp_seq_free"), _unconverted("spp_seq_table")
@@ -641,6 +667,13 @@ class PagePool:
         out = spp_page_layout()
         check(lib().spp_pool_page_layout(ctypes.byref(self.cfg), ctypes.byref(out)),
               "spp_pool_page_layout")
+        return out
+
+    def scale_layout(self) -> spp_scale_layout:
+        """Where the scales of a pool of 8-bit codes are (spp_pool_scale_layout)."""
+        out = spp_scale_layout()
+        check(lib().spp_pool_scale_layout(ctypes.byref(self.cfg), ctypes.byref(out)),
+              "spp_pool_scale_layout")
         return out
 
     def info(self) -> spp_pool_info:
@@ -791,6 +824,65 @@ class PagedAttention:
         if rc < 0:
             raise SppError(rc, "spp_paged_attention")
         return out
+
+
+class PagedCells:
+    """spp_paged_write and spp_paged_read over fixed tables of a pool of 8-bit codes: rows rows[i] ..
+    rows[i + 1] - 1 of k and v, [n_rows][n_kv_heads][head_dim], are the cells first[i] .. of sequence
+    i, at most max_cells of each.  table [n][max_pages], first [n] and rows [n + 1] are int32 device
+    tensors whose values may change between calls; the object lives until its calls have finished."""
+
+    def __init__(self, pool: PagePool, layer: int, table, first, rows, max_cells: int,
+                 io_bf16: bool = True):
+        import torch
+        self._dev = dev = pool.device
+        if not pool.handle:
+            raise ValueError("the pool is closed")
+        if any(t.get_device() != dev for t in (table, first, rows)):
+            raise ValueError("table, first and rows are on the pool's device")
+        if any(t.dtype != torch.int32 for t in (table, first, rows)) or table.dim() != 2 or \
+                first.shape != table.shape[:1] or rows.shape != (table.shape[0] + 1,) or \
+                not first.is_contiguous() or not rows.is_contiguous() or \
+                (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table [n][max_pages], first [n] and rows [n + 1]: int32, contiguous rows")
+        n, width = table.shape
+        c = pool.cfg
+        self._keep = (pool, table, first, rows)
+        self._dtype = torch.bfloat16 if io_bf16 else torch.float32
+        self._shape = (c.n_kv_heads, c.head_dim)
+        self._a = spp_paged_cells(pool.handle.value, layer, n, table.data_ptr(),
+                                  table.stride(0) if n > 1 else width, width, first.data_ptr(),
+                                  rows.data_ptr(), 0, max_cells,
+                                  SPP_DTYPE_BF16 if io_bf16 else SPP_DTYPE_F32)
+        self._ref = ctypes.byref(self._a)
+        self._write, self._read = _unconverted("spp_paged_write"), _unconverted("spp_paged_read")
+        a, row = self._a, c.n_kv_heads * c.head_dim  # (a bad layer or max_cells shows here: no rows, no device)
+        a.k = a.v = pool.pages.data_ptr()
+        a.k_stride = a.v_stride = row
+        check(lib().spp_paged_read(self._ref, None), "spp_paged_read")
+
+    def _call(self, fn, name, k, v, stream):
+        if k.dtype != self._dtype or v.dtype != self._dtype or k.shape != v.shape or \
+                k.dim() != 3 or k.shape[1:] != self._shape:
+            raise ValueError(f"k and v: {self._dtype} of shape (rows, {self._shape[0]}, {self._shape[1]})")
+        if k.get_device() != self._dev or v.get_device() != self._dev or not self._keep[0].handle:
+            raise ValueError("k and v are on the pool's device, the pool is open")
+        a, row = self._a, self._shape[0] * self._shape[1]
+        a.n_rows = k.shape[0]
+        a.k, a.k_stride = k.data_ptr(), row if k.is_contiguous() else _row_stride(k, "k")
+        a.v, a.v_stride = v.data_ptr(), row if v.is_contiguous() else _row_stride(v, "v")
+        rc = fn(self._ref, ctypes.c_void_p(_stream_of(stream, self._dev)))
+        if rc < 0:
+            raise SppError(rc, name)
+
+    def write(self, k, v, stream=None) -> None:
+        """Quantises the rows into their cells (spp_paged_write)."""
+        self._call(self._write, "spp_paged_write", k, v, stream)
+
+    def read(self, k, v, stream=None):
+        """The cells' values into the rows (spp_paged_read); returns k and v."""
+        self._call(self._read, "spp_paged_read", k, v, stream)
+        return k, v
 
 
 @dataclasses.dataclass

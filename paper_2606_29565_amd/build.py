@@ -14,7 +14,8 @@ LIB = os.path.join(HERE, "libspp.so")
 OBJDIR = os.path.join(HERE, "_build")
 
 SOURCES = ["gemm.hip", "gemm_tile.hip", "gemm_fp4.hip", "attention.hip", "elementwise.hip",
-           "vocab.hip", "paged.hip", "logits.hip", "runtime.cpp", "pool.cpp"]
+           "vocab.hip", "paged.hip", "paged_codes.hip", "logits.hip", "runtime.cpp", "pool.cpp",
+           "cells.cpp"]
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I", INCLUDE, "-I", CSRC,
                # packed fp32 instructions stay off on these GPUs (wrong results seen at times)
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -30,63 +30,13 @@
 #include <algorithm>
 #include <cmath>
 
-#include "common.hpp"
-#include "paged.hpp"
+#include "paged_device.hpp"
 
 namespace spp {
 namespace {
 
-constexpr int kWaves = 4;      // waves of an attention workgroup, each with its own key range
-constexpr int kMaxSplits = 256;
-
 template <typename T>
 constexpr int step_keys() { return 8 * Elem<T>::kPerFrag; }
-
-// Cells of a key range: a sequence's cells dealt out evenly over at most `splits` ranges of
-// whole steps of all waves.  (On the device, from the length as it is at the launch.)
-__device__ __forceinline__ int range_cells(int len, int splits, int unit) {
-  const int units = (len + unit - 1) / unit;
-  return (units + splits - 1) / splits * unit;
-}
-
-__device__ __forceinline__ int live_cells(const PagedAttn& a, int shift, int seq) {
-  const int len = a.lengths[seq], most = a.max_pages << shift;
-  return len < 0 ? 0 : (len < most ? len : most);
-}
-
-__device__ __forceinline__ void store_out(const PagedAttn& a, int64_t i, float v) {
-  if (a.out_mode == 0) {
-    static_cast<float*>(a.out)[i] = v;
-  } else if (a.out_mode == 1) {
-    static_cast<bf16_t*>(a.out)[i].bits = f32_to_bf16(v);
-  } else {
-    store_act(static_cast<bf16_t*>(a.out), static_cast<bf16_t*>(a.out_lo), i, v);
-  }
-}
-
-// Eight or four query elements in two parts of the cells' type (hi alone in fp32).
-__device__ __forceinline__ void query_frag(const void* q, bool q_bf16, int64_t at, uint4& hi, uint4& lo, bf16_t) {
-  if (q_bf16) {
-    hi = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(q) + at);
-    lo = make_uint4(0, 0, 0, 0);
-    return;
-  }
-  const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(q) + at);
-  const float4 b = *reinterpret_cast<const float4*>(static_cast<const float*>(q) + at + 4);
-  split_pair(a.x, a.y, hi.x, lo.x);
-  split_pair(a.z, a.w, hi.y, lo.y);
-  split_pair(b.x, b.y, hi.z, lo.z);
-  split_pair(b.z, b.w, hi.w, lo.w);
-}
-__device__ __forceinline__ void query_frag(const void* q, bool q_bf16, int64_t at, uint4& hi, uint4& lo, float) {
-  if (q_bf16) {
-    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(q) + at);
-    hi = make_uint4(w.x << 16, w.x & 0xFFFF0000u, w.y << 16, w.y & 0xFFFF0000u);
-  } else {
-    hi = *reinterpret_cast<const uint4*>(static_cast<const float*>(q) + at);
-  }
-  lo = make_uint4(0, 0, 0, 0);
-}
 
 // The first n of a unit's elements (E of T), the others zero.
 __device__ __forceinline__ uint4 keep_first(const uint4& v, int n, bf16_t) {
@@ -529,15 +479,23 @@ hipError_t launch_attn(const PageView& v, int64_t layer_off, const PagedAttn& a,
   else
     SPP_LAUNCH((paged_attn_kernel<T, DH, false>), grid, dim3(64 * kWaves), 0, st, v, layer_off, a, scale2, tiles,
                o_part, ml_part);
-  if (splits > 1)
-    SPP_LAUNCH((paged_join_kernel<DH>), dim3(a.n_q, a.n), dim3(kMaxSplits), 0, st, a, v.shift, splits,
-               step_keys<T>() * kWaves, o_part, ml_part);
+  if (splits > 1) return k::paged_join(v, a, splits, step_keys<T>() * kWaves, o_part, ml_part, st);
   return hipGetLastError();
 }
 
 }  // namespace
 
 namespace k {
+
+hipError_t paged_join(const PageView& v, const PagedAttn& a, int splits, int unit, const float* o_part,
+                      const float2* ml_part, hipStream_t st) {
+  const dim3 grid(a.n_q, a.n), block(kMaxSplits);
+  if (v.dh == 128)
+    SPP_LAUNCH((paged_join_kernel<128>), grid, block, 0, st, a, v.shift, splits, unit, o_part, ml_part);
+  else
+    SPP_LAUNCH((paged_join_kernel<64>), grid, block, 0, st, a, v.shift, splits, unit, o_part, ml_part);
+  return hipGetLastError();
+}
 
 // Ranges of a sequence and kv head.  A range is at least one step of its workgroup's waves (256
 // cells in bf16, 128 in fp32).
@@ -553,7 +511,7 @@ namespace k {
 //    most, however many, 263; 128 of up to 2000 cells: one range 125 us, two 134, four 142).
 int paged_splits(const PageView& v, int n, int n_q, int max_pages) {
   const int tiles = (n_q / v.n_kv + 15) / 16;
-  const int unit = (v.elem == 2 ? step_keys<bf16_t>() : step_keys<float>()) * kWaves;
+  const int unit = (v.code ? kCodeStep : v.elem == 2 ? step_keys<bf16_t>() : step_keys<float>()) * kWaves;
   const int64_t most = (((int64_t)max_pages << v.shift) + unit - 1) / unit, wgs = (int64_t)n * v.n_kv * tiles;
   if (most <= (wgs >= 128 ? 4 : 2)) return 1;
   const int64_t want = std::max<int64_t>(std::min<int64_t>(4, most / 8), kSplitWorkgroups / wgs);
@@ -568,7 +526,8 @@ size_t paged_work_bytes(const PageView& v, int n, int n_q, int max_pages) {
 hipError_t paged_attention(const PageView& v, int layer, const PagedAttn& a, void* work, hipStream_t st) {
   if (a.n <= 0) return hipSuccess;
   const int splits = paged_splits(v, a.n, a.n_q, a.max_pages);
-  const int64_t off = 2 * v.half() * layer;
+  if (v.code) return code_attention(v, layer, a, splits, work, st);
+  const int64_t off = v.layer() * layer;
   if (v.elem == 2)
     return v.dh == 128 ? launch_attn<bf16_t, 128>(v, off, a, splits, work, st)
                        : launch_attn<bf16_t, 64>(v, off, a, splits, work, st);
@@ -597,6 +556,7 @@ hipError_t page_session(const PageView& v, const PageList& l, int n, void* kv, i
                         bool to_pages, hipStream_t st) {
   if (n <= 0) return hipSuccess;
   if (n > kPageBatch) return hipErrorInvalidValue;
+  if (v.code) return code_session(v, l, n, kv, cap, c0, cells, to_pages, st);
   const dim3 grid(v.n_layers * 2 * v.n_kv * n), block(256);
 #define SPP_SESSION(T, D) \
   SPP_LAUNCH((page_session_kernel<T, D>), grid, block, 0, st, v, l, n, static_cast<T*>(kv), cap, c0, cells)
@@ -612,8 +572,10 @@ hipError_t page_session(const PageView& v, const PageList& l, int n, void* kv, i
 hipError_t paged_epilogue(const Shape& s, const StepView& sv, int n_rows, int layer, const PageView& v,
                           const int32_t* table, int64_t table_stride, const float* partials, int splits,
                           const float* ss, const float2* rope, float* q_out, hipStream_t st) {
+  if (v.code)
+    return code_epilogue(s, sv, n_rows, layer, v, table, table_stride, partials, splits, ss, rope, q_out, st);
   const dim3 grid(n_rows, s.n_q + 2 * s.n_kv);
-  const int64_t off = 2 * v.half() * layer;
+  const int64_t off = v.layer() * layer;
   if (s.bf16)
     SPP_LAUNCH((paged_epilogue_kernel<bf16_t>), grid, dim3(64), 0, st, s, sv, n_rows, off, v, table, table_stride,
                partials, splits, ss, res_blocks(s), rope, q_out);

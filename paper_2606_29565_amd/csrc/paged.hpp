@@ -6,15 +6,25 @@
 
 namespace spp {
 
+constexpr int kBlockCells = 16;  // cells of a head that share a scale in a cache of 8-bit codes
+
 // A pool's pages as the kernels see them: [page][layer][K, V][n_kv * page_cells * dh], K as
-// [head][cell][dim], V as [head][dim][cell].
+// [head][cell][dim], V as [head][dim][cell].  Where the elements are 8-bit codes, each layer ends with
+// their fp32 scales, [K, V][head][block of 16 cells], filled up to 128 bytes.
 struct PageView {
   char* base;
   int32_t n_pages, n_layers, n_kv, dh, shift;  // 1 << shift cells per page
   int32_t elem;                                // bytes of an element
+  int32_t code = 0;                            // spp_cell_codes, or 0: the elements are values
+  int32_t given = 0;                           // code: bytes of an element of the session that is copied
   __host__ __device__ int64_t half() const { return ((int64_t)n_kv * dh << shift) * elem; }  // bytes of K (or V) of a layer
-  __host__ __device__ int64_t page() const { return 2 * half() * n_layers; }
+  __host__ __device__ int blocks() const { return (1 << shift) / kBlockCells; }
+  __host__ __device__ int64_t scales() const { return code ? (8ll * n_kv * blocks() + 127) / 128 * 128 : 0; }
+  __host__ __device__ int64_t layer() const { return 2 * half() + scales(); }
+  __host__ __device__ int64_t page() const { return layer() * n_layers; }
 };
+// The pages of a pool and its device.
+const PageView& pool_view(spp_pool_t pool, int* device);
 
 // One attention call: tables and lengths on the device.
 struct PagedAttn {
@@ -32,6 +42,24 @@ struct PagedAttn {
   int64_t out_stride;
   int32_t out_mode;          // 0 fp32, 1 bf16, 2 bf16 pair
 };
+
+// Rows [rows[i], rows[i+1]) of k and v are cells first[i] .. of sequence i.
+struct CellRows {
+  int32_t n;
+  const int32_t* table;
+  int64_t table_stride;
+  int32_t max_pages;
+  const int32_t *first, *rows;
+  int32_t n_rows, max_cells;
+  int32_t bf16;
+  void* k;                   // [n_rows][n_kv][dh], rows k_stride elements apart
+  int64_t k_stride;
+  void* v;
+  int64_t v_stride;
+};
+
+// Keys of a step of a wave of the attention over 8-bit codes.
+constexpr int kCodeStep = 64;
 
 // Pages copied in one launch travel as a kernel argument.
 constexpr int kPageBatch = 256;
@@ -54,6 +82,10 @@ size_t paged_work_bytes(const PageView& v, int n, int n_q, int max_pages);
 hipError_t paged_attention(const PageView& v, int layer, const PagedAttn& a, void* work,
                            hipStream_t st);
 
+// The ranges of a call joined into its outputs (unit: the cells that ranges are multiples of).
+hipError_t paged_join(const PageView& v, const PagedAttn& a, int splits, int unit, const float* o_part,
+                      const float2* ml_part, hipStream_t st);
+
 // dst page b[i] = src page a[i], i < n <= kPageBatch; no page is both.
 hipError_t page_copy(const PageView& v, const PageList& l, int n, hipStream_t st);
 // Cells [c0, c0 + cells) of every layer between a session's buffer (cap cells a layer) and
@@ -68,6 +100,19 @@ hipError_t paged_epilogue(const Shape& s, const StepView& sv, int n_rows, int la
                           const PageView& v, const int32_t* table, int64_t table_stride,
                           const float* partials, int splits, const float* ss, const float2* rope,
                           float* q_out, hipStream_t st);
+
+// The same over pages of 8-bit codes (their callers are the three above).
+hipError_t code_attention(const PageView& v, int layer, const PagedAttn& a, int splits, void* work,
+                          hipStream_t st);
+hipError_t code_session(const PageView& v, const PageList& l, int n, void* kv, int64_t cap, int64_t c0,
+                        int cells, bool to_pages, hipStream_t st);
+hipError_t code_epilogue(const Shape& s, const StepView& sv, int n_rows, int layer, const PageView& v,
+                         const int32_t* table, int64_t table_stride, const float* partials, int splits,
+                         const float* ss, const float2* rope, float* q_out, hipStream_t st);
+
+// Rows of a caller into cells of 8-bit codes, and such cells into rows.
+hipError_t code_write(const PageView& v, int layer, const CellRows& c, hipStream_t st);
+hipError_t code_read(const PageView& v, int layer, const CellRows& c, hipStream_t st);
 
 // Workspace of this very call (of fewer rows it may be more, see kShortSliceTokens).
 size_t adjust_work_bytes(int n, int vocab);

@@ -1,0 +1,791 @@
+// Paged caches of 8-bit codes: cells written and read back, a session's cells copied in and out,
+// the QKV epilogue that appends, and attention of one new token per sequence.
+//
+// An element is a code times the scale of its block, 16 cells of one head (keys and values apart):
+//   s = the smallest power of two with max |x| / s <= Q, at least 2^-100;  code = x / s rounded
+// to the nearest, ties to even, Q = 127 (signed integers) or 448 (e4m3 floats).  Cells appended to a
+// block that holds cells already keep s at least what it was, and where it grows the codes there
+// are rounded to the new one.  That s is a power of two makes all of this exact but the
+// rounding to a code; a scale that grows at least doubles, so the roundings of a cell that is
+// kept sum to less than one step of the last scale, however often it grew; and a code of at most 8
+// significant bits times its scale is exact in bf16.  A block that is given an infinity or a NaN
+// has the scale NaN, and so reads.
+#include <algorithm>
+#include <cmath>
+
+#include "paged_device.hpp"
+
+namespace spp {
+namespace {
+
+// Code formats: int8 (SPP_CELLS_I8) and e4m3 (SPP_CELLS_E4M3).
+constexpr bool is_i8(int code) { return code == SPP_CELLS_I8; }
+
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+// The scale that values of at most |x| need, from the bits of |x|.
+template <int CODE>
+__device__ __forceinline__ float scale_for(uint32_t top) {
+  // x = 1.f 2^(E - 127): x / 2^(E - 133) < 128 and x / 2^(E - 135) < 512, at most Q up to a fraction
+  // of 127 / 64 - 1 (of 448 / 256 - 1), else the next power of two
+  constexpr uint32_t most = is_i8(CODE) ? 0x7E0000u : 0x600000u;
+  constexpr int below = is_i8(CODE) ? 6 : 8;
+  const int e = (int)(top >> 23) - below + ((top & 0x7FFFFFu) > most ? 1 : 0);
+  return top >= kInfBits ? __builtin_nanf("") : __uint_as_float((uint32_t)max(e, 27) << 23);
+}
+// 1 / s of a power of two from 2^-100 to 2^122 (NaN for NaN).
+__device__ __forceinline__ float inverse(float s) {
+  const uint32_t e = __float_as_uint(s) >> 23;
+  return e >= 255 ? __builtin_nanf("") : __uint_as_float((254u - e) << 23);
+}
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// Four values, already divided by the scale, as codes (the first in the low byte).
+template <int CODE>
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
+  if constexpr (is_i8(CODE)) {
+    const uint32_t lo = __builtin_amdgcn_perm((uint32_t)(int)__builtin_rintf(b), (uint32_t)(int)__builtin_rintf(a), 0x0C0C0400u);
+    const uint32_t hi = __builtin_amdgcn_perm((uint32_t)(int)__builtin_rintf(d), (uint32_t)(int)__builtin_rintf(c), 0x0C0C0400u);
+    return lo | hi << 16;
+  } else {
+    return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+  }
+}
+template <int CODE>
+__device__ __forceinline__ void decode4(uint32_t w, float (&x)[4]) {
+  if constexpr (is_i8(CODE)) {
+    x[0] = (float)(int8_t)w;
+    x[1] = (float)(int8_t)(w >> 8);
+    x[2] = (float)(int8_t)(w >> 16);
+    x[3] = (float)(int8_t)(w >> 24);
+  } else {
+    x[0] = __builtin_amdgcn_cvt_f32_fp8(w, 0);
+    x[1] = __builtin_amdgcn_cvt_f32_fp8(w, 1);
+    x[2] = __builtin_amdgcn_cvt_f32_fp8(w, 2);
+    x[3] = __builtin_amdgcn_cvt_f32_fp8(w, 3);
+  }
+}
+// Codes of a scale that grew, at the new one (ratio = old / new).
+template <int CODE>
+__device__ __forceinline__ uint32_t shrink4(uint32_t w, float ratio) {
+  float x[4];
+  decode4<CODE>(w, x);
+  return encode4<CODE>(x[0] * ratio, x[1] * ratio, x[2] * ratio, x[3] * ratio);
+}
+// Four codes as values, two bf16 pairs or four floats.
+template <int CODE>
+__device__ __forceinline__ void values4(uint32_t w, float scale, bf16_t* out) {
+  float x[4];
+  decode4<CODE>(w, x);
+  uint2 o;  // (exact: the upper halves)
+  o.x = __builtin_amdgcn_perm(__float_as_uint(x[1] * scale), __float_as_uint(x[0] * scale), 0x07060302u);
+  o.y = __builtin_amdgcn_perm(__float_as_uint(x[3] * scale), __float_as_uint(x[2] * scale), 0x07060302u);
+  *reinterpret_cast<uint2*>(out) = o;
+}
+template <int CODE>
+__device__ __forceinline__ void values4(uint32_t w, float scale, float* out) {
+  float x[4];
+  decode4<CODE>(w, x);
+  *reinterpret_cast<float4*>(out) = make_float4(x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale);
+}
+
+__device__ __forceinline__ uint32_t wave_top(uint32_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  return v;
+}
+
+// Where a head's block is: its codes (K: the block's first cell, V: its first cell of dim 0) and scale.
+struct BlockAt {
+  uint8_t* codes;
+  float* scale;
+};
+__device__ __forceinline__ BlockAt block_at(const PageView& v, int64_t layer_off, int page, int which, int head,
+                                            int cell) {
+  char* layer = v.base + page * v.page() + layer_off;
+  char* codes = layer + which * v.half() + ((int64_t)head * v.dh << v.shift) + (which ? cell : cell * v.dh);
+  float* scales = reinterpret_cast<float*>(layer + 2 * v.half()) + (which * v.n_kv + head) * v.blocks();
+  return BlockAt{reinterpret_cast<uint8_t*>(codes), scales + cell / kBlockCells};
+}
+
+// The scale of a block that keeps its first `kept` cells and is given values of at most |top|.
+template <int CODE>
+__device__ __forceinline__ float grown(float old, int kept, uint32_t top) {
+  const float need = scale_for<CODE>(top);
+  if (kept == 0) return need;
+  return need != need || old != old ? __builtin_nanf("") : fmaxf(need, old);
+}
+
+// The codes of a key block's first `kept` cells at a scale that grew: the wave's 4-byte words.
+template <int CODE>
+__device__ __forceinline__ void shrink_keys(uint8_t* codes, int kept, int dh, float ratio, int lane) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(codes);
+  for (int i = lane; i < kept * dh / 4; i += 64) w[i] = shrink4<CODE>(w[i], ratio);
+}
+
+// 16 codes of one dim of a value block: the first `kept` as they are (at a scale that grew if
+// `grew`), those from there on of `fresh`.
+template <int CODE>
+__device__ __forceinline__ uint4 merge_values(uint4 was, uint4 fresh, int kept, bool grew, float ratio) {
+  uint32_t o[4], w[4] = {was.x, was.y, was.z, was.w}, f[4] = {fresh.x, fresh.y, fresh.z, fresh.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (grew) w[j] = shrink4<CODE>(w[j], ratio);
+    const int n = kept - 4 * j;  // codes of this word that are kept
+    const uint32_t mask = n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+    o[j] = (w[j] & mask) | (f[j] & ~mask);
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// What a wave of a write or a read has: a block of one head's keys or values, and the rows of the
+// caller that are its cells lo .. hi - 1.
+struct BlockRows {
+  bool any;
+  int page, cell, lo, hi;  // the block's first cell in its page; lo: cells before it are kept
+  int64_t row;             // of cell 0 of the block (before the sequence's first row for cells < lo)
+};
+__device__ __forceinline__ BlockRows block_rows(const PageView& v, const CellRows& c, int b, int seq) {
+  BlockRows r{};
+  const int first = c.first[seq], r0 = c.rows[seq], r1 = min(max(c.rows[seq + 1], 0), c.n_rows);
+  if (first < 0 || r0 < 0) return r;
+  const int count = min(min(r1 - r0, c.max_cells), (c.max_pages << v.shift) - first);
+  if (count <= 0) return r;  // (so first is below 2^30)
+  const int at = (first & -kBlockCells) + kBlockCells * b;
+  if (at >= first + count) return r;
+  r.any = true;
+  r.page = c.table[seq * c.table_stride + (at >> v.shift)];
+  r.cell = at & ((1 << v.shift) - 1);
+  r.lo = max(first - at, 0);
+  r.hi = min(first + count - at, kBlockCells);
+  r.row = (int64_t)r0 + at - first;
+  return r;
+}
+
+// Grid (blocks of a sequence, K and V of each head, sequences), one wave each.
+template <typename T, int CODE, int DH>
+__global__ __launch_bounds__(64) void write_kernel(PageView v, int64_t layer_off, CellRows c) {
+  const int lane = threadIdx.x, head = blockIdx.y >> 1, which = blockIdx.y & 1;
+  const BlockRows b = block_rows(v, c, blockIdx.x, blockIdx.z);
+  if (!b.any || (unsigned)b.page >= (unsigned)v.n_pages) return;
+  const BlockAt to = block_at(v, layer_off, b.page, which, head, b.cell);
+  const T* src = static_cast<const T*>(which ? c.v : c.k) + head * DH;
+  const int64_t stride = which ? c.v_stride : c.k_stride;
+  const float old = b.lo ? *to.scale : 0.f;
+  uint32_t top = 0;
+  if (which == 0) {  // 16 bytes of a row a lane
+    constexpr int E = Elem<T>::kPerFrag, UPR = DH / E, N = kBlockCells * UPR / 64;
+    uint4 x[N];
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+      const int u = p * 64 + lane, cell = min(max(u / UPR, b.lo), b.hi - 1);
+      x[p] = *reinterpret_cast<const uint4*>(src + (b.row + cell) * stride + u % UPR * E);
+    }
+    // (rows outside [lo, hi) repeat one inside)
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+      float f[8];
+      if constexpr (E == 8) frag_to_f32(x[p], f); else frag_to_f32(x[p], reinterpret_cast<float(&)[4]>(f));
+#pragma unroll
+      for (int e = 0; e < E; ++e) top = max(top, magnitude(f[e]));
+    }
+    top = wave_top(top);
+    const float scale = grown<CODE>(old, b.lo, top), inv = inverse(scale);
+    if (b.lo && scale > old) shrink_keys<CODE>(to.codes, b.lo, DH, old * inv, lane);
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+      const int u = p * 64 + lane, cell = u / UPR;
+      float f[8];
+      if constexpr (E == 8) frag_to_f32(x[p], f); else frag_to_f32(x[p], reinterpret_cast<float(&)[4]>(f));
+      if (cell < b.lo || cell >= b.hi) continue;
+      uint32_t* dst = reinterpret_cast<uint32_t*>(to.codes + cell * DH + u % UPR * E);
+      const uint32_t w0 = encode4<CODE>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+      if constexpr (E == 8)
+        *reinterpret_cast<uint2*>(dst) = make_uint2(w0, encode4<CODE>(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
+      else
+        *dst = w0;
+    }
+    if (lane == 0) *to.scale = scale;
+    return;
+  }
+  // one or two dims of every cell a lane
+  constexpr int D = DH / 64;
+  float x[kBlockCells][D];
+#pragma unroll
+  for (int i = 0; i < kBlockCells; ++i) {
+    const T* p = src + (b.row + min(max(i, b.lo), b.hi - 1)) * stride + lane * D;
+#pragma unroll
+    for (int d = 0; d < D; ++d) x[i][d] = load_elem(p, d);
+  }
+#pragma unroll
+  for (int i = 0; i < kBlockCells; ++i)
+#pragma unroll
+    for (int d = 0; d < D; ++d) top = max(top, magnitude(x[i][d]));
+  top = wave_top(top);
+  const float scale = grown<CODE>(old, b.lo, top), inv = inverse(scale);
+#pragma unroll
+  for (int d = 0; d < D; ++d) {
+    uint4* dst = reinterpret_cast<uint4*>(to.codes + ((lane * D + d) << v.shift));
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      w[j] = encode4<CODE>(x[4 * j][d] * inv, x[4 * j + 1][d] * inv, x[4 * j + 2][d] * inv, x[4 * j + 3][d] * inv);
+    uint4 o = make_uint4(w[0], w[1], w[2], w[3]);
+    if (b.lo) o = merge_values<CODE>(*dst, o, b.lo, scale > old, old * inv);
+    *dst = o;
+  }
+  if (lane == 0) *to.scale = scale;
+}
+
+// The same grid: cells as values into the caller's rows; zeros where the page is not listed.
+template <typename T, int CODE, int DH>
+__global__ __launch_bounds__(64) void read_kernel(PageView v, int64_t layer_off, CellRows c) {
+  const int lane = threadIdx.x, head = blockIdx.y >> 1, which = blockIdx.y & 1;
+  const BlockRows b = block_rows(v, c, blockIdx.x, blockIdx.z);
+  if (!b.any) return;
+  T* dst = static_cast<T*>(which ? c.v : c.k) + head * DH;
+  const int64_t stride = which ? c.v_stride : c.k_stride;
+  const bool listed = (unsigned)b.page < (unsigned)v.n_pages;
+  const BlockAt at = block_at(v, layer_off, listed ? b.page : 0, which, head, b.cell);
+  const float scale = listed ? *at.scale : 0.f;
+  if (which == 0) {
+    constexpr int UPR = DH / 16, N = kBlockCells * UPR / 64;
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+      const int u = p * 64 + lane, cell = u / UPR;
+      uint4 w = *reinterpret_cast<const uint4*>(at.codes + u * 16);
+      if (!listed) w = make_uint4(0, 0, 0, 0);
+      if (cell < b.lo || cell >= b.hi) continue;
+      T* o = dst + (b.row + cell) * stride + u % UPR * 16;
+      values4<CODE>(w.x, scale, o);
+      values4<CODE>(w.y, scale, o + 4);
+      values4<CODE>(w.z, scale, o + 8);
+      values4<CODE>(w.w, scale, o + 12);
+    }
+    return;
+  }
+  constexpr int D = DH / 64;
+  uint4 w[D];
+#pragma unroll
+  for (int d = 0; d < D; ++d) {
+    w[d] = *reinterpret_cast<const uint4*>(at.codes + ((lane * D + d) << v.shift));
+    if (!listed) w[d] = make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float x[D][4];
+#pragma unroll
+    for (int d = 0; d < D; ++d) decode4<CODE>(j == 0 ? w[d].x : j == 1 ? w[d].y : j == 2 ? w[d].z : w[d].w, x[d]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int cell = 4 * j + i;
+      if (cell < b.lo || cell >= b.hi) continue;
+      T* o = dst + (b.row + cell) * stride + lane * D;
+#pragma unroll
+      for (int d = 0; d < D; ++d) store_elem(o, d, x[d][i] * scale);
+    }
+  }
+}
+
+// Grid (blocks of the pages' cells, four to a workgroup, fastest, times layers * 2 * kv heads), a wave
+// to a block: one block of a session's cells into its page, or out of it.  Only live cells move; the cells of the
+// session past the last stay as they are.
+template <typename T, int CODE, int DH, bool TO_PAGES>
+__global__ __launch_bounds__(256) void session_kernel(PageView v, PageList l, int groups, T* kv, int64_t cap,
+                                                      int64_t c0, int cells) {
+  constexpr int E = Elem<T>::kPerFrag;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int at = (blockIdx.x % groups * 4 + wave) * kBlockCells;  // of the cells that are copied
+  if (at >= cells) return;
+  const int hd = blockIdx.x / groups, head = hd % v.n_kv, which = hd / v.n_kv % 2, layer = hd / v.n_kv / 2;
+  const int live = min(kBlockCells, cells - at);
+  const BlockAt page = block_at(v, v.layer() * layer, l.a[at >> v.shift], which, head, at & ((1 << v.shift) - 1));
+  T* sess = kv + ((int64_t)(2 * layer + which) * v.n_kv + head) * cap * DH;
+  sess += which ? c0 + at : (c0 + at) * DH;
+  uint32_t top = 0;
+  float scale = 0.f, inv = 0.f;
+  if constexpr (!TO_PAGES) scale = *page.scale;
+  if (which == 0) {
+    constexpr int N = kBlockCells * DH / E / 64;
+    if constexpr (TO_PAGES) {
+      uint4 x[N];
+#pragma unroll
+      for (int p = 0; p < N; ++p)
+        x[p] = *reinterpret_cast<const uint4*>(sess + (int64_t)min(p * 64 + lane, live * (DH / E) - 1) * E);
+      float f[N][8];
+#pragma unroll
+      for (int p = 0; p < N; ++p) {
+        if constexpr (E == 8) frag_to_f32(x[p], f[p]); else frag_to_f32(x[p], reinterpret_cast<float(&)[4]>(f[p]));
+#pragma unroll
+        for (int e = 0; e < E; ++e) top = max(top, magnitude(f[p][e]));
+      }
+      scale = scale_for<CODE>(wave_top(top));
+      inv = inverse(scale);
+#pragma unroll
+      for (int p = 0; p < N; ++p) {
+        const int u = p * 64 + lane;
+        if (u >= live * (DH / E)) continue;
+        uint32_t* dst = reinterpret_cast<uint32_t*>(page.codes + u * E);
+        dst[0] = encode4<CODE>(f[p][0] * inv, f[p][1] * inv, f[p][2] * inv, f[p][3] * inv);
+        if constexpr (E == 8) dst[1] = encode4<CODE>(f[p][4] * inv, f[p][5] * inv, f[p][6] * inv, f[p][7] * inv);
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < N; ++p) {
+        const int u = p * 64 + lane;
+        if (u >= live * (DH / E)) continue;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(page.codes + u * E);
+        values4<CODE>(src[0], scale, sess + u * E);
+        if constexpr (E == 8) values4<CODE>(src[1], scale, sess + u * E + 4);
+      }
+    }
+  } else {
+    // a row of 16 cells of one or two dims a lane (the session's rows hold whole blocks: cap is a
+    // multiple of 64)
+    constexpr int D = DH / 64, U = kBlockCells / E;
+    if constexpr (TO_PAGES) {
+      uint4 x[D][U];
+#pragma unroll
+      for (int d = 0; d < D; ++d)
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[d][u] = *reinterpret_cast<const uint4*>(sess + (lane + 64 * d) * cap + u * E);
+      float f[D][U][8];
+#pragma unroll
+      for (int d = 0; d < D; ++d)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if constexpr (E == 8) frag_to_f32(x[d][u], f[d][u]); else frag_to_f32(x[d][u], reinterpret_cast<float(&)[4]>(f[d][u]));
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            if (u * E + e >= live) f[d][u][e] = 0.f;  // (whatever lies behind the last cell)
+            top = max(top, magnitude(f[d][u][e]));
+          }
+        }
+      scale = scale_for<CODE>(wave_top(top));
+      inv = inverse(scale);
+#pragma unroll
+      for (int d = 0; d < D; ++d) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float* g = f[d][4 * j / E] + 4 * j % E;
+          w[j] = encode4<CODE>(g[0] * inv, g[1] * inv, g[2] * inv, g[3] * inv);
+        }
+        *reinterpret_cast<uint4*>(page.codes + ((lane + 64 * d) << v.shift)) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    } else {
+#pragma unroll
+      for (int d = 0; d < D; ++d) {
+        const uint4 q = *reinterpret_cast<const uint4*>(page.codes + ((lane + 64 * d) << v.shift));
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        T* o = sess + (lane + 64 * d) * cap;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (4 * j + 4 <= live) {
+            values4<CODE>(w[j], scale, o + 4 * j);
+          } else {
+            float x[4];
+            decode4<CODE>(w[j], x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (4 * j + e < live) store_elem(o, 4 * j + e, x[e] * scale);
+          }
+        }
+      }
+    }
+  }
+  if constexpr (TO_PAGES) {
+    if (lane == 0) *page.scale = scale;
+  }
+}
+
+// One wave per (row, head) of the fused QKV output of a step whose rows are one token of one
+// sequence each, as paged_epilogue_kernel: a key or value joins the block at the sequence's end.
+template <int CODE>
+__global__ __launch_bounds__(64) void code_epilogue_kernel(Shape s, StepView sv, int M, int64_t layer_off, PageView v,
+                                                           const int32_t* table, int64_t table_stride, const float* P,
+                                                           int splits, const float* ss, int nb, const float2* rope,
+                                                           float* q_out) {
+  const int r = blockIdx.x, hh = blockIdx.y, i = threadIdx.x;
+  const int dh = s.dh, half = dh / 2;
+  const int N = (s.n_q + 2 * s.n_kv) * dh;
+  const int64_t split_stride = (int64_t)M * N;
+  const int64_t pr = (int64_t)r * N + (int64_t)hh * dh;
+  const int kind = hh < s.n_q ? 0 : (hh < s.n_q + s.n_kv ? 1 : 2);
+  const int pos = sv.row[r].pos;
+  const float inv_rms = row_inv(ss, r, nb, s.d, s.eps);
+  float a = 0.f, b = 0.f;  // of dims i and i + half (lanes past the half, dh 64: none)
+  const bool in = i < half;
+  if (in) {
+    a = add_splits(0.f, P, split_stride, splits, pr + i) * inv_rms;
+    b = add_splits(0.f, P, split_stride, splits, pr + i + half) * inv_rms;
+    if (kind < 2) {
+      const float2 cs = rope[(int64_t)r * half + i];
+      const float a2 = a * cs.x - b * cs.y;
+      const float b2 = a * cs.y + b * cs.x;
+      a = a2;
+      b = b2;
+    }
+  }
+  if (kind == 0) {
+    if (in) {
+      q_out[((int64_t)r * s.n_q + hh) * dh + i] = a;
+      q_out[((int64_t)r * s.n_q + hh) * dh + i + half] = b;
+    }
+    return;
+  }
+  const int page = table[(int64_t)r * table_stride + (pos >> v.shift)];
+  const int which = kind - 1, head = hh - s.n_q - which * s.n_kv, cell = pos & ((1 << v.shift) - 1);
+  const int kept = cell % kBlockCells;
+  const BlockAt to = block_at(v, layer_off, page, which, head, cell - kept);
+  const float old = kept ? *to.scale : 0.f;
+  const uint32_t top = wave_top(max(magnitude(a), magnitude(b)));
+  const float scale = grown<CODE>(old, kept, top), inv = inverse(scale);
+  const bool grew = kept && scale > old;
+  const uint32_t codes = encode4<CODE>(a * inv, b * inv, 0.f, 0.f);
+  if (which == 0) {
+    if (grew) shrink_keys<CODE>(to.codes, kept, dh, old * inv, i);
+    if (in) {
+      to.codes[kept * dh + i] = (uint8_t)codes;
+      to.codes[kept * dh + i + half] = (uint8_t)(codes >> 8);
+    }
+  } else if (in) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      uint4* dst = reinterpret_cast<uint4*>(to.codes + ((i + k * half) << v.shift));
+      const uint32_t w = (codes >> (8 * k) & 0xFFu) * 0x01010101u;  // (behind the last cell: anything)
+      uint4 o = make_uint4(w, w, w, w);
+      if (kept) o = merge_values<CODE>(*dst, o, kept, grew, old * inv);
+      *dst = o;
+    }
+  }
+  if (i == 0) *to.scale = scale;
+}
+
+// ---- attention ----------------------------------------------------------------------------
+
+// Eight codes as eight bf16, exactly: the operand of a 16x16x32 product.
+template <int CODE>
+__device__ __forceinline__ uint4 code_frag(uint32_t w0, uint32_t w1) {
+  const uint32_t w[2] = {w0, w1};
+  uint32_t o[4];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if constexpr (is_i8(CODE)) {
+      float x[4];
+      decode4<CODE>(w[j], x);
+      o[2 * j] = __builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302u);
+      o[2 * j + 1] = __builtin_amdgcn_perm(__float_as_uint(x[3]), __float_as_uint(x[2]), 0x07060302u);
+    } else {
+      o[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[j], 1.f, false));
+      o[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[j], 1.f, true));
+    }
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// The first n of 16 codes, the others zero.
+__device__ __forceinline__ uint4 keep_codes(const uint4& v, int n) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t o[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int k = n - 4 * j;
+    o[j] = k >= 4 ? w[j] : k <= 0 ? 0u : w[j] & ((1u << (8 * k)) - 1);
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// Attention over codes: the plan of paged_attn_kernel (both products turned over, nothing
+// exchanged between lanes but the maximum, cells straight from the page to the operands), with a
+// step of 64 keys whose lane group g holds the scores and values of block g of 16 cells.  So a lane
+// has one scale for its 16 scores and one for its 16 probabilities, applied in fp32 outside the
+// products:
+//   s_j = scale log2(e) sk q.ck_j,   o = sum_j (p_j sv) cv_j / sum_j p_j.
+// Row r of key tile t stands for key 16 (r / 4) + 4 t + r % 4.  A 16-byte load of a key's row is 16
+// dims, two operands of the 16x16x32 products; the queries are laid out alike.
+// HBM bounds it: a cell is 2 (dh + 1/4) bytes and 4 G dh operations.
+template <int CODE, int DH, bool QLO>
+__global__ __launch_bounds__(64 * kWaves, 2) void code_attn_kernel(PageView v, int64_t layer_off, PagedAttn a,
+                                                                float scale2, int tiles, float* o_part,
+                                                                float2* ml_part) {
+  constexpr int KT = kCodeStep, NT = 4, NK = DH / 64, ND = DH / 16, B = kBlockCells;
+  constexpr int OS = DH + 4;
+  __shared__ float o_lds[kWaves * 16 * OS];
+  __shared__ float2 ml_lds[kWaves * 16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i = lane & 15, g = lane >> 4;
+  const int split = blockIdx.x, splits = gridDim.x, seq = blockIdx.z;
+  const int head = blockIdx.y / tiles, tile = blockIdx.y % tiles;
+  const int G = a.n_q / v.n_kv, q0 = head * G + tile * 16, nh = min(16, G - tile * 16);
+
+  const int len = live_cells(a, v.shift, seq);
+  const int range = range_cells(len, splits, KT * kWaves);
+  const int r0 = split * range;
+  if (r0 >= len && split > 0) return;  // (the join counts the ranges alike)
+  const int r1 = min(len, r0 + range), share = range / kWaves;
+  const int k_begin = r0 + wave * share, k_end = min(r1, k_begin + share);
+  const bool solo = range >= len;  // (an empty sequence: range 0, this writes its zeros)
+
+  uint4 qh[2 * NK], ql[2 * NK];
+  const int64_t q_at = (int64_t)seq * a.q_stride + (int64_t)(q0 + min(i, nh - 1)) * DH + g * 16;
+#pragma unroll
+  for (int c = 0; c < 2 * NK; ++c)
+    query_frag(a.q, a.q_bf16, q_at + c / 2 * 64 + c % 2 * 8, qh[c], ql[c], bf16_t{});
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const int P1 = (1 << v.shift) - 1;
+  const int32_t* tab = a.table + (int64_t)seq * a.table_stride;
+  const int64_t page_bytes = v.page(), half = v.half();
+  const char* kbase = v.base + layer_off + ((int64_t)head * DH << v.shift);
+  const char* vbase = kbase + half;
+  const char* sbase = v.base + layer_off + 2 * half + (int64_t)head * v.blocks() * 4;
+  const int64_t v_scales = (int64_t)v.n_kv * v.blocks() * 4;
+  const int last_page = (len - 1) >> v.shift;
+  const int trips = k_begin < k_end ? (k_end - k_begin + KT - 1) / KT : 0;
+
+  int kp, vp, vq;
+  auto pages = [&](int k) {
+    const int k0 = k_begin + k * KT;
+    kp = tab[min((k0 + B * (i >> 2)) >> v.shift, last_page)];
+    vp = tab[min((k0 + B * g) >> v.shift, last_page)];
+  };
+  uint4 kf[NT][NK], vf[ND];
+  float ks, vs;
+  int nl;
+  auto issue_keys = [&](int k) {
+    const int kb = k_begin + k * KT + B * (i >> 2);
+    const char* kr = kbase + ((unsigned)kp < (unsigned)v.n_pages ? kp : 0) * page_bytes +
+                     ((kb & P1) + (i & 3)) * DH + g * 16;
+    vq = vp;
+    pages(k + 1);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int c = 0; c < NK; ++c) kf[t][c] = ld_global(kr + t * 4 * DH + c * 64);
+  };
+  auto issue_values = [&](int k) {
+    const int vb = k_begin + k * KT + B * g;
+    const bool ok = (unsigned)vq < (unsigned)v.n_pages;
+    nl = ok ? min(k_end - vb, B) : 0;
+    const int64_t page = (ok ? vq : 0) * page_bytes;
+    const char* vr = vbase + page + (((int64_t)i << v.shift) + (vb & P1));
+    const char* sr = sbase + page + (vb & P1) / B * 4;
+    ks = __uint_as_float(ld_global_u32(sr));
+    vs = __uint_as_float(ld_global_u32(sr + v_scales));
+#pragma unroll
+    for (int d = 0; d < ND; ++d) vf[d] = ld_global(vr + (((int64_t)d * 16) << v.shift));
+  };
+  float s[B];
+  auto scores = [&]() {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      f32x4 d = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {
+        const uint4 k0 = code_frag<CODE>(kf[t][c].x, kf[t][c].y), k1 = code_frag<CODE>(kf[t][c].z, kf[t][c].w);
+        d = mma_frag(k0, qh[2 * c], d, bf16_t{});
+        d = mma_frag(k1, qh[2 * c + 1], d, bf16_t{});
+        if constexpr (QLO) {
+          d = mma_frag(k0, ql[2 * c], d, bf16_t{});
+          d = mma_frag(k1, ql[2 * c + 1], d, bf16_t{});
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[4 * t + j] = d[j];
+    }
+  };
+  auto fold = [&]() {
+    const bool whole = __all(nl == B);
+    const float f = ks * scale2;
+#pragma unroll
+    for (int j = 0; j < B; ++j) s[j] = whole || j < nl ? s[j] * f : -INFINITY;
+    float top = s[0];
+#pragma unroll
+    for (int j = 1; j < B; ++j) top = fmaxf(top, s[j]);
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float mn = fmaxf(m, top);
+    const float mu = mn == -INFINITY ? 0.f : mn;  // nothing live yet
+    const float alpha = __builtin_amdgcn_exp2f(m - mu);
+    m = mn;
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < B; ++j) {
+      s[j] = __builtin_amdgcn_exp2f(s[j] - mu);
+      sum += s[j];
+    }
+    l = l * alpha + sum;
+    if (!__all(alpha == 1.f)) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) acc[d] *= alpha;
+    }
+    const float w = nl > 0 ? vs : 0.f;
+#pragma unroll
+    for (int j = 0; j < B; ++j) s[j] *= w;
+    uint4 ph[2], pl[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      split_pair(s[8 * u], s[8 * u + 1], ph[u].x, pl[u].x);
+      split_pair(s[8 * u + 2], s[8 * u + 3], ph[u].y, pl[u].y);
+      split_pair(s[8 * u + 4], s[8 * u + 5], ph[u].z, pl[u].z);
+      split_pair(s[8 * u + 6], s[8 * u + 7], ph[u].w, pl[u].w);
+    }
+    if (!whole) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) vf[d] = keep_codes(vf[d], nl);
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      const uint4 v0 = code_frag<CODE>(vf[d].x, vf[d].y), v1 = code_frag<CODE>(vf[d].z, vf[d].w);
+      acc[d] = mma_frag(v0, ph[0], acc[d], bf16_t{});
+      acc[d] = mma_frag(v0, pl[0], acc[d], bf16_t{});
+      acc[d] = mma_frag(v1, ph[1], acc[d], bf16_t{});
+      acc[d] = mma_frag(v1, pl[1], acc[d], bf16_t{});
+    }
+  };
+  if (trips > 0) {
+    pages(0);
+    issue_keys(0);
+    issue_values(0);
+    for (int k = 0; k + 1 < trips; ++k) {
+      scores();
+      __builtin_amdgcn_sched_barrier(0);
+      issue_keys(k + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      fold();
+      __builtin_amdgcn_sched_barrier(0);
+      issue_values(k + 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    scores();
+    fold();
+  }
+  // l over the key groups of the step
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (g == 0) ml_lds[wave * 16 + i] = make_float2(m, l);
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+    *reinterpret_cast<float4*>(o_lds + (wave * 16 + i) * OS + d * 16 + g * 4) =
+        make_float4(acc[d][0], acc[d][1], acc[d][2], acc[d][3]);
+  __syncthreads();
+  for (int e = tid; e < nh * DH; e += 64 * kWaves) {
+    const int h = e / DH, d = e % DH;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, ml_lds[w * 16 + h].x);
+    const float mu = M == -INFINITY ? 0.f : M;
+    float o = 0.f, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float2 ml = ml_lds[w * 16 + h];
+      const float f = __builtin_amdgcn_exp2f(ml.x - mu);
+      o += f * o_lds[(w * 16 + h) * OS + d];
+      L += f * ml.y;
+    }
+    if (solo) {
+      store_out(a, (int64_t)seq * a.out_stride + (int64_t)(q0 + h) * DH + d, L == 0.f ? 0.f : o / L);
+    } else {
+      const int64_t at = ((int64_t)seq * a.n_q + q0 + h) * splits + split;
+      o_part[at * DH + d] = o;
+      if (d == 0) ml_part[at] = make_float2(M, L);
+    }
+  }
+}
+
+template <int CODE, int DH>
+hipError_t launch_attn(const PageView& v, int64_t layer_off, const PagedAttn& a, int splits, void* work,
+                       hipStream_t st) {
+  const int G = a.n_q / v.n_kv, tiles = (G + 15) / 16;
+  const float scale = a.scale != 0.f ? a.scale : (float)(1.0 / std::sqrt((double)DH));
+  const float scale2 = (float)(scale * 1.4426950408889634);
+  float* o_part = static_cast<float*>(work);
+  float2* ml_part = reinterpret_cast<float2*>(o_part + (int64_t)a.n * a.n_q * splits * DH);
+  const dim3 grid(splits, v.n_kv * tiles, a.n), block(64 * kWaves);
+  if (a.q_bf16)
+    SPP_LAUNCH((code_attn_kernel<CODE, DH, false>), grid, block, 0, st, v, layer_off, a, scale2, tiles, o_part, ml_part);
+  else
+    SPP_LAUNCH((code_attn_kernel<CODE, DH, true>), grid, block, 0, st, v, layer_off, a, scale2, tiles, o_part, ml_part);
+  if (splits > 1) return k::paged_join(v, a, splits, kCodeStep * kWaves, o_part, ml_part, st);
+  return hipGetLastError();
+}
+
+// Calls F<T, CODE, DH> for the types at hand.
+#define SPP_CODES(F, BF16, ...)                                                                          \
+  do {                                                                                                   \
+    if (v.code == SPP_CELLS_I8) {                                                                        \
+      if (v.dh == 128) { if (BF16) F(bf16_t, SPP_CELLS_I8, 128, __VA_ARGS__); else F(float, SPP_CELLS_I8, 128, __VA_ARGS__); } \
+      else { if (BF16) F(bf16_t, SPP_CELLS_I8, 64, __VA_ARGS__); else F(float, SPP_CELLS_I8, 64, __VA_ARGS__); }               \
+    } else {                                                                                             \
+      if (v.dh == 128) { if (BF16) F(bf16_t, SPP_CELLS_E4M3, 128, __VA_ARGS__); else F(float, SPP_CELLS_E4M3, 128, __VA_ARGS__); } \
+      else { if (BF16) F(bf16_t, SPP_CELLS_E4M3, 64, __VA_ARGS__); else F(float, SPP_CELLS_E4M3, 64, __VA_ARGS__); }               \
+    }                                                                                                    \
+  } while (0)
+
+dim3 rows_grid(const PageView& v, const CellRows& c) {
+  return dim3((c.max_cells + kBlockCells - 2) / kBlockCells + 1, 2 * v.n_kv, c.n);
+}
+
+}  // namespace
+
+namespace k {
+
+hipError_t code_attention(const PageView& v, int layer, const PagedAttn& a, int splits, void* work, hipStream_t st) {
+  const int64_t off = v.layer() * layer;
+  if (v.code == SPP_CELLS_I8)
+    return v.dh == 128 ? launch_attn<SPP_CELLS_I8, 128>(v, off, a, splits, work, st)
+                       : launch_attn<SPP_CELLS_I8, 64>(v, off, a, splits, work, st);
+  return v.dh == 128 ? launch_attn<SPP_CELLS_E4M3, 128>(v, off, a, splits, work, st)
+                     : launch_attn<SPP_CELLS_E4M3, 64>(v, off, a, splits, work, st);
+}
+
+hipError_t code_session(const PageView& v, const PageList& l, int n, void* kv, int64_t cap, int64_t c0, int cells,
+                        bool to_pages, hipStream_t st) {
+  const int groups = (cells + 4 * kBlockCells - 1) / (4 * kBlockCells);
+  const dim3 grid(groups * 2 * v.n_kv * v.n_layers), block(256);
+#define SPP_SESSION(T, C, D, W) \
+  SPP_LAUNCH((session_kernel<T, C, D, W>), grid, block, 0, st, v, l, groups, static_cast<T*>(kv), cap, c0, cells)
+  if (to_pages)
+    SPP_CODES(SPP_SESSION, v.given == 2, true);
+  else
+    SPP_CODES(SPP_SESSION, v.given == 2, false);
+#undef SPP_SESSION
+  return hipGetLastError();
+}
+
+hipError_t code_epilogue(const Shape& s, const StepView& sv, int n_rows, int layer, const PageView& v,
+                         const int32_t* table, int64_t table_stride, const float* partials, int splits,
+                         const float* ss, const float2* rope, float* q_out, hipStream_t st) {
+  const dim3 grid(n_rows, s.n_q + 2 * s.n_kv), block(64);
+  const int64_t off = v.layer() * layer;
+  if (v.code == SPP_CELLS_I8)
+    SPP_LAUNCH((code_epilogue_kernel<SPP_CELLS_I8>), grid, block, 0, st, s, sv, n_rows, off, v, table, table_stride,
+               partials, splits, ss, res_blocks(s), rope, q_out);
+  else
+    SPP_LAUNCH((code_epilogue_kernel<SPP_CELLS_E4M3>), grid, block, 0, st, s, sv, n_rows, off, v, table, table_stride,
+               partials, splits, ss, res_blocks(s), rope, q_out);
+  return hipGetLastError();
+}
+
+hipError_t code_write(const PageView& v, int layer, const CellRows& c, hipStream_t st) {
+  const int64_t off = v.layer() * layer;
+#define SPP_WRITE(T, C, D, W) SPP_LAUNCH((write_kernel<T, C, D>), rows_grid(v, c), dim3(64), 0, st, v, off, c)
+  SPP_CODES(SPP_WRITE, c.bf16, 0);
+#undef SPP_WRITE
+  return hipGetLastError();
+}
+
+hipError_t code_read(const PageView& v, int layer, const CellRows& c, hipStream_t st) {
+  const int64_t off = v.layer() * layer;
+#define SPP_READ(T, C, D, W) SPP_LAUNCH((read_kernel<T, C, D>), rows_grid(v, c), dim3(64), 0, st, v, off, c)
+  SPP_CODES(SPP_READ, c.bf16, 0);
+#undef SPP_READ
+  return hipGetLastError();
+}
+
+}  // namespace k
+}  // namespace spp

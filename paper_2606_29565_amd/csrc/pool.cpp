@@ -51,17 +51,22 @@ struct spp_pool_s {
 
 namespace {
 
+bool is_code(int32_t dtype) { return dtype == SPP_CELLS_I8 || dtype == SPP_CELLS_E4M3; }
+int elem_bytes(int32_t dtype) { return is_code(dtype) ? 1 : dtype == SPP_DTYPE_BF16 ? 2 : 4; }
+
 spp_status check_pool_config(const spp_pool_config& c) {
   if (c.n_layers < 1 || c.n_kv_heads < 1 || (c.head_dim != 64 && c.head_dim != 128) ||
-      (c.dtype != SPP_DTYPE_BF16 && c.dtype != SPP_DTYPE_F32))
-    return fail(SPP_E_INVALID_ARG, "n_layers and n_kv_heads >= 1, head_dim 64 or 128, dtype F32 or BF16");
+      (c.dtype != SPP_DTYPE_BF16 && c.dtype != SPP_DTYPE_F32 && !is_code(c.dtype)))
+    return fail(SPP_E_INVALID_ARG,
+                "n_layers and n_kv_heads >= 1, head_dim 64 or 128, dtype F32, BF16, I8 or E4M3 codes");
   const int p = c.page_cells;
   if (p != 16 && p != 32 && p != 64 && p != 128 && p != 256)
     return fail(SPP_E_INVALID_ARG, "page_cells must be 16, 32, 64, 128 or 256");
   if (c.n_pages < 1 || c.max_seqs < 1 || c.max_seqs > 65536)
     return fail(SPP_E_INVALID_ARG, "n_pages >= 1 and 1 <= max_seqs <= 65536");
   // bytes of a page below 2^31: kernels address inside one with 32 bits
-  const double page = 2.0 * c.n_layers * c.n_kv_heads * c.head_dim * p * (c.dtype == SPP_DTYPE_BF16 ? 2 : 4);
+  const double scales = is_code(c.dtype) ? c.n_layers * (8.0 * c.n_kv_heads * (p / kBlockCells) + 127) : 0.0;
+  const double page = 2.0 * c.n_layers * c.n_kv_heads * c.head_dim * p * elem_bytes(c.dtype) + scales;
   if (page >= 2147483648.0) return fail(SPP_E_INVALID_ARG, "a page of %g bytes (2 GiB is too many)", page);
   return SPP_OK;
 }
@@ -70,7 +75,7 @@ PageView view_of(const spp_pool_config& c, void* base) {
   int shift = 4;
   while ((1 << shift) < c.page_cells) ++shift;
   return PageView{static_cast<char*>(base), c.n_pages, c.n_layers, c.n_kv_heads, c.head_dim, shift,
-                  c.dtype == SPP_DTYPE_BF16 ? 2 : 4};
+                  elem_bytes(c.dtype), is_code(c.dtype) ? c.dtype : 0};
 }
 
 // Pages that hold `cells` cells.
@@ -231,7 +236,7 @@ spp_status reserve(spp_pool_s& p, int32_t n, const int32_t* seqs, int32_t cells,
 
 spp_status check_model(const spp_pool_s& p, const Model& m) {
   if (m.s.n_layers != p.cfg.n_layers || m.s.n_kv != p.cfg.n_kv_heads || m.s.dh != p.cfg.head_dim ||
-      m.cfg.dtype != p.cfg.dtype || m.device != p.device)
+      (m.cfg.dtype != p.cfg.dtype && !is_code(p.cfg.dtype)) || m.device != p.device)
     return fail(SPP_E_INVALID_ARG, "the model's layers, kv heads, head_dim, dtype or device are not the pool's");
   return SPP_OK;
 }
@@ -247,12 +252,14 @@ spp_status copy_session(spp_pool_s& p, const std::vector<int32_t>& pages, int n,
   if (const spp_status rc = order_after(p, st); rc != SPP_OK) return rc;
   if (const spp_status rc = after_steps(m, st); rc != SPP_OK) return rc;
   const int count = pages_for(p, n);
+  PageView v = p.v;
+  v.given = (int)m.elem;
   const auto copy = [&](int at) -> spp_status {
     PageList l;
     const int c = std::min(kPageBatch, count - at);
     std::copy_n(pages.begin() + at, c, l.a);
     const int64_t c0 = (int64_t)at << p.v.shift;
-    HIPCHK(k::page_session(p.v, l, c, s.kv, s.cap_stride, c0, (int)std::min<int64_t>(n - c0, (int64_t)c << p.v.shift),
+    HIPCHK(k::page_session(v, l, c, s.kv, s.cap_stride, c0, (int)std::min<int64_t>(n - c0, (int64_t)c << p.v.shift),
                            to_pages, st));
     return SPP_OK;
   };
@@ -345,6 +352,11 @@ spp_status guarded(F&& f) {
 
 }  // namespace
 
+const PageView& spp::pool_view(spp_pool_t pool, int* device) {
+  *device = pool->device;
+  return pool->v;
+}
+
 extern "C" {
 
 size_t spp_pool_bytes(const spp_pool_config* cfg) {
@@ -357,7 +369,16 @@ spp_status spp_pool_page_layout(const spp_pool_config* cfg, spp_page_layout* out
   if (const spp_status rc = check_pool_config(*cfg); rc != SPP_OK) return rc;
   const PageView v = view_of(*cfg, nullptr);
   const int64_t P = cfg->page_cells, dh = cfg->head_dim;
-  *out = spp_page_layout{v.page(), 2 * v.half(), v.half(), {P * dh, dh, 1}, {P * dh, 1, P}, v.elem};
+  *out = spp_page_layout{v.page(), v.layer(), v.half(), {P * dh, dh, 1}, {P * dh, 1, P}, v.elem};
+  return SPP_OK;
+}
+
+spp_status spp_pool_scale_layout(const spp_pool_config* cfg, spp_scale_layout* out) {
+  if (!cfg || !out) return fail(SPP_E_INVALID_ARG, "null argument");
+  if (const spp_status rc = check_pool_config(*cfg); rc != SPP_OK) return rc;
+  if (!is_code(cfg->dtype)) return fail(SPP_E_INVALID_ARG, "cells of dtype %d have no scales", cfg->dtype);
+  const PageView v = view_of(*cfg, nullptr);
+  *out = spp_scale_layout{2 * v.half(), 2 * v.half() + 4ll * v.n_kv * v.blocks(), {v.blocks(), 1}, kBlockCells};
   return SPP_OK;
 }
 
