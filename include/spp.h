@@ -716,6 +716,42 @@ spp_status spp_adjust_logits(int32_t n, int32_t vocab, const spp_adjust* rows,
                              spp_summary* summaries, void* work, size_t work_bytes,
                              void* stream);
 
+/* ---- log probabilities -------------------------------------------------------------- */
+
+/* A row of logits and the tokens whose log probabilities are asked: logprobs[i] receives
+ * log p(tokens[i]), p = softmax of the row; NaN for a token outside [0, vocab) (a list may be
+ * filled with -1). */
+typedef struct {
+  const float* logits;       /* device, [vocab]                                           */
+  const int32_t* tokens;     /* device, [n_tokens]                                        */
+  float* logprobs;           /* device, [n_tokens]                                        */
+  int32_t n_tokens;          /* 0..2^30                                                   */
+} spp_logprob_row;
+
+#define SPP_MAX_TOP 64
+
+/* Bytes of workspace that suffice for n rows, and for fewer (0 for bad arguments). */
+size_t spp_logprobs_work_bytes(int32_t n, int32_t vocab, int32_t n_top);
+/* Log probabilities of given tokens over n rows of logits -- those of a resume, a decode step or
+ * adjusted ones -- by which continuations of one state are compared, with what tells how sure
+ * the model was: per row (each nullable) lse[i], the log of the sum of exp(x), and entropy[i] =
+ * -sum p log p in nats; and the n_top (0..SPP_MAX_TOP) most probable tokens, top_tokens and
+ * top_logprobs (device, [n][n_top]), in order, of equal logits the lower index first.
+ * A logit of -inf has probability 0, log probability -inf, and is no alternative; where fewer than n_top
+ * tokens are, the rest are -1 with -inf.  A NaN or +inf makes its row's log probabilities, lse and
+ * entropy NaN (alternatives are still in the order of the logits, NaN left out); a row without any
+ * logit above -inf has lse -inf, and NaN for its log probabilities and entropy.  Sums are of fp32; the largest logit's own
+ * term is kept apart, so a log probability near 0 keeps its relative precision.
+ * rows: host array, read during the call.  No result overlaps another or a logit.  The workspace (device, 16-byte
+ * aligned) is written before it is read; two calls that may run at once need two.  Every pointer
+ * is 4-byte aligned and on the current device.  Only launches kernels on `stream`: it may be
+ * captured into a graph, whose replays read logits and tokens as they are then.
+ * SPP_E_INVALID_ARG for n outside [0, 2^20], vocab outside [1, 2^24], a null pointer or a value
+ * outside what the fields say (then nothing ran). */
+spp_status spp_logprobs(int32_t n, int32_t vocab, const spp_logprob_row* rows, int32_t n_top,
+                        int32_t* top_tokens, float* top_logprobs, float* lse, float* entropy,
+                        void* work, size_t work_bytes, void* stream);
+
 /* ---- gate calibration ------------------------------------------------------------- */
 
 /* One threshold of the gate's risk-coverage curve (Sec. 2.4, Eqs. (coverage), (risk)):

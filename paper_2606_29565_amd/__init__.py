@@ -149,6 +149,11 @@ class spp_adjust(ctypes.Structure):
                 ("presence", ctypes.c_float), ("fill", ctypes.c_float)]
 
 
+class spp_logprob_row(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("tokens", ctypes.c_void_p),
+                ("logprobs", ctypes.c_void_p), ("n_tokens", ctypes.c_int32)]
+
+
 EXPORTS = ["spp_model_create", "spp_model_destroy", "spp_session_kv_bytes", "spp_session_kv_layout",
            "spp_session_create", "spp_session_destroy", "spp_session_id", "spp_session_restore",
            "spp_kv_append_delta", "spp_preposition", "spp_ready_summary", "spp_gate",
@@ -164,7 +169,8 @@ EXPORTS = ["spp_model_create", "spp_model_destroy", "spp_session_kv_bytes", "spp
            "spp_seq_export", "spp_seq_summaries", "spp_decode_batch",
            "spp_paged_attention_work_bytes", "spp_paged_attention",
            "spp_pool_scale_layout", "spp_paged_write", "spp_paged_read",
-           "spp_adjust_logits_work_bytes", "spp_adjust_logits"]
+           "spp_adjust_logits_work_bytes", "spp_adjust_logits",
+           "spp_logprobs_work_bytes", "spp_logprobs"]
 
 _lib = None
 
@@ -237,6 +243,8 @@ def lib() -> ctypes.CDLL:
         "spp_paged_read": (st, [ctypes.POINTER(spp_paged_cells), P]),
         "spp_adjust_logits_work_bytes": (sz, [i32, i32]),
         "spp_adjust_logits": (st, [i32, i32, ctypes.POINTER(spp_adjust), P, P, sz, P]),
+        "spp_logprobs_work_bytes": (sz, [i32, i32, i32]),
+        "spp_logprobs": (st, [i32, i32, ctypes.POINTER(spp_logprob_row), i32, P, P, P, P, P, sz, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -977,6 +985,64 @@ class LogitsAdjust:
         if rc < 0:
             raise SppError(rc, "spp_adjust_logits")
         return self._summ
+
+
+@dataclasses.dataclass
+class LogProbResult:
+    """What LogProbs gives, device tensors: logprobs [n][tokens], lse and entropy [n], top_tokens and
+    top_logprobs [n][top]."""
+    logprobs: object
+    lse: object
+    entropy: object
+    top_tokens: object
+    top_logprobs: object
+
+
+class LogProbs:
+    """spp_logprobs with its rows marshalled once: each call() gives the log probabilities of tokens
+    (int32 device tensor [n][m]; entries outside the vocabulary give NaN) under the rows of logits
+    (fp32 device tensors of the vocabulary), the rows' log-sum-exp and entropy, and their `top` most
+    probable tokens, as a LogProbResult that the next call overwrites.  The workspace is held here:
+    one call at a time, and the object lives until its calls have finished.  A decode keeps one
+    object over its steps: what the tensors hold is read at each call."""
+
+    def __init__(self, vocab: int, rows: Sequence, tokens=None, top: int = 0):
+        import torch
+        n = len(rows)
+        if not n:
+            raise ValueError("no rows")
+        if any(r is None for r in rows):
+            raise ValueError("a row is a tensor of logits")
+        self._dev = dev = rows[0].get_device()
+        if tokens is not None and (tokens.dim() != 2 or tokens.shape[0] != n or tokens.dtype != torch.int32 or
+                                   tokens.get_device() != dev or
+                                   (tokens.shape[1] > 1 and tokens.stride(1) != 1)):
+            raise ValueError("tokens [n][m]: int32 with contiguous rows on the device of the first row")
+        m = 0 if tokens is None else tokens.shape[1]
+        self._keep, self._current_device = (list(rows), tokens), torch.cuda.current_device
+        ptrs = [_vector(r, torch.float32, vocab, dev, i, "logits") for i, r in enumerate(rows)]
+        nbytes = lib().spp_logprobs_work_bytes(n, vocab, top)
+        if not nbytes:
+            raise ValueError("vocab outside [1, 2^24] or top outside [0, 64]")
+        new = lambda *shape, dtype=torch.float32: torch.empty(  # noqa: E731
+            *shape, dtype=dtype, device=rows[0].device)
+        self._out = r = LogProbResult(new(n, m), new(n), new(n), new(n, top, dtype=torch.int32), new(n, top))
+        self._rows = (spp_logprob_row * n)()
+        for i, p in enumerate(ptrs):
+            self._rows[i] = spp_logprob_row(p, tokens.data_ptr() + 4 * i * tokens.stride(0) if m else None,
+                                            r.logprobs.data_ptr() + 4 * i * m if m else None, m)
+        self._work = new(nbytes, dtype=torch.uint8)
+        self._args = (n, vocab, self._rows, top, *(ctypes.c_void_p(_ptr(t)) for t in (
+            r.top_tokens, r.top_logprobs, r.lse, r.entropy, self._work)), ctypes.c_size_t(nbytes))
+        self._call = _unconverted("spp_logprobs")
+
+    def __call__(self, stream=None) -> LogProbResult:
+        if self._current_device() != self._dev:
+            raise ValueError(f"the rows are on device {self._dev}, which is not the current one")
+        rc = self._call(*self._args, ctypes.c_void_p(_stream_of(stream, self._dev)))
+        if rc < 0:
+            raise SppError(rc, "spp_logprobs")
+        return self._out
 
 
 def pack_weight(cfg: spp_model_config, which: int, src, dst, stream=None) -> None:

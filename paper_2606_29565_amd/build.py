@@ -14,15 +14,15 @@ LIB = os.path.join(HERE, "libspp.so")
 OBJDIR = os.path.join(HERE, "_build")
 
 SOURCES = ["gemm.hip", "gemm_tile.hip", "gemm_fp4.hip", "attention.hip", "elementwise.hip",
-           "vocab.hip", "paged.hip", "paged_codes.hip", "logits.hip", "runtime.cpp", "pool.cpp",
-           "cells.cpp"]
+           "vocab.hip", "paged.hip", "paged_codes.hip", "logits.hip", "logprobs.hip",
+           "runtime.cpp", "pool.cpp", "cells.cpp", "logprobs.cpp"]
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I", INCLUDE, "-I", CSRC,
                # packed fp32 instructions stay off on these GPUs (wrong results seen at times)
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 
 def _compile(src: str, verbose: bool) -> str:
-    obj = os.path.join(OBJDIR, os.path.splitext(src)[0] + ".o")
+    obj = os.path.join(OBJDIR, src + ".o")
     cmd = ["hipcc", *HIPCC_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
     if src.endswith(".cpp"):
         cmd[1:1] = ["-x", "hip"]

@@ -1,4 +1,4 @@
-// Internal interface of the kernels over paged caches and adjusted logits.
+// Internal interface of the kernels over paged caches, adjusted logits and log probabilities.
 #pragma once
 
 #include "kernels.hpp"
@@ -118,6 +118,11 @@ hipError_t code_read(const PageView& v, int layer, const CellRows& c, hipStream_
 size_t adjust_work_bytes(int n, int vocab);
 hipError_t adjust_logits(int n, int vocab, const spp_adjust* rows, spp_summary* summaries,
                          void* work, hipStream_t st);
+
+// (No fewer rows need more.)
+size_t logprob_work_bytes(int n, int vocab, int top);
+hipError_t logprobs(int n, int vocab, const spp_logprob_row* rows, int top, int32_t* top_tokens,
+                    float* top_logprobs, float* lse, float* entropy, void* work, hipStream_t st);
 
 }  // namespace k
 }  // namespace spp
