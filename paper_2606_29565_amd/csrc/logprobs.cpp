@@ -1,4 +1,6 @@
 // Log probabilities of rows of logits behind the C ABI (include/spp.h).
+#include <algorithm>
+
 #include "paged.hpp"
 #include "runtime.hpp"
 
@@ -17,7 +19,10 @@ bool shape_ok(int32_t n, int32_t vocab, int32_t n_top) {
 extern "C" {
 
 size_t spp_logprobs_work_bytes(int32_t n, int32_t vocab, int32_t n_top) {
-  return n >= 1 && shape_ok(n, vocab, n_top) ? k::logprob_work_bytes(n, vocab, n_top) : 0;
+  if (n < 1 || !shape_ok(n, vocab, n_top)) return 0;
+  // the most rows that are cut into the shorter slices may take more than n rows
+  const int few = std::min(n, kShortSliceTokens / vocab);
+  return std::max(k::logprob_work_bytes(n, vocab, n_top), few ? k::logprob_work_bytes(few, vocab, n_top) : 0);
 }
 
 spp_status spp_logprobs(int32_t n, int32_t vocab, const spp_logprob_row* rows, int32_t n_top, int32_t* top_tokens,

@@ -70,7 +70,7 @@ struct PageList {
 // Workgroups of an attention call that its ranges make up to: as many sequences or more get no
 // more ranges each for being fewer.
 constexpr int kSplitWorkgroups = 1024;
-// Tokens of all rows up to which adjusted logits are cut into the shorter slices.
+// Tokens of all rows up to which adjusted logits and log probabilities are cut into the shorter slices.
 constexpr int kShortSliceTokens = 2048 * 1024;
 
 namespace k {
@@ -119,7 +119,7 @@ size_t adjust_work_bytes(int n, int vocab);
 hipError_t adjust_logits(int n, int vocab, const spp_adjust* rows, spp_summary* summaries,
                          void* work, hipStream_t st);
 
-// (No fewer rows need more.)
+// Workspace of this very call (of fewer rows it may be more, see kShortSliceTokens).
 size_t logprob_work_bytes(int n, int vocab, int top);
 hipError_t logprobs(int n, int vocab, const spp_logprob_row* rows, int top, int32_t* top_tokens,
                     float* top_logprobs, float* lse, float* entropy, void* work, hipStream_t st);
