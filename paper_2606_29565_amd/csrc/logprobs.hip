@@ -6,15 +6,16 @@
 // cancels: a token of probability near one keeps the relative precision of its log probability, and H is a sum
 // of terms of one sign.
 //
-// Bound by memory: a row is read once, into registers.  A workgroup takes a slice of a row, a
-// second launch puts the slices together (a row of one slice is done in the first).
+// Bound by memory: a row is read once, into registers, a slice of it to a workgroup; a second launch puts
+// the slices together (a row of one slice is done in the first).
 //
-// The alternatives go through a floor that all of them reach.  The lanes of a wave hold their
-// largest values; the largest value that c of them reach is found bit by bit with ballots, on the upper half
-// of the bits.  With c a quarter of n_top the least of the four waves' is a floor of the slice, with
-// c = n_top each wave's is (the floor where a wave has too few values).  What reaches it goes to a short
-// list, whose order is counted.  Ties go to the lower index: an entry of a list is the value's bits,
-// made to order as unsigned integers, above the complement of the index.
+// The alternatives go through a floor that all of them reach: where n_top groups of tokens have largest
+// values that reach a number, so do the n_top largest.  A slice leaves the largest value of
+// every group of 32 tokens, a 32nd of what it reads, with no work on alternatives of its own; the merge finds the
+// floor, reads again the few groups that reach it, and counts the order of the few values that do.  Ties go to the
+// lower index: an entry of that list is the value's bits, made to order as unsigned integers, above
+// the complement of the index.  (The first form had a list in order from every slice: 64 rows of
+// 128256, with 8 alternatives 11.8 us and 4.6 of merge, with 50 14.2 and 6.1; without any 7.8 and 3.3.)
 #include <algorithm>
 
 #include "common.hpp"
@@ -24,8 +25,9 @@ namespace spp {
 namespace {
 
 constexpr int kTpb = 256;
-constexpr int kList = 1024;                     // entries of a slice's short list
-constexpr int kMergeList = 2048;                // entries of all lists of a row that are merged in LDS
+constexpr int kList = 1024;                     // entries of the list of alternatives, and groups they are in
+constexpr int kHeld = 32;                       // groups a thread of the merge keeps in registers
+constexpr int kGroup = 32;                      // tokens of a group: 8 units
 constexpr int kRows = 96;                       // rows of a launch, within 4 KB of arguments
 template <int R>
 struct LogprobBatch {
@@ -33,7 +35,6 @@ struct LogprobBatch {
 };
 static_assert(sizeof(LogprobBatch<kRows>) + 96 <= 4096, "a kernel's argument");
 
-// Where the results go, and what the slices leave for the merge.
 struct LogprobOut {
   int32_t* top_tokens;
   float* top_logprobs;
@@ -78,7 +79,25 @@ __device__ __forceinline__ uint32_t wave_floor(uint32_t u, int c) {
   return floor;
 }
 
-// The entries of `list` in order, the first `top` to out (0 behind the last).  All of the workgroup.
+// A number that `top` of the workgroup's threads' values reach: the least of the waves' floors of a
+// quarter of them, or, where a wave has too few (a mask, or the row's end), the largest of their floors of
+// all, or the lowest number.  All of the workgroup; `lds` 8 words.
+__device__ __forceinline__ float workgroup_floor(float mine, int top, uint32_t* lds) {
+  const uint32_t u = ordered(mine), f = wave_floor(u, (top + 3) / 4);
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) lds[wave] = f;
+  __syncthreads();
+  uint32_t floor = min(min(lds[0], lds[1]), min(lds[2], lds[3]));
+  if (floor == 0) {
+    const uint32_t g = wave_floor(u, top);
+    if ((threadIdx.x & 63) == 0) lds[4 + wave] = g;
+    __syncthreads();
+    floor = max(max(lds[4], lds[5]), max(lds[6], lds[7]));
+  }
+  return floor ? unordered(floor) : -3.402823466e38f;
+}
+
+// The first `top` entries of `list` in order to out (0 behind the last).  All of the workgroup.
 __device__ __forceinline__ void store_top(const uint64_t* list, int n, int top, uint64_t* out) {
   for (int i = threadIdx.x; i < n; i += kTpb) {
     const uint64_t e = list[i];
@@ -90,11 +109,32 @@ __device__ __forceinline__ void store_top(const uint64_t* list, int n, int top, 
   for (int i = n + (int)threadIdx.x; i < top; i += kTpb) out[i] = 0;
 }
 
-__device__ __forceinline__ uint64_t wave_most(uint64_t b) {
+// Where a row starts against 16-byte boundaries: unit u of four tokens starts at token 4 u - a, the
+// whole ones from lo to hi (none: hi < lo).
+struct RowUnits {
+  const float* src;
+  int V, a, lo, hi;
+  __device__ __forceinline__ RowUnits(const float* s, int v) : src(s), V(v) {
+    a = (int)((reinterpret_cast<uintptr_t>(s) & 15) / 4);
+    lo = a ? 4 - a : 0;
+    hi = ((V + a) & ~3) - 4 - a;
+  }
+  // The unit that starts at token t; -inf outside the row.
+  __device__ __forceinline__ void load(int t, float (&x)[4]) const {
+    float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (t >= lo && t <= hi) {
+      q = *reinterpret_cast<const float4*>(src + t);
+    } else if (t + 3 >= 0 && t < V) {
+      q.x = src[min(max(t, 0), V - 1)];
+      q.y = src[min(max(t + 1, 0), V - 1)];
+      q.z = src[min(max(t + 2, 0), V - 1)];
+      q.w = src[min(max(t + 3, 0), V - 1)];
+    }
+    const float f[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) b = max(b, (uint64_t)__shfl_xor((unsigned long long)b, o, 64));
-  return b;
-}
+    for (int e = 0; e < 4; ++e) x[e] = t + e >= 0 && t + e < V ? f[e] : -INFINITY;
+  }
+};
 
 // The first of a thread's tokens and its logit, on their way while the rest is computed.
 struct Given {
@@ -137,73 +177,126 @@ __device__ __forceinline__ void finish_row(const spp_logprob_row& job, int64_t r
   }
 }
 
-// Grid (slices, rows), UNITS * 1024 tokens a slice.  Units of four tokens at 16-byte boundaries of the
-// row, whatever its alignment, unit u of the slice to thread u % 256 (as adjust_kernel).
-template <int UNITS, int R>
-__global__ __launch_bounds__(kTpb) void logprob_slice_kernel(int V, LogprobBatch<R> jobs, int top, Sums* parts,
-                                                             uint64_t* lists, LogprobOut out) {
-  constexpr int S = UNITS * 4 * kTpb;
-  __shared__ Sums wave_sums[4];
-  __shared__ uint32_t floors[2][4];
-  __shared__ uint64_t list[kList];
-  __shared__ uint64_t sorted[SPP_MAX_TOP];
-  __shared__ uint64_t best[4];
-  __shared__ int count;
-  const spp_logprob_row job = jobs.row[blockIdx.y];
-  const float* src = job.logits;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int a = (int)((reinterpret_cast<uintptr_t>(src) & 15) / 4);
-  const int v0 = (int)blockIdx.x * S - a;  // first token of the slice (before the row: none)
-  float x[UNITS][4];
-  const int t_lo = a ? 4 - a : 0, t_hi = ((V + a) & ~3) - 4 - a;  // the row's first and last whole unit
-  if (v0 >= t_lo && v0 + S - 4 <= t_hi) {
+// The alternatives of a row in which too many values reach the floor (the same value over and over, as
+// behind a mask's finite fill): the n_top-th largest value exactly, eight bits at a time by how many have
+// them, then what is above it and the first of its equals.  All of the workgroup, a few times over the row.
+__device__ void exact_top(const float* src, int V, int top, uint32_t* bins, uint64_t* list, int* count,
+                          uint64_t* sorted) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  uint32_t prefix = 0;  // the value's upper bits so far
+  int need = top;       // of those with these bits, so many are still to be found
+  bool all = false;     // fewer than n_top values at all
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int b = tid; b < 256; b += kTpb) bins[b] = 0;
+    __syncthreads();
+    for (int i0 = 0; i0 < V; i0 += kTpb) {
+      const int i = i0 + tid;
+      const uint32_t u = i < V ? ordered(src[i]) : 0u;
+      const bool in = u && (shift == 24 || u >> (shift + 8) == prefix >> (shift + 8));
+      const uint32_t bin = u >> shift & 255u;
+      const uint64_t who = __ballot(in);
+      if (who == 0) continue;
+      // (lanes of one bin, the common case here, add up first)
+      const int lead = __ffsll((unsigned long long)who) - 1;
+      const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)bin, lead);
+      if (__ballot(in && bin == one) == who) {
+        if (lane == lead) atomicAdd(bins + one, (uint32_t)__popcll(who));
+      } else if (in) {
+        atomicAdd(bins + bin, 1u);
+      }
+    }
+    __syncthreads();
+    if (tid == 0) {
+      int b = 255, above = 0;
+      while (b > 0 && above + (int)bins[b] < need) above += bins[b--];
+      count[0] = b;
+      count[1] = need - above;
+      count[2] = b == 0 && above + (int)bins[0] < need;
+    }
+    __syncthreads();
+    prefix |= (uint32_t)count[0] << shift;
+    need = count[1];
+    all = all || count[2] != 0;
+    __syncthreads();
+  }
+  // what is above it (fewer than n_top), then the first of its equals; fewer than n_top at all: each
+  const uint32_t least = all ? 1u : prefix + 1;  // (no value's bits are all ones: that is a NaN)
+  if (tid == 0) count[0] = 0, count[1] = 0;
+  __syncthreads();
+  for (int i = tid; i < V; i += kTpb) {
+    const uint32_t u = ordered(src[i]);
+    if (u >= least) list[atomicAdd(count, 1)] = entry(u, i);
+  }
+  for (int i0 = 0; !all && i0 < V && count[1] < need; i0 += 64) {  // (the first wave's, in order)
+    __syncthreads();
+    if (tid < 64) {
+      const int i = i0 + lane, had = count[1];
+      const bool is = i < V && ordered(src[i]) == prefix;
+      const uint64_t who = __ballot(is);
+      const int at = had + __popcll(who & ((1ull << lane) - 1));
+      if (is && at < need) list[top - need + at] = entry(prefix, i);
+      if (lane == 0) count[1] = min(need, had + __popcll(who));
+    }
+    __syncthreads();
+  }
+  __syncthreads();
+  store_top(list, all ? count[0] : top, top, sorted);
+}
+
+// The slice's tokens into registers.
+template <int UNITS>
+__device__ __forceinline__ void load_slice(const RowUnits& row, int v0, float (&x)[UNITS][4]) {
+  const int tid = threadIdx.x;
+  if (v0 >= row.lo && v0 + UNITS * 4 * kTpb - 4 <= row.hi) {
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-      const float4 q = *reinterpret_cast<const float4*>(src + v0 + 4 * (u * kTpb + tid));
+      const float4 q = *reinterpret_cast<const float4*>(row.src + v0 + 4 * (u * kTpb + tid));
       x[u][0] = q.x; x[u][1] = q.y; x[u][2] = q.z; x[u][3] = q.w;
     }
   } else {
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-      const int t = v0 + 4 * (u * kTpb + tid);
-      float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (t >= t_lo && t <= t_hi) {
-        q = *reinterpret_cast<const float4*>(src + t);
-      } else if (t + 3 >= 0 && t < V) {
-        q.x = src[min(max(t, 0), V - 1)];
-        q.y = src[min(max(t + 1, 0), V - 1)];
-        q.z = src[min(max(t + 2, 0), V - 1)];
-        q.w = src[min(max(t + 3, 0), V - 1)];
-      }
-      const float f[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[u][e] = t + e >= 0 && t + e < V ? f[e] : -INFINITY;
-    }
+    for (int u = 0; u < UNITS; ++u) row.load(v0 + 4 * (u * kTpb + tid), x[u]);
   }
+}
 
-  const bool solo = gridDim.x == 1;
-  Given given{-1, 0.f};
-  if (solo) given = first_given(job, V);
-  float of[UNITS], mine = -INFINITY;  // largest values of a unit and of all, NaN left out
-#pragma unroll
-  for (int u = 0; u < UNITS; ++u) {
-    of[u] = fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3]));
-    mine = fmaxf(mine, of[u]);
-  }
-  const float m = wave_max_all(mine), mu = m == -INFINITY ? 0.f : m;
-  // All terms, the largest one's 1 among them; where it outweighs the others it is left out
-  // instead of taken off.
+// The slice's sums, in every thread; `mine` is the thread's largest value.
+//
+// A thread's own sums are against its largest value so far, eight tokens at a time: they are formed while
+// the later loads are on their way, with nothing to wait for in other lanes.
+template <int UNITS>
+__device__ __forceinline__ Sums slice_sums(const float (&x)[UNITS][4], float& mine, Sums* wave_sums) {
+  mine = -INFINITY;  // (NaN left out)
   float r = 0.f, t = 0.f;
 #pragma unroll
-  for (int u = 0; u < UNITS; ++u)
+  for (int u0 = 0; u0 < UNITS; u0 += 2) {
+    float most = mine;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float d = x[u][e] - mu, w = exp_of(d);
-      r += w;
-      t += w * fmaxf(d, -1e4f);  // (of -inf: nothing)
+    for (int u = u0; u < u0 + 2; ++u)
+      most = fmaxf(most, fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3])));
+    const float mu = most == -INFINITY ? 0.f : most;
+    if (u0) {
+      const float back = mine - mu, w = exp_of(back);
+      t = w * (t + r * fmaxf(back, -1e4f));
+      r *= w;
     }
-  r = wave_sum_all(r);
-  t = wave_sum_all(t);
+    mine = most;
+#pragma unroll
+    for (int u = u0; u < u0 + 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float d = x[u][e] - mu, w = exp_of(d);
+        r += w;
+        t += w * fmaxf(d, -1e4f);  // (of -inf: nothing)
+      }
+  }
+  // The wave's: all terms, the largest one's 1 among them; where it outweighs the others it is left
+  // out instead of taken off.
+  const float m = wave_max_all(mine), mu = m == -INFINITY ? 0.f : m;
+  {
+    const float back = mine - mu, w = exp_of(back);
+    t = wave_sum_all(w * (t + r * fmaxf(back, -1e4f)));
+    r = wave_sum_all(w * r);
+  }
   if (m == -INFINITY) {
     // (no term, or NaN)
   } else if (r >= 2.f) {
@@ -220,113 +313,127 @@ __global__ __launch_bounds__(kTpb) void logprob_slice_kernel(int V, LogprobBatch
       }
     r = wave_sum_all(rest) + (wave_sum_all(same) - 1.f);
   }
-  if (lane == 0) wave_sums[wave] = Sums{m, r, t};
-  if (top > 0) {
-    const uint32_t f = wave_floor(ordered(mine), (top + 3) / 4);
-    if (lane == 0) floors[0][wave] = f;
-    if (tid == 0) count = 0;
-  }
+  if ((threadIdx.x & 63) == 0) wave_sums[threadIdx.x >> 6] = Sums{m, r, t};
   __syncthreads();
-  Sums all;
-  {
-    float M = -INFINITY;
-    int p = 0;
+  float M = -INFINITY;
+  int p = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (wave_sums[k].m > M) M = wave_sums[k].m, p = k;
-    all = wave_sums[p];
+  for (int k = 0; k < 4; ++k)
+    if (wave_sums[k].m > M) M = wave_sums[k].m, p = k;
+  Sums all = wave_sums[p];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k != p) add_part(all, wave_sums[k], M);
-  }
+  for (int k = 0; k < 4; ++k)
+    if (k != p) add_part(all, wave_sums[k], M);
+  return all;
+}
+
+// Grid (slices, rows), UNITS * 1024 tokens a slice: unit u of the slice to thread u % 256.  Leaves the
+// slice's sums and, with `maxima`, the largest values of its groups: of 8 units a thread's, of 2 those
+// of four neighbours.
+template <int UNITS, int R>
+__global__ __launch_bounds__(kTpb) void logprob_slice_kernel(int V, LogprobBatch<R> jobs, Sums* parts, float* maxima) {
+  static_assert(UNITS == 8 || UNITS == 2, "groups of 8 units");
+  constexpr int S = UNITS * 4 * kTpb, GROUPS = S / kGroup;
+  __shared__ Sums wave_sums[4];
+  const RowUnits row(jobs.row[blockIdx.y].logits, V);
+  const int tid = threadIdx.x;
   const int64_t part = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-  if (!solo && tid == 0) parts[part] = all;
-  uint64_t* to = solo ? sorted : lists + part * top;
+  float x[UNITS][4], mine;
+  load_slice<UNITS>(row, (int)blockIdx.x * S - row.a, x);
+  const Sums all = slice_sums<UNITS>(x, mine, wave_sums);
+  if (tid == 0) parts[part] = all;
+  if (!maxima) return;
+  maxima += part * GROUPS;
+  if constexpr (UNITS == 8) {
+    maxima[tid] = mine;
+  } else {
+    mine = fmaxf(mine, __shfl_xor(mine, 1, 64));
+    mine = fmaxf(mine, __shfl_xor(mine, 2, 64));
+    if (tid % 4 == 0) maxima[tid / 4] = mine;
+  }
+}
+// The first token of unit j of group g of a row whose slices are of UNITS units.
+__device__ __forceinline__ int group_token(int units, int a, int g, int j) {
+  const int groups = units * 4 * kTpb / kGroup, slice = g / groups, k = g % groups;
+  const int unit = units == 8 ? j * kTpb + k : (j >> 2) * kTpb + 4 * k + (j & 3);
+  return slice * units * 4 * kTpb - a + 4 * unit;
+}
+
+// Grid (rows): a row of one slice, start to end.
+template <int R>
+__global__ __launch_bounds__(kTpb) void logprob_row_kernel(int V, LogprobBatch<R> jobs, int top, LogprobOut out) {
+  constexpr int UNITS = 8;
+  __shared__ Sums wave_sums[4];
+  __shared__ uint32_t floors[8], bins[256];
+  __shared__ uint64_t list[kList], sorted[SPP_MAX_TOP];
+  __shared__ int count[4];
+  const spp_logprob_row job = jobs.row[blockIdx.x];
+  const RowUnits row(job.logits, V);
+  const int tid = threadIdx.x;
+  float x[UNITS][4], mine;
+  load_slice<UNITS>(row, -row.a, x);
+  const Given given = first_given(job, V);
+  if (tid == 0) count[0] = 0;
+  const Sums all = slice_sums<UNITS>(x, mine, wave_sums);
   if (top > 0) {
-    uint32_t floor = min(min(floors[0][0], floors[0][1]), min(floors[0][2], floors[0][3]));
-    if (floor == 0) {  // (a wave with few values: a mask, or the row's end)
-      const uint32_t f = wave_floor(ordered(mine), top);
-      if (lane == 0) floors[1][wave] = f;
-      __syncthreads();
-      floor = max(max(floors[1][0], floors[1][1]), max(floors[1][2], floors[1][3]));
-    }
-    // (as a number to compare with; NaN compares false, -inf has to)
-    const float least = floor ? unordered(floor) : -3.402823466e38f;
+    const float least = workgroup_floor(mine, top, floors);  // (NaN and -inf compare false with it)
+    if (mine >= least) {
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u)
-      if (of[u] >= least) {
+      for (int u = 0; u < UNITS; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (x[u][e] >= least) {
-            const int at = atomicAdd(&count, 1);
-            if (at < kList) list[at] = entry(ordered(x[u][e]), v0 + 4 * (u * kTpb + tid) + e);
+            const int at = atomicAdd(count, 1);
+            if (at < kList) list[at] = entry(ordered(x[u][e]), 4 * (u * kTpb + tid) + e - row.a);
           }
-      }
+    }
     __syncthreads();
-    const int n = count;
+    const int n = count[0];
     if (n <= kList) {
-      store_top(list, n, top, to);
+      store_top(list, n, top, sorted);
     } else {
-      // Too many (a row of the same value over and over): one after the other, each the largest
-      // below the last.
-      uint64_t last = ~0ull;
-      for (int i = 0; i < top; ++i) {
-        uint64_t b = 0;
+      __syncthreads();
+      exact_top(job.logits, V, top, bins, list, count, sorted);
+    }
+    __syncthreads();
+  }
+  finish_row(job, blockIdx.x, V, all, given, sorted, top, out);
+}
+
+// Grid (rows): the slices of a row put together, in their order, and its alternatives found.
+template <int R>
+__global__ __launch_bounds__(kTpb) void logprob_merge_kernel(int V, LogprobBatch<R> jobs, int units, int slices,
+                                                             int top, const Sums* parts, const float* maxima,
+                                                             LogprobOut out) {
+  __shared__ float red[4], red_r[4], red_t[4];
+  __shared__ int red_p[4], count[4], groups[kList];
+  __shared__ uint32_t floors[8], bins[256];
+  __shared__ uint64_t list[kList], sorted[SPP_MAX_TOP];
+  const spp_logprob_row job = jobs.row[blockIdx.x];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n_groups = slices * (units * 4 * kTpb / kGroup);
+  parts += (int64_t)blockIdx.x * slices;
+  maxima += (int64_t)blockIdx.x * n_groups;
+
+  // All loads go out together: a slice and a token a thread, and the groups' largest values.
+  Sums own{-INFINITY, 0.f, 0.f};
+  if (tid < slices) own = parts[tid];
+  const Given given = first_given(job, V);
+  float held[kHeld], mine = -INFINITY;
+  if (top > 0) {
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u)
+    for (int h = 0; h < kHeld; h += 16) {
+      if (h * kTpb < n_groups) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t o = ordered(x[u][e]);
-            const uint64_t c = o ? entry(o, v0 + 4 * (u * kTpb + tid) + e) : 0;
-            b = c < last && c > b ? c : b;
-          }
-        b = wave_most(b);
-        if (lane == 0) best[wave] = b;
-        __syncthreads();
-        last = max(max(best[0], best[1]), max(best[2], best[3]));
-        __syncthreads();
-        if (tid == 0) to[i] = last;
+        for (int j = h; j < h + 16; ++j) held[j] = maxima[min(j * kTpb + tid, n_groups - 1)];
+      } else {
+#pragma unroll
+        for (int j = h; j < h + 16; ++j) held[j] = -INFINITY;
       }
     }
   }
-  if (!solo) return;
-  __syncthreads();
-  finish_row(job, blockIdx.y, V, all, given, sorted, top, out);
-}
+  if (tid < 4) count[tid] = 0;
 
-// Grid (rows): the slices of a row put together, in their order.
-//
-// Every slice's list is in order, so j lists whose entry number p (from 0) reaches a value have j (p + 1)
-// entries that do: the largest value that ceil(top / (p + 1)) of the lists' entries p reach is a floor of the
-// alternatives, for every p, and the highest of those tried counts.
-template <int R>
-__global__ __launch_bounds__(kTpb) void logprob_merge_kernel(int V, LogprobBatch<R> jobs, int slices, int top,
-                                                             const Sums* parts, const uint64_t* lists, LogprobOut out) {
-  __shared__ float red[4];
-  __shared__ float red_r[4], red_t[4];
-  __shared__ int red_p[4];
-  __shared__ uint64_t red_most[4];
-  __shared__ uint64_t all[kMergeList], list[kMergeList];
-  __shared__ uint64_t sorted[SPP_MAX_TOP];
-  __shared__ int count;
-  const spp_logprob_row job = jobs.row[blockIdx.x];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int entries = min((int64_t)slices * top, (int64_t)kMergeList + 1);
-  parts += (int64_t)blockIdx.x * slices;
-  lists += (int64_t)blockIdx.x * slices * top;
-  // All loads go out together: a first slice and token a thread, and the lists.
-  const Given given = first_given(job, V);
-  Sums own{-INFINITY, 0.f, 0.f};
-  if (tid < slices) own = parts[tid];
-  const bool fits = top > 0 && entries <= kMergeList;
-  if (fits) {
-    constexpr int N = kMergeList / kTpb;
-    uint64_t e[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) e[j] = lists[min(tid + j * kTpb, entries - 1)];
-#pragma unroll
-    for (int j = 0; j < N; ++j) all[tid + j * kTpb] = e[j];
-  }
   float m = own.m;
   int at = m > -INFINITY ? tid : 0x7FFFFFFF;
   for (int s = tid + kTpb; s < slices; s += kTpb) {
@@ -336,10 +443,21 @@ __global__ __launch_bounds__(kTpb) void logprob_merge_kernel(int V, LogprobBatch
   const float wm = wave_max_all(m);
   const int wp = wave_min_all(m == wm ? at : 0x7FFFFFFF);
   if (lane == 0) red[wave] = wm, red_p[wave] = wp;
-  if (tid == 0) count = 0;
-  __syncthreads();
+  float least = 0.f;
+  if (top > 0) {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      held[j] = j * kTpb + tid < n_groups ? held[j] : -INFINITY;
+      mine = fmaxf(mine, held[j]);
+    }
+    for (int g = kHeld * kTpb + tid; g < n_groups; g += kTpb) mine = fmaxf(mine, maxima[g]);
+    least = workgroup_floor(mine, top, floors);
+  } else {
+    __syncthreads();
+  }
   const float M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
   int p = 0x7FFFFFFF;
+#pragma unroll
   for (int k = 0; k < 4; ++k)
     if (red[k] == M) p = min(p, red_p[k]);
   Sums a{M, 0.f, 0.f};
@@ -355,47 +473,45 @@ __global__ __launch_bounds__(kTpb) void logprob_merge_kernel(int V, LogprobBatch
   a.r = wave_sum_all(a.r);
   a.t = wave_sum_all(a.t);
   if (lane == 0) red_r[wave] = a.r, red_t[wave] = a.t;
-  uint64_t most = 1;
-  if (fits) {
-    // entries p of about thrice a list's share, and the last
-    const int ps = min(top, 3 * top / slices + 2);
-    for (int i = tid; i < slices * ps; i += kTpb) {
-      const int s0 = i / ps, k = i % ps + 1 == ps ? top - 1 : i % ps, need = (top + k) / (k + 1);
-      const uint64_t e = all[s0 * top + k];
-      int reach = 0;
-#pragma unroll 8
-      for (int s = 0; s < slices; ++s) reach += all[s * top + k] >= e;
-      if (reach >= need) most = max(most, e);
-    }
+  if (top > 0 && mine >= least) {
+    auto take = [&](int g) {
+      const int k = atomicAdd(count + 1, 1);
+      if (k < kList) groups[k] = g;
+    };
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+      if (held[j] >= least) take(j * kTpb + tid);
+    for (int g = kHeld * kTpb + tid; g < n_groups; g += kTpb)
+      if (maxima[g] >= least) take(g);
   }
-  most = wave_most(most);
-  if (lane == 0) red_most[wave] = most;
   __syncthreads();
   a.r = red_r[0] + red_r[1] + red_r[2] + red_r[3];
   a.t = red_t[0] + red_t[1] + red_t[2] + red_t[3];
-  if (fits) {
-    const uint64_t floor = max(max(red_most[0], red_most[1]), max(red_most[2], red_most[3]));
-    for (int i = tid; i < entries; i += kTpb)
-      if (all[i] >= floor) list[atomicAdd(&count, 1)] = all[i];
-    __syncthreads();
-    store_top(list, count, top, sorted);
-  } else {  // (more than fit: one after the other, each the largest below the last)
-    uint64_t last = ~0ull;
-    for (int i = 0; i < top; ++i) {
-      uint64_t b = 0;
-      for (int64_t k = tid; k < (int64_t)slices * top; k += kTpb) {
-        const uint64_t e = lists[k];
-        b = e < last && e > b ? e : b;
+  if (top > 0) {
+    const RowUnits row(job.logits, V);
+    const int n = count[1];
+    if (n <= kList) {
+      for (int i = tid; i < 8 * n; i += kTpb) {
+        const int t = group_token(units, row.a, groups[i >> 3], i & 7);
+        float x[4];
+        row.load(t, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (x[e] >= least) {
+            const int k = atomicAdd(count, 1);
+            if (k < kList) list[k] = entry(ordered(x[e]), t + e);
+          }
       }
-      b = wave_most(b);
       __syncthreads();
-      if (lane == 0) red_most[wave] = b;
-      __syncthreads();
-      last = max(max(red_most[0], red_most[1]), max(red_most[2], red_most[3]));
-      if (tid == 0) sorted[i] = last;
     }
+    if (n <= kList && count[0] <= kList) {
+      store_top(list, count[0], top, sorted);
+    } else {
+      __syncthreads();
+      exact_top(job.logits, V, top, bins, list, count, sorted);
+    }
+    __syncthreads();
   }
-  __syncthreads();
   finish_row(job, blockIdx.x, V, a, given, sorted, top, out);
 }
 
@@ -407,34 +523,38 @@ int slice_units(int n, int vocab) {
 int slices_of(int units, int vocab) {  // whatever the row's alignment
   return (vocab + 3 + units * 4 * kTpb - 1) / (units * 4 * kTpb);
 }
-size_t work_of(int units, int n, int vocab, int top) {
-  const size_t slices = (size_t)n * slices_of(units, vocab);
-  return (slices * sizeof(Sums) + 15) / 16 * 16 + slices * top * sizeof(uint64_t);
-}
 
 template <int UNITS, int R>
-void launch_rows(int m, int vocab, const spp_logprob_row* rows, int top, Sums* parts, uint64_t* lists, LogprobOut out,
-                 hipStream_t st) {
+void launch_rows(int m, int vocab, const spp_logprob_row* rows, int top, Sums* parts, float* maxima,
+                 const LogprobOut& out, hipStream_t st) {
   LogprobBatch<R> b{};
   std::copy_n(rows, m, b.row);
   const int slices = slices_of(UNITS, vocab);
-  SPP_LAUNCH((logprob_slice_kernel<UNITS, R>), dim3(slices, m), dim3(kTpb), 0, st, vocab, b, top, parts, lists, out);
-  if (slices > 1)
-    SPP_LAUNCH((logprob_merge_kernel<R>), dim3(m), dim3(kTpb), 0, st, vocab, b, slices, top, parts, lists, out);
+  if (slices == 1) {
+    SPP_LAUNCH((logprob_row_kernel<R>), dim3(m), dim3(kTpb), 0, st, vocab, b, top, out);
+    return;
+  }
+  SPP_LAUNCH((logprob_slice_kernel<UNITS, R>), dim3(slices, m), dim3(kTpb), 0, st, vocab, b, parts,
+             top > 0 ? maxima : nullptr);
+  SPP_LAUNCH((logprob_merge_kernel<R>), dim3(m), dim3(kTpb), 0, st, vocab, b, UNITS, slices, top, parts, maxima, out);
 }
+
+size_t parts_bytes(int n, int slices) { return ((size_t)n * slices * sizeof(Sums) + 15) / 16 * 16; }
 
 }  // namespace
 
 namespace k {
 
-size_t logprob_work_bytes(int n, int vocab, int top) { return work_of(slice_units(n, vocab), n, vocab, top); }
+size_t logprob_work_bytes(int n, int vocab, int top) {
+  const int units = slice_units(n, vocab), slices = slices_of(units, vocab);
+  return parts_bytes(n, slices) + (top ? (size_t)n * slices * (units * 4 * kTpb / kGroup) * sizeof(float) : 0);
+}
 
 hipError_t logprobs(int n, int vocab, const spp_logprob_row* rows, int top, int32_t* top_tokens, float* top_logprobs,
                     float* lse, float* entropy, void* work, hipStream_t st) {
   const int units = slice_units(n, vocab), slices = slices_of(units, vocab);
   Sums* parts = static_cast<Sums*>(work);
-  uint64_t* lists = reinterpret_cast<uint64_t*>(static_cast<char*>(work) +
-                                                ((size_t)n * slices * sizeof(Sums) + 15) / 16 * 16);
+  float* maxima = reinterpret_cast<float*>(static_cast<char*>(work) + parts_bytes(n, slices));
   const int launches = (n - 1) / kRows + 1, step = (n - 1) / launches + 1;  // (of like size)
   for (int r0 = 0; r0 < n; r0 += step) {
     const int m = std::min(step, n - r0);
@@ -442,7 +562,7 @@ hipError_t logprobs(int n, int vocab, const spp_logprob_row* rows, int top, int3
     const LogprobOut out{top_tokens + t, top_logprobs + t, lse ? lse + r0 : nullptr, entropy ? entropy + r0 : nullptr};
     const auto launch = units == 2 ? (m == 1 ? launch_rows<2, 1> : launch_rows<2, kRows>)
                                    : (m == 1 ? launch_rows<8, 1> : launch_rows<8, kRows>);
-    launch(m, vocab, rows + r0, top, parts + p, lists + p * top, out, st);
+    launch(m, vocab, rows + r0, top, parts + p, maxima + p * (units * 4 * kTpb / kGroup), out, st);
   }
   return hipGetLastError();
 }
