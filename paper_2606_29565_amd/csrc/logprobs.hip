@@ -25,8 +25,9 @@ namespace spp {
 namespace {
 
 constexpr int kTpb = 256;
+constexpr int kMergeTpb = 512;                  // of the merge, whose steps wait for each other
 constexpr int kList = 1024;                     // entries of the list of alternatives, and groups they are in
-constexpr int kHeld = 32;                       // groups a thread of the merge keeps in registers
+constexpr int kHeld = 16;                       // groups a thread of the merge keeps in registers
 constexpr int kGroup = 32;                      // tokens of a group: 8 units
 constexpr int kRows = 96;                       // rows of a launch, within 4 KB of arguments
 template <int R>
@@ -68,45 +69,87 @@ __device__ __forceinline__ float unordered(uint32_t u) {
 }
 __device__ __forceinline__ uint64_t entry(uint32_t u, int index) { return (uint64_t)u << 32 | (uint32_t)~index; }
 
-// The largest value, lower half zero, that c lanes of the wave reach (0: so many have none).
-__device__ __forceinline__ uint32_t wave_floor(uint32_t u, int c) {
-  uint32_t floor = 0;
-#pragma unroll
-  for (int b = 31; b >= 16; --b) {
-    const uint32_t next = floor | 1u << b;
-    floor = __popcll(__ballot(u >= next)) >= c ? next : floor;
+// A number that c lanes of the wave reach, at most 2^17 numbers below the largest such; hi: the wave's
+// largest.  (0: so many have no value.)
+__device__ __forceinline__ uint32_t wave_floor(uint32_t u, uint32_t hi, int c) {
+  uint32_t lo = (uint32_t)wave_min_all((int)(u ^ 0x80000000u)) ^ 0x80000000u;  // (the order of signed integers)
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  while (hi - lo > 0x20000u) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (__popcll(__ballot(u >= mid)) >= c)
+      lo = mid;
+    else
+      hi = mid;
   }
-  return floor;
+  return lo;
 }
 
-// A number that `top` of the workgroup's threads' values reach: the least of the waves' floors of a
-// quarter of them, or, where a wave has too few (a mask, or the row's end), the largest of their floors of
-// all, or the lowest number.  All of the workgroup; `lds` 8 words.
-__device__ __forceinline__ float workgroup_floor(float mine, int top, uint32_t* lds) {
-  const uint32_t u = ordered(mine), f = wave_floor(u, (top + 3) / 4);
-  const int wave = threadIdx.x >> 6;
+// A number that `top` of the workgroup's threads' values reach, W waves: the least of the waves' floors of
+// a Wth of them, or, where a wave has too few (a mask, or the row's end), the largest of their floors of all,
+// or the lowest number.  All of the workgroup; `lds` 2 W words.
+template <int W>
+__device__ __forceinline__ float workgroup_floor(float mine, float wave_most, int top, uint32_t* lds) {
+  const int wave = threadIdx.x >> 6, c = (top + W - 1) / W;
+  const uint32_t u = ordered(mine), hi = ordered(wave_most), f = c == 1 ? hi : wave_floor(u, hi, c);
   if ((threadIdx.x & 63) == 0) lds[wave] = f;
   __syncthreads();
-  uint32_t floor = min(min(lds[0], lds[1]), min(lds[2], lds[3]));
+  uint32_t floor = lds[0];
+#pragma unroll
+  for (int k = 1; k < W; ++k) floor = min(floor, lds[k]);
   if (floor == 0) {
-    const uint32_t g = wave_floor(u, top);
-    if ((threadIdx.x & 63) == 0) lds[4 + wave] = g;
+    const uint32_t g = wave_floor(u, hi, top);
+    if ((threadIdx.x & 63) == 0) lds[W + wave] = g;
     __syncthreads();
-    floor = max(max(lds[4], lds[5]), max(lds[6], lds[7]));
+#pragma unroll
+    for (int k = 0; k < W; ++k) floor = max(floor, lds[W + k]);
   }
-  return floor ? unordered(floor) : -3.402823466e38f;
+  return floor >= 0x00800000u ? unordered(floor) : -3.402823466e38f;
 }
 
-// The first `top` entries of `list` in order to out (0 behind the last).  All of the workgroup.
+// Sum over the four lanes of a quad.
+__device__ __forceinline__ int quad_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, true);  // lanes 1 0 3 2
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, true);  // lanes 2 3 0 1
+}
+// The first `top` entries of `list` in order to out (0 behind the last): four threads count how many are
+// above an entry.  All of the workgroup.
 __device__ __forceinline__ void store_top(const uint64_t* list, int n, int top, uint64_t* out) {
-  for (int i = threadIdx.x; i < n; i += kTpb) {
-    const uint64_t e = list[i];
+  const int part = threadIdx.x & 3;
+  for (int i0 = 0; i0 < n; i0 += blockDim.x / 4) {
+    const int i = i0 + (threadIdx.x >> 2);
+    const uint64_t e = list[min(i, n - 1)];
     int rank = 0;
 #pragma unroll 8
-    for (int j = 0; j < n; ++j) rank += list[j] > e;
-    if (rank < top) out[rank] = e;
+    for (int j = part; j < n; j += 4) rank += list[j] > e;
+    rank = quad_sum(rank);
+    if (i < n && part == 0 && rank < top) out[rank] = e;
   }
-  for (int i = n + (int)threadIdx.x; i < top; i += kTpb) out[i] = 0;
+  for (int i = n + (int)threadIdx.x; i < top; i += blockDim.x) out[i] = 0;
+}
+
+// The wave's lanes append item(j) to a list of `cap` entries for every j of N with has(j): one addition to
+// its length for all.  (Over `cap` the length still grows.)
+template <int N, typename H, typename F>
+__device__ __forceinline__ void append(int* length, int cap, H has, F put) {
+  uint64_t who[N];
+  int total = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    who[j] = __ballot(has(j));
+    total += __popcll(who[j]);
+  }
+  if (total == 0) return;
+  int at = 0;
+  if ((threadIdx.x & 63) == 0) at = atomicAdd(length, total);
+  at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (who[j]) {
+      const int mine = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(who[j] >> 32),
+                                                      __builtin_amdgcn_mbcnt_lo((uint32_t)who[j], 0u));
+      if (has(j) && mine < cap) put(j, mine);
+      at += __popcll(who[j]);
+    }
 }
 
 // Where a row starts against 16-byte boundaries: unit u of four tokens starts at token 4 u - a, the
@@ -118,6 +161,12 @@ struct RowUnits {
     a = (int)((reinterpret_cast<uintptr_t>(s) & 15) / 4);
     lo = a ? 4 - a : 0;
     hi = ((V + a) & ~3) - 4 - a;
+  }
+  // The same of a row that has a whole unit: one load whatever t is, and others only at the row's ends.
+  __device__ __forceinline__ void load_long(int t, float (&x)[4]) const {
+    const float4 q = *reinterpret_cast<const float4*>(src + min(max(t, lo), hi));
+    x[0] = q.x; x[1] = q.y; x[2] = q.z; x[3] = q.w;
+    if (t < lo || t > hi) load(t, x);
   }
   // The unit that starts at token t; -inf outside the row.
   __device__ __forceinline__ void load(int t, float (&x)[4]) const {
@@ -150,30 +199,40 @@ __device__ __forceinline__ Given first_given(const spp_logprob_row& job, int V) 
   return g;
 }
 
-// A row's results from its sums and its alternatives in order.  All of the workgroup.
-__device__ __forceinline__ void finish_row(const spp_logprob_row& job, int64_t row, int V, const Sums& a, Given g,
-                                           const uint64_t* sorted, int top, const LogprobOut& out) {
+// What every log probability of a row is formed from: log p = (x - m) - rest.
+struct RowLog {
+  float m, rest;
+  __device__ __forceinline__ float operator()(float x) const { return (x - m) - rest; }
+};
+
+// A row's sums, and its tokens' log probabilities.  All of the workgroup.
+__device__ __forceinline__ RowLog finish_sums(const spp_logprob_row& job, int64_t row, int V, const Sums& a, Given g,
+                                              const LogprobOut& out) {
   // without a finite largest value nothing has a probability
-  const bool none = a.m == -INFINITY && a.r == a.r, bad = !(a.m > -INFINITY && a.m < INFINITY) && !none;
+  const bool none = a.m == -INFINITY && a.r == a.r, bad = !(a.m > -INFINITY && a.m < INFINITY);
   const float nan = __builtin_nanf("");
-  const float rest = bad ? nan : log1pf(a.r);
-  const int tid = threadIdx.x;
+  const RowLog log{a.m, bad ? nan : log1pf(a.r)};
+  const int tid = threadIdx.x, step = blockDim.x;
   if (tid == 0) {
-    if (out.lse) out.lse[row] = none ? -INFINITY : a.m + rest;
-    if (out.entropy) out.entropy[row] = none ? nan : rest - a.t / (1.f + a.r);
+    if (out.lse) out.lse[row] = none ? -INFINITY : a.m + log.rest;
+    if (out.entropy) out.entropy[row] = log.rest - a.t / (1.f + a.r);
   }
-  auto logprob = [&](float x) { return none ? nan : (x - a.m) - rest; };
-  for (int i = tid; i < job.n_tokens; i += kTpb) {
-    job.logprobs[i] = (unsigned)g.token < (unsigned)V ? logprob(g.logit) : nan;
-    if (i + kTpb < job.n_tokens) {
-      g.token = job.tokens[i + kTpb];
+  for (int i = tid; i < job.n_tokens; i += step) {
+    job.logprobs[i] = (unsigned)g.token < (unsigned)V ? log(g.logit) : nan;
+    if (i + step < job.n_tokens) {
+      g.token = job.tokens[i + step];
       g.logit = job.logits[min(max(g.token, 0), V - 1)];
     }
   }
-  for (int i = tid; i < top; i += kTpb) {
+  return log;
+}
+// Its alternatives, in order.
+__device__ __forceinline__ void finish_top(int64_t row, const RowLog& log, const uint64_t* sorted, int top,
+                                           const LogprobOut& out) {
+  for (int i = threadIdx.x; i < top; i += blockDim.x) {
     const uint64_t e = sorted[i];
     out.top_tokens[row * top + i] = e ? (int32_t)~(uint32_t)e : -1;
-    out.top_logprobs[row * top + i] = e ? logprob(unordered((uint32_t)(e >> 32))) : -INFINITY;
+    out.top_logprobs[row * top + i] = e ? log(unordered((uint32_t)(e >> 32))) : -INFINITY;
   }
 }
 
@@ -187,9 +246,9 @@ __device__ void exact_top(const float* src, int V, int top, uint32_t* bins, uint
   int need = top;       // of those with these bits, so many are still to be found
   bool all = false;     // fewer than n_top values at all
   for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int b = tid; b < 256; b += kTpb) bins[b] = 0;
+    for (int b = tid; b < 256; b += blockDim.x) bins[b] = 0;
     __syncthreads();
-    for (int i0 = 0; i0 < V; i0 += kTpb) {
+    for (int i0 = 0; i0 < V; i0 += blockDim.x) {
       const int i = i0 + tid;
       const uint32_t u = i < V ? ordered(src[i]) : 0u;
       const bool in = u && (shift == 24 || u >> (shift + 8) == prefix >> (shift + 8));
@@ -223,7 +282,7 @@ __device__ void exact_top(const float* src, int V, int top, uint32_t* bins, uint
   const uint32_t least = all ? 1u : prefix + 1;  // (no value's bits are all ones: that is a NaN)
   if (tid == 0) count[0] = 0, count[1] = 0;
   __syncthreads();
-  for (int i = tid; i < V; i += kTpb) {
+  for (int i = tid; i < V; i += blockDim.x) {
     const uint32_t u = ordered(src[i]);
     if (u >= least) list[atomicAdd(count, 1)] = entry(u, i);
   }
@@ -259,12 +318,12 @@ __device__ __forceinline__ void load_slice(const RowUnits& row, int v0, float (&
   }
 }
 
-// The slice's sums, in every thread; `mine` is the thread's largest value.
+// The slice's sums, in every thread; `mine` is the thread's largest value, wave_most the wave's.
 //
 // A thread's own sums are against its largest value so far, eight tokens at a time: they are formed while
 // the later loads are on their way, with nothing to wait for in other lanes.
 template <int UNITS>
-__device__ __forceinline__ Sums slice_sums(const float (&x)[UNITS][4], float& mine, Sums* wave_sums) {
+__device__ __forceinline__ Sums slice_sums(const float (&x)[UNITS][4], float& mine, float& wave_most, Sums* wave_sums) {
   mine = -INFINITY;  // (NaN left out)
   float r = 0.f, t = 0.f;
 #pragma unroll
@@ -292,6 +351,7 @@ __device__ __forceinline__ Sums slice_sums(const float (&x)[UNITS][4], float& mi
   // The wave's: all terms, the largest one's 1 among them; where it outweighs the others it is left
   // out instead of taken off.
   const float m = wave_max_all(mine), mu = m == -INFINITY ? 0.f : m;
+  wave_most = m;
   {
     const float back = mine - mu, w = exp_of(back);
     t = wave_sum_all(w * (t + r * fmaxf(back, -1e4f)));
@@ -338,9 +398,9 @@ __global__ __launch_bounds__(kTpb) void logprob_slice_kernel(int V, LogprobBatch
   const RowUnits row(jobs.row[blockIdx.y].logits, V);
   const int tid = threadIdx.x;
   const int64_t part = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-  float x[UNITS][4], mine;
+  float x[UNITS][4], mine, most;
   load_slice<UNITS>(row, (int)blockIdx.x * S - row.a, x);
-  const Sums all = slice_sums<UNITS>(x, mine, wave_sums);
+  const Sums all = slice_sums<UNITS>(x, mine, most, wave_sums);
   if (tid == 0) parts[part] = all;
   if (!maxima) return;
   maxima += part * GROUPS;
@@ -352,11 +412,13 @@ __global__ __launch_bounds__(kTpb) void logprob_slice_kernel(int V, LogprobBatch
     if (tid % 4 == 0) maxima[tid / 4] = mine;
   }
 }
-// The first token of unit j of group g of a row whose slices are of UNITS units.
-__device__ __forceinline__ int group_token(int units, int a, int g, int j) {
-  const int groups = units * 4 * kTpb / kGroup, slice = g / groups, k = g % groups;
-  const int unit = units == 8 ? j * kTpb + k : (j >> 2) * kTpb + 4 * k + (j & 3);
-  return slice * units * 4 * kTpb - a + 4 * unit;
+// The first token of unit j of group g of a row.
+template <int UNITS>
+__device__ __forceinline__ int group_token(int a, int g, int j) {
+  constexpr int GROUPS = UNITS * 4 * kTpb / kGroup;
+  const int slice = g / GROUPS, k = g % GROUPS;
+  const int unit = UNITS == 8 ? j * kTpb + k : (j >> 2) * kTpb + 4 * k + (j & 3);
+  return slice * (UNITS * 4 * kTpb) - a + 4 * unit;
 }
 
 // Grid (rows): a row of one slice, start to end.
@@ -370,23 +432,20 @@ __global__ __launch_bounds__(kTpb) void logprob_row_kernel(int V, LogprobBatch<R
   const spp_logprob_row job = jobs.row[blockIdx.x];
   const RowUnits row(job.logits, V);
   const int tid = threadIdx.x;
-  float x[UNITS][4], mine;
+  float x[UNITS][4], mine, most;
   load_slice<UNITS>(row, -row.a, x);
   const Given given = first_given(job, V);
   if (tid == 0) count[0] = 0;
-  const Sums all = slice_sums<UNITS>(x, mine, wave_sums);
+  const Sums all = slice_sums<UNITS>(x, mine, most, wave_sums);
   if (top > 0) {
-    const float least = workgroup_floor(mine, top, floors);  // (NaN and -inf compare false with it)
-    if (mine >= least) {
+    const float least = workgroup_floor<4>(mine, most, top, floors);  // (NaN and -inf compare false with it)
 #pragma unroll
-      for (int u = 0; u < UNITS; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (x[u][e] >= least) {
-            const int at = atomicAdd(count, 1);
-            if (at < kList) list[at] = entry(ordered(x[u][e]), 4 * (u * kTpb + tid) + e - row.a);
-          }
-    }
+    for (int u = 0; u < UNITS; u += 2)
+      append<8>(
+          count, kList, [&](int j) { return x[u + j / 4][j % 4] >= least; },
+          [&](int j, int at) {
+            list[at] = entry(ordered(x[u + j / 4][j % 4]), 4 * ((u + j / 4) * kTpb + tid) + j % 4 - row.a);
+          });
     __syncthreads();
     const int n = count[0];
     if (n <= kList) {
@@ -397,122 +456,150 @@ __global__ __launch_bounds__(kTpb) void logprob_row_kernel(int V, LogprobBatch<R
     }
     __syncthreads();
   }
-  finish_row(job, blockIdx.x, V, all, given, sorted, top, out);
+  finish_top(blockIdx.x, finish_sums(job, blockIdx.x, V, all, given, out), sorted, top, out);
 }
 
-// Grid (rows): the slices of a row put together, in their order, and its alternatives found.
-template <int R>
-__global__ __launch_bounds__(kTpb) void logprob_merge_kernel(int V, LogprobBatch<R> jobs, int units, int slices,
-                                                             int top, const Sums* parts, const float* maxima,
-                                                             LogprobOut out) {
-  __shared__ float red[4], red_r[4], red_t[4];
-  __shared__ int red_p[4], count[4], groups[kList];
-  __shared__ uint32_t floors[8], bins[256];
+// Grid (rows): the slices of a row put together, in their order, and its alternatives found.  What it
+// takes is the waits of its steps for each other.
+template <int UNITS, int R>
+__global__ __launch_bounds__(kMergeTpb) void logprob_merge_kernel(int V, LogprobBatch<R> jobs, int slices, int top,
+                                                                  const Sums* parts, const float* maxima,
+                                                                  LogprobOut out) {
+  constexpr int W = kMergeTpb / 64, GROUPS = UNITS * 4 * kTpb / kGroup;
+  __shared__ float red[W], red_r[W], red_t[W];
+  __shared__ int red_p[W], count[4], groups[kList];
+  __shared__ uint32_t floors[2 * W], bins[256];
   __shared__ uint64_t list[kList], sorted[SPP_MAX_TOP];
   const spp_logprob_row job = jobs.row[blockIdx.x];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int n_groups = slices * (units * 4 * kTpb / kGroup);
+  const int n_groups = slices * GROUPS;
   parts += (int64_t)blockIdx.x * slices;
   maxima += (int64_t)blockIdx.x * n_groups;
 
   // All loads go out together: a slice and a token a thread, and the groups' largest values.
   Sums own{-INFINITY, 0.f, 0.f};
   if (tid < slices) own = parts[tid];
-  const Given given = first_given(job, V);
   float held[kHeld], mine = -INFINITY;
   if (top > 0) {
 #pragma unroll
-    for (int h = 0; h < kHeld; h += 16) {
-      if (h * kTpb < n_groups) {
+    for (int h = 0; h < kHeld; h += 8) {
+      if (h * kMergeTpb < n_groups) {
 #pragma unroll
-        for (int j = h; j < h + 16; ++j) held[j] = maxima[min(j * kTpb + tid, n_groups - 1)];
+        for (int j = h; j < h + 8; ++j) held[j] = maxima[min(j * kMergeTpb + tid, n_groups - 1)];
       } else {
 #pragma unroll
-        for (int j = h; j < h + 16; ++j) held[j] = -INFINITY;
+        for (int j = h; j < h + 8; ++j) held[j] = -INFINITY;
       }
     }
   }
+  const Given given = first_given(job, V);
   if (tid < 4) count[tid] = 0;
 
   float m = own.m;
-  int at = m > -INFINITY ? tid : 0x7FFFFFFF;
-  for (int s = tid + kTpb; s < slices; s += kTpb) {
-    const float v = parts[s].m;
-    if (v > m) m = v, at = s;
-  }
+  for (int s = tid + kMergeTpb; s < slices; s += kMergeTpb) m = fmaxf(m, parts[s].m);
   const float wm = wave_max_all(m);
-  const int wp = wave_min_all(m == wm ? at : 0x7FFFFFFF);
-  if (lane == 0) red[wave] = wm, red_p[wave] = wp;
+  if (lane == 0) red[wave] = wm;
   float least = 0.f;
   if (top > 0) {
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
-      held[j] = j * kTpb + tid < n_groups ? held[j] : -INFINITY;
+      held[j] = j * kMergeTpb + tid < n_groups ? held[j] : -INFINITY;
       mine = fmaxf(mine, held[j]);
     }
-    for (int g = kHeld * kTpb + tid; g < n_groups; g += kTpb) mine = fmaxf(mine, maxima[g]);
-    least = workgroup_floor(mine, top, floors);
+    for (int g = kHeld * kMergeTpb + tid; g < n_groups; g += kMergeTpb) mine = fmaxf(mine, maxima[g]);
+    least = workgroup_floor<W>(mine, wave_max_all(mine), top, floors);
   } else {
     __syncthreads();
   }
-  const float M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  int p = 0x7FFFFFFF;
+  float M = red[0];
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (red[k] == M) p = min(p, red_p[k]);
+  for (int k = 1; k < W; ++k) M = fmaxf(M, red[k]);
+  // (every term, the largest one's among them)
   Sums a{M, 0.f, 0.f};
-  for (int s = tid; s < slices; s += kTpb) {
-    const Sums v = s == tid ? own : parts[s];
-    if (s == p) {
-      a.r += v.r;
-      a.t += v.t;
-    } else {
-      add_part(a, v, M);
-    }
-  }
+  if (tid < slices) add_part(a, own, M);
+  for (int s = tid + kMergeTpb; s < slices; s += kMergeTpb) add_part(a, parts[s], M);
   a.r = wave_sum_all(a.r);
   a.t = wave_sum_all(a.t);
   if (lane == 0) red_r[wave] = a.r, red_t[wave] = a.t;
-  if (top > 0 && mine >= least) {
-    auto take = [&](int g) {
-      const int k = atomicAdd(count + 1, 1);
-      if (k < kList) groups[k] = g;
-    };
-#pragma unroll
-    for (int j = 0; j < kHeld; ++j)
-      if (held[j] >= least) take(j * kTpb + tid);
-    for (int g = kHeld * kTpb + tid; g < n_groups; g += kTpb)
-      if (maxima[g] >= least) take(g);
+  if (top > 0) {
+    append<kHeld>(
+        count + 1, kList, [&](int j) { return held[j] >= least; },
+        [&](int j, int at) { groups[at] = j * kMergeTpb + tid; });
+    for (int g0 = kHeld * kMergeTpb; g0 < n_groups; g0 += kMergeTpb) {
+      const int g = g0 + tid;
+      const float v = g < n_groups ? maxima[g] : -INFINITY;
+      append<1>(
+          count + 1, kList, [&](int) { return v >= least; }, [&](int, int at) { groups[at] = g; });
+    }
   }
   __syncthreads();
-  a.r = red_r[0] + red_r[1] + red_r[2] + red_r[3];
-  a.t = red_t[0] + red_t[1] + red_t[2] + red_t[3];
-  if (top > 0) {
-    const RowUnits row(job.logits, V);
-    const int n = count[1];
-    if (n <= kList) {
-      for (int i = tid; i < 8 * n; i += kTpb) {
-        const int t = group_token(units, row.a, groups[i >> 3], i & 7);
-        float x[4];
-        row.load(t, x);
+  const RowUnits row(job.logits, V);
+  const int n = top > 0 ? 8 * min(count[1], kList + 1) : 0;  // units of the groups
+  const bool listed = n <= 8 * kList;
+  constexpr int AHEAD = 2;
+  float x[AHEAD][4];
+  int t[AHEAD];
+  auto units_at = [&](int i0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (x[e] >= least) {
-            const int k = atomicAdd(count, 1);
-            if (k < kList) list[k] = entry(ordered(x[e]), t + e);
-          }
-      }
-      __syncthreads();
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = i0 + k * kMergeTpb + tid;
+      t[k] = i < n ? group_token<UNITS>(row.a, groups[min(i, n - 1) >> 3], i & 7) : V;
+      row.load_long(t[k], x[k]);
     }
-    if (n <= kList && count[0] <= kList) {
-      store_top(list, count[0], top, sorted);
-    } else {
-      __syncthreads();
-      exact_top(job.logits, V, top, bins, list, count, sorted);
+  };
+  if (top > 0 && listed) units_at(0);
+  a.r = red_r[0];
+  a.t = red_t[0];
+#pragma unroll
+  for (int k = 1; k < W; ++k) a.r += red_r[k], a.t += red_t[k];
+  if (a.m == -INFINITY) {
+    // (no term, or NaN)
+  } else if (a.r >= 2.f) {
+    a.r -= 1.f;
+  } else {
+    // The largest term outweighs the others: the first slice that has it gives its R as it is.
+    int at = tid < slices && own.m == M ? tid : 0x7FFFFFFF;
+    for (int s = tid + kMergeTpb; s < slices; s += kMergeTpb)
+      if (parts[s].m == M) at = min(at, s);
+    at = wave_min_all(at);
+    if (lane == 0) red_p[wave] = at;
+    __syncthreads();
+    int p = red_p[0];
+#pragma unroll
+    for (int k = 1; k < W; ++k) p = min(p, red_p[k]);
+    Sums b{M, 0.f, 0.f};
+    for (int s = tid; s < slices; s += kMergeTpb) {
+      if (s == p)
+        b.r += parts[s].r;
+      else
+        add_part(b, parts[s], M);
+    }
+    b.r = wave_sum_all(b.r);
+    if (lane == 0) red[wave] = b.r;
+    __syncthreads();
+    a.r = red[0];
+#pragma unroll
+    for (int k = 1; k < W; ++k) a.r += red[k];
+  }
+  const RowLog log = finish_sums(job, blockIdx.x, V, a, given, out);
+  if (top == 0) return;
+  if (listed) {
+    for (int i0 = 0; i0 < n; i0 += AHEAD * kMergeTpb) {
+      append<4 * AHEAD>(
+          count, kList, [&](int j) { return x[j / 4][j % 4] >= least; },
+          [&](int j, int at) { list[at] = entry(ordered(x[j / 4][j % 4]), t[j / 4] + j % 4); });
+      if (i0 + AHEAD * kMergeTpb < n) units_at(i0 + AHEAD * kMergeTpb);
     }
     __syncthreads();
   }
-  finish_row(job, blockIdx.x, V, a, given, sorted, top, out);
+  if (listed && count[0] <= kList) {
+    store_top(list, count[0], top, sorted);
+  } else {
+    __syncthreads();
+    exact_top(job.logits, V, top, bins, list, count, sorted);
+  }
+  __syncthreads();
+  finish_top(blockIdx.x, log, sorted, top, out);
 }
 
 // Tokens of a slice: 8192 where that makes one of a row, which is then done in one launch; else 2048
@@ -536,7 +623,7 @@ void launch_rows(int m, int vocab, const spp_logprob_row* rows, int top, Sums* p
   }
   SPP_LAUNCH((logprob_slice_kernel<UNITS, R>), dim3(slices, m), dim3(kTpb), 0, st, vocab, b, parts,
              top > 0 ? maxima : nullptr);
-  SPP_LAUNCH((logprob_merge_kernel<R>), dim3(m), dim3(kTpb), 0, st, vocab, b, UNITS, slices, top, parts, maxima, out);
+  SPP_LAUNCH((logprob_merge_kernel<UNITS, R>), dim3(m), dim3(kMergeTpb), 0, st, vocab, b, slices, top, parts, maxima, out);
 }
 
 size_t parts_bytes(int n, int slices) { return ((size_t)n * slices * sizeof(Sums) + 15) / 16 * 16; }
