@@ -119,8 +119,13 @@ __device__ __forceinline__ void store_top(const uint64_t* list, int n, int top, 
     const int i = i0 + (threadIdx.x >> 2);
     const uint64_t e = list[min(i, n - 1)];
     int rank = 0;
-#pragma unroll 8
-    for (int j = part; j < n; j += 4) rank += list[j] > e;
+    for (int j0 = part; j0 - part < n; j0 += 32) {  // (eight reads on their way together)
+      uint64_t o[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] = list[min(j0 + 4 * k, kList - 1)];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) rank += j0 + 4 * k < n && o[k] > e;
+    }
     rank = quad_sum(rank);
     if (i < n && part == 0 && rank < top) out[rank] = e;
   }
@@ -239,7 +244,7 @@ __device__ __forceinline__ void finish_top(int64_t row, const RowLog& log, const
 // The alternatives of a row in which too many values reach the floor (the same value over and over, as
 // behind a mask's finite fill): the n_top-th largest value exactly, eight bits at a time by how many have
 // them, then what is above it and the first of its equals.  All of the workgroup, a few times over the row.
-__device__ void exact_top(const float* src, int V, int top, uint32_t* bins, uint64_t* list, int* count,
+__device__ __attribute__((noinline)) void exact_top(const float* src, int V, int top, uint32_t* bins, uint64_t* list, int* count,
                           uint64_t* sorted) {
   const int tid = threadIdx.x, lane = tid & 63;
   uint32_t prefix = 0;  // the value's upper bits so far
