@@ -162,240 +162,313 @@ __device__ __forceinline__ BlockRows block_rows(const PageView& v, const CellRow
   return r;
 }
 
-// Grid (blocks of a sequence, K and V of each head, sequences), one wave each.
+// A wave's rows of 16 cells of one head: lane l has unit l % UPR (16 bytes, E dims) of the C cells from
+// C (l / UPR) on.
+template <typename T, int DH>
+struct RowMap {
+  static constexpr int E = Elem<T>::kPerFrag, UPR = DH / E, C = kBlockCells * UPR / 64, D = DH / 64;
+  // Where a dim's 16 codes are in the wave's LDS: 16 bytes more every E dims, so that the lanes of a
+  // row write other banks.
+  static constexpr int kBytes = DH * 16 + DH / E * 16;
+  static __device__ __forceinline__ int at(int dim) { return dim * 16 + dim / E * 16; }
+};
+template <typename T>
+__device__ __forceinline__ void unit_values(const uint4& x, float* f) {
+  if constexpr (Elem<T>::kPerFrag == 8) frag_to_f32(x, reinterpret_cast<float(&)[8]>(*f));
+  else frag_to_f32(x, reinterpret_cast<float(&)[4]>(*f));
+}
+// What the wave's lanes have written to LDS is there for its lanes to read.
+__device__ __forceinline__ void wave_lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Grid (blocks of a sequence, fastest, times K and V of each head, four to a workgroup; sequences), a
+// wave to a block.  Values change from rows of dims to rows of cells in LDS.
+//
+// Bound by memory: 15000 cells of 5 prompts, 8 heads of 128 in bf16, 79 MB.
 template <typename T, int CODE, int DH>
-__global__ __launch_bounds__(64) void write_kernel(PageView v, int64_t layer_off, CellRows c) {
-  const int lane = threadIdx.x, head = blockIdx.y >> 1, which = blockIdx.y & 1;
-  const BlockRows b = block_rows(v, c, blockIdx.x, blockIdx.z);
+__global__ __launch_bounds__(256) void write_kernel(PageView v, int64_t layer_off, CellRows c, int blocks) {
+  using M = RowMap<T, DH>;
+  __shared__ __align__(16) uint8_t lds[4 * M::kBytes];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int job = blockIdx.x * 4 + wave, hw = job / blocks, head = hw >> 1, which = hw & 1;
+  if (head >= v.n_kv) return;
+  const BlockRows b = block_rows(v, c, job % blocks, blockIdx.y);
   if (!b.any || (unsigned)b.page >= (unsigned)v.n_pages) return;
   const BlockAt to = block_at(v, layer_off, b.page, which, head, b.cell);
-  const T* src = static_cast<const T*>(which ? c.v : c.k) + head * DH;
   const int64_t stride = which ? c.v_stride : c.k_stride;
+  const int unit = lane % M::UPR, cell0 = lane / M::UPR * M::C;
+  const T* src = static_cast<const T*>(which ? c.v : c.k) + head * DH + unit * M::E;
   const float old = b.lo ? *to.scale : 0.f;
+  uint4 x[M::C];  // (rows outside [lo, hi) repeat one inside)
+#pragma unroll
+  for (int p = 0; p < M::C; ++p)
+    x[p] = *reinterpret_cast<const uint4*>(src + (b.row + min(max(cell0 + p, b.lo), b.hi - 1)) * stride);
+  float f[M::C][M::E];
   uint32_t top = 0;
-  if (which == 0) {  // 16 bytes of a row a lane
-    constexpr int E = Elem<T>::kPerFrag, UPR = DH / E, N = kBlockCells * UPR / 64;
-    uint4 x[N];
 #pragma unroll
-    for (int p = 0; p < N; ++p) {
-      const int u = p * 64 + lane, cell = min(max(u / UPR, b.lo), b.hi - 1);
-      x[p] = *reinterpret_cast<const uint4*>(src + (b.row + cell) * stride + u % UPR * E);
-    }
-    // (rows outside [lo, hi) repeat one inside)
+  for (int p = 0; p < M::C; ++p) {
+    unit_values<T>(x[p], f[p]);
 #pragma unroll
-    for (int p = 0; p < N; ++p) {
-      float f[8];
-      if constexpr (E == 8) frag_to_f32(x[p], f); else frag_to_f32(x[p], reinterpret_cast<float(&)[4]>(f));
-#pragma unroll
-      for (int e = 0; e < E; ++e) top = max(top, magnitude(f[e]));
-    }
-    top = wave_top(top);
-    const float scale = grown<CODE>(old, b.lo, top), inv = inverse(scale);
+    for (int e = 0; e < M::E; ++e) top = max(top, magnitude(f[p][e]));
+  }
+  top = wave_top(top);
+  const float scale = grown<CODE>(old, b.lo, top), inv = inverse(scale);
+  if (lane == 0) *to.scale = scale;
+  if (which == 0) {
     if (b.lo && scale > old) shrink_keys<CODE>(to.codes, b.lo, DH, old * inv, lane);
 #pragma unroll
-    for (int p = 0; p < N; ++p) {
-      const int u = p * 64 + lane, cell = u / UPR;
-      float f[8];
-      if constexpr (E == 8) frag_to_f32(x[p], f); else frag_to_f32(x[p], reinterpret_cast<float(&)[4]>(f));
+    for (int p = 0; p < M::C; ++p) {
+      const int cell = cell0 + p;
       if (cell < b.lo || cell >= b.hi) continue;
-      uint32_t* dst = reinterpret_cast<uint32_t*>(to.codes + cell * DH + u % UPR * E);
-      const uint32_t w0 = encode4<CODE>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
-      if constexpr (E == 8)
-        *reinterpret_cast<uint2*>(dst) = make_uint2(w0, encode4<CODE>(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
+      uint32_t* dst = reinterpret_cast<uint32_t*>(to.codes + cell * DH + unit * M::E);
+      const uint32_t w0 = encode4<CODE>(f[p][0] * inv, f[p][1] * inv, f[p][2] * inv, f[p][3] * inv);
+      if constexpr (M::E == 8)
+        *reinterpret_cast<uint2*>(dst) =
+            make_uint2(w0, encode4<CODE>(f[p][4] * inv, f[p][5] * inv, f[p][6] * inv, f[p][7] * inv));
       else
         *dst = w0;
     }
-    if (lane == 0) *to.scale = scale;
     return;
   }
-  // one or two dims of every cell a lane
-  constexpr int D = DH / 64;
-  float x[kBlockCells][D];
+  uint8_t* mine = lds + wave * M::kBytes;
 #pragma unroll
-  for (int i = 0; i < kBlockCells; ++i) {
-    const T* p = src + (b.row + min(max(i, b.lo), b.hi - 1)) * stride + lane * D;
+  for (int e = 0; e < M::E; ++e) {
+    uint8_t* at = mine + M::at(unit * M::E + e) + cell0;
+    if constexpr (M::C == 2) {
+      *reinterpret_cast<uint16_t*>(at) = (uint16_t)encode4<CODE>(f[0][e] * inv, f[1][e] * inv, 0.f, 0.f);
+    } else {
 #pragma unroll
-    for (int d = 0; d < D; ++d) x[i][d] = load_elem(p, d);
+      for (int p = 0; p < M::C; p += 4)
+        *reinterpret_cast<uint32_t*>(at + p) =
+            encode4<CODE>(f[p][e] * inv, f[p + 1][e] * inv, f[p + 2][e] * inv, f[p + 3][e] * inv);
+    }
   }
+  wave_lds_sync();
 #pragma unroll
-  for (int i = 0; i < kBlockCells; ++i)
-#pragma unroll
-    for (int d = 0; d < D; ++d) top = max(top, magnitude(x[i][d]));
-  top = wave_top(top);
-  const float scale = grown<CODE>(old, b.lo, top), inv = inverse(scale);
-#pragma unroll
-  for (int d = 0; d < D; ++d) {
-    uint4* dst = reinterpret_cast<uint4*>(to.codes + ((lane * D + d) << v.shift));
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w[j] = encode4<CODE>(x[4 * j][d] * inv, x[4 * j + 1][d] * inv, x[4 * j + 2][d] * inv, x[4 * j + 3][d] * inv);
-    uint4 o = make_uint4(w[0], w[1], w[2], w[3]);
+  for (int d = 0; d < M::D; ++d) {
+    const int dim = lane + 64 * d;
+    uint4* dst = reinterpret_cast<uint4*>(to.codes + (dim << v.shift));
+    uint4 o = *reinterpret_cast<const uint4*>(mine + M::at(dim));
     if (b.lo) o = merge_values<CODE>(*dst, o, b.lo, scale > old, old * inv);
     *dst = o;
   }
-  if (lane == 0) *to.scale = scale;
 }
 
 // The same grid: cells as values into the caller's rows; zeros where the page is not listed.
 template <typename T, int CODE, int DH>
-__global__ __launch_bounds__(64) void read_kernel(PageView v, int64_t layer_off, CellRows c) {
-  const int lane = threadIdx.x, head = blockIdx.y >> 1, which = blockIdx.y & 1;
-  const BlockRows b = block_rows(v, c, blockIdx.x, blockIdx.z);
+__global__ __launch_bounds__(256) void read_kernel(PageView v, int64_t layer_off, CellRows c, int blocks) {
+  using M = RowMap<T, DH>;
+  __shared__ __align__(16) uint8_t lds[4 * M::kBytes];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int job = blockIdx.x * 4 + wave, hw = job / blocks, head = hw >> 1, which = hw & 1;
+  if (head >= v.n_kv) return;
+  const BlockRows b = block_rows(v, c, job % blocks, blockIdx.y);
   if (!b.any) return;
-  T* dst = static_cast<T*>(which ? c.v : c.k) + head * DH;
   const int64_t stride = which ? c.v_stride : c.k_stride;
   const bool listed = (unsigned)b.page < (unsigned)v.n_pages;
   const BlockAt at = block_at(v, layer_off, listed ? b.page : 0, which, head, b.cell);
-  const float scale = listed ? *at.scale : 0.f;
+  const float held = *at.scale, scale = listed ? held : 0.f;
+  const int unit = lane % M::UPR, cell0 = lane / M::UPR * M::C;
+  T* dst = static_cast<T*>(which ? c.v : c.k) + head * DH + unit * M::E;
+  uint32_t w[M::C][M::E / 4];  // codes of the lane's dims, cell by cell
   if (which == 0) {
-    constexpr int UPR = DH / 16, N = kBlockCells * UPR / 64;
 #pragma unroll
-    for (int p = 0; p < N; ++p) {
-      const int u = p * 64 + lane, cell = u / UPR;
-      uint4 w = *reinterpret_cast<const uint4*>(at.codes + u * 16);
-      if (!listed) w = make_uint4(0, 0, 0, 0);
-      if (cell < b.lo || cell >= b.hi) continue;
-      T* o = dst + (b.row + cell) * stride + u % UPR * 16;
-      values4<CODE>(w.x, scale, o);
-      values4<CODE>(w.y, scale, o + 4);
-      values4<CODE>(w.z, scale, o + 8);
-      values4<CODE>(w.w, scale, o + 12);
+    for (int p = 0; p < M::C; ++p) {
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(at.codes + (cell0 + p) * DH + unit * M::E);
+#pragma unroll
+      for (int k = 0; k < M::E / 4; ++k) w[p][k] = src[k];
     }
-    return;
-  }
-  constexpr int D = DH / 64;
-  uint4 w[D];
+  } else {
+    uint8_t* mine = lds + wave * M::kBytes;
 #pragma unroll
-  for (int d = 0; d < D; ++d) {
-    w[d] = *reinterpret_cast<const uint4*>(at.codes + ((lane * D + d) << v.shift));
-    if (!listed) w[d] = make_uint4(0, 0, 0, 0);
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    float x[D][4];
-#pragma unroll
-    for (int d = 0; d < D; ++d) decode4<CODE>(j == 0 ? w[d].x : j == 1 ? w[d].y : j == 2 ? w[d].z : w[d].w, x[d]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int cell = 4 * j + i;
-      if (cell < b.lo || cell >= b.hi) continue;
-      T* o = dst + (b.row + cell) * stride + lane * D;
-#pragma unroll
-      for (int d = 0; d < D; ++d) store_elem(o, d, x[d][i] * scale);
+    for (int d = 0; d < M::D; ++d) {
+      const int dim = lane + 64 * d;
+      *reinterpret_cast<uint4*>(mine + M::at(dim)) = *reinterpret_cast<const uint4*>(at.codes + (dim << v.shift));
     }
+    wave_lds_sync();
+#pragma unroll
+    for (int k = 0; k < M::E / 4; ++k) {
+#pragma unroll
+      for (int p = 0; p < M::C; ++p) w[p][k] = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint8_t* from = mine + M::at(unit * M::E + 4 * k + e) + cell0;
+        uint32_t q[(M::C + 3) / 4];
+        if constexpr (M::C == 2) {
+          q[0] = *reinterpret_cast<const uint16_t*>(from);
+        } else {
+#pragma unroll
+          for (int p = 0; p < M::C / 4; ++p) q[p] = *reinterpret_cast<const uint32_t*>(from + 4 * p);
+        }
+#pragma unroll
+        for (int p = 0; p < M::C; ++p) w[p][k] |= (q[p / 4] >> (8 * (p % 4)) & 0xFFu) << (8 * e);
+      }
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < M::C; ++p) {
+    const int cell = cell0 + p;
+    float x[M::E];
+#pragma unroll
+    for (int k = 0; k < M::E / 4; ++k) decode4<CODE>(listed ? w[p][k] : 0u, reinterpret_cast<float(&)[4]>(x[4 * k]));
+    if (cell < b.lo || cell >= b.hi) continue;
+    uint32_t o[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (M::E == 8)  // (exact: the upper halves)
+        o[k] = __builtin_amdgcn_perm(__float_as_uint(x[2 * k + 1] * scale), __float_as_uint(x[2 * k] * scale), 0x07060302u);
+      else
+        o[k] = __float_as_uint(x[k] * scale);
+    }
+    *reinterpret_cast<uint4*>(dst + (b.row + cell) * stride) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
 
-// Grid (blocks of the pages' cells, four to a workgroup, fastest, times layers * 2 * kv heads), a wave
-// to a block: one block of a session's cells into its page, or out of it.  Only live cells move; the cells of the
-// session past the last stay as they are.
+// Grid (64 cells of the copy, fastest, times layers * 2 * kv heads): four blocks of one head's keys or values,
+// between a session's buffer and their pages.  Keys: a wave to a block, rows of dims on both sides.  Values:
+// rows of cells on both sides, read and written 16 bytes of the session's at a time, UPR lanes to a row of 64
+// cells, so that whole lines move; a block's largest value is put together over the workgroup.  Only live
+// cells move; the cells of the session past the last stay as they are.  The loads pass the L2 by (they are
+// read once).
 template <typename T, int CODE, int DH, bool TO_PAGES>
 __global__ __launch_bounds__(256) void session_kernel(PageView v, PageList l, int groups, T* kv, int64_t cap,
                                                       int64_t c0, int cells) {
   constexpr int E = Elem<T>::kPerFrag;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int at = (blockIdx.x % groups * 4 + wave) * kBlockCells;  // of the cells that are copied
-  if (at >= cells) return;
+  __shared__ uint32_t tops[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int base = blockIdx.x % groups * 64;  // of the cells that are copied
   const int hd = blockIdx.x / groups, head = hd % v.n_kv, which = hd / v.n_kv % 2, layer = hd / v.n_kv / 2;
-  const int live = min(kBlockCells, cells - at);
-  const BlockAt page = block_at(v, v.layer() * layer, l.a[at >> v.shift], which, head, at & ((1 << v.shift) - 1));
+  const int64_t layer_off = v.layer() * layer;
   T* sess = kv + ((int64_t)(2 * layer + which) * v.n_kv + head) * cap * DH;
-  sess += which ? c0 + at : (c0 + at) * DH;
-  uint32_t top = 0;
-  float scale = 0.f, inv = 0.f;
-  if constexpr (!TO_PAGES) scale = *page.scale;
+  auto load = [](const void* p) {
+    const u32x4 q = __builtin_nontemporal_load(static_cast<const u32x4*>(p));
+    return make_uint4(q.x, q.y, q.z, q.w);
+  };
   if (which == 0) {
+    const int at = base + wave * kBlockCells, live = min(kBlockCells, cells - at);
+    if (live <= 0) return;
+    const BlockAt page = block_at(v, layer_off, l.a[at >> v.shift], 0, head, at & ((1 << v.shift) - 1));
+    sess += (c0 + at) * DH;
     constexpr int N = kBlockCells * DH / E / 64;
+    const int units = live * (DH / E);
     if constexpr (TO_PAGES) {
       uint4 x[N];
 #pragma unroll
-      for (int p = 0; p < N; ++p)
-        x[p] = *reinterpret_cast<const uint4*>(sess + (int64_t)min(p * 64 + lane, live * (DH / E) - 1) * E);
-      float f[N][8];
+      for (int p = 0; p < N; ++p) x[p] = load(sess + (int64_t)min(p * 64 + lane, units - 1) * E);
+      float f[N][E];
+      uint32_t top = 0;
 #pragma unroll
       for (int p = 0; p < N; ++p) {
-        if constexpr (E == 8) frag_to_f32(x[p], f[p]); else frag_to_f32(x[p], reinterpret_cast<float(&)[4]>(f[p]));
+        unit_values<T>(x[p], f[p]);
 #pragma unroll
         for (int e = 0; e < E; ++e) top = max(top, magnitude(f[p][e]));
       }
-      scale = scale_for<CODE>(wave_top(top));
-      inv = inverse(scale);
+      const float scale = scale_for<CODE>(wave_top(top)), inv = inverse(scale);
 #pragma unroll
       for (int p = 0; p < N; ++p) {
         const int u = p * 64 + lane;
-        if (u >= live * (DH / E)) continue;
+        if (u >= units) continue;
         uint32_t* dst = reinterpret_cast<uint32_t*>(page.codes + u * E);
-        dst[0] = encode4<CODE>(f[p][0] * inv, f[p][1] * inv, f[p][2] * inv, f[p][3] * inv);
-        if constexpr (E == 8) dst[1] = encode4<CODE>(f[p][4] * inv, f[p][5] * inv, f[p][6] * inv, f[p][7] * inv);
+        const uint32_t w0 = encode4<CODE>(f[p][0] * inv, f[p][1] * inv, f[p][2] * inv, f[p][3] * inv);
+        if constexpr (E == 8)
+          *reinterpret_cast<uint2*>(dst) =
+              make_uint2(w0, encode4<CODE>(f[p][4] * inv, f[p][5] * inv, f[p][6] * inv, f[p][7] * inv));
+        else
+          *dst = w0;
       }
+      if (lane == 0) *page.scale = scale;
     } else {
+      const float scale = *page.scale;
+      uint32_t w[N][E / 4];
+#pragma unroll
+      for (int p = 0; p < N; ++p) {
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(page.codes + min(p * 64 + lane, units - 1) * E);
+#pragma unroll
+        for (int k = 0; k < E / 4; ++k) w[p][k] = __builtin_nontemporal_load(src + k);
+      }
 #pragma unroll
       for (int p = 0; p < N; ++p) {
         const int u = p * 64 + lane;
-        if (u >= live * (DH / E)) continue;
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(page.codes + u * E);
-        values4<CODE>(src[0], scale, sess + u * E);
-        if constexpr (E == 8) values4<CODE>(src[1], scale, sess + u * E + 4);
+        if (u < units)
+#pragma unroll
+          for (int k = 0; k < E / 4; ++k) values4<CODE>(w[p][k], scale, sess + u * E + 4 * k);
       }
     }
-  } else {
-    // a row of 16 cells of one or two dims a lane (the session's rows hold whole blocks: cap is a
-    // multiple of 64)
-    constexpr int D = DH / 64, U = kBlockCells / E;
-    if constexpr (TO_PAGES) {
-      uint4 x[D][U];
-#pragma unroll
-      for (int d = 0; d < D; ++d)
-#pragma unroll
-        for (int u = 0; u < U; ++u) x[d][u] = *reinterpret_cast<const uint4*>(sess + (lane + 64 * d) * cap + u * E);
-      float f[D][U][8];
-#pragma unroll
-      for (int d = 0; d < D; ++d)
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if constexpr (E == 8) frag_to_f32(x[d][u], f[d][u]); else frag_to_f32(x[d][u], reinterpret_cast<float(&)[4]>(f[d][u]));
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            if (u * E + e >= live) f[d][u][e] = 0.f;  // (whatever lies behind the last cell)
-            top = max(top, magnitude(f[d][u][e]));
-          }
-        }
-      scale = scale_for<CODE>(wave_top(top));
-      inv = inverse(scale);
-#pragma unroll
-      for (int d = 0; d < D; ++d) {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float* g = f[d][4 * j / E] + 4 * j % E;
-          w[j] = encode4<CODE>(g[0] * inv, g[1] * inv, g[2] * inv, g[3] * inv);
-        }
-        *reinterpret_cast<uint4*>(page.codes + ((lane + 64 * d) << v.shift)) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    } else {
-#pragma unroll
-      for (int d = 0; d < D; ++d) {
-        const uint4 q = *reinterpret_cast<const uint4*>(page.codes + ((lane + 64 * d) << v.shift));
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-        T* o = sess + (lane + 64 * d) * cap;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (4 * j + 4 <= live) {
-            values4<CODE>(w[j], scale, o + 4 * j);
-          } else {
-            float x[4];
-            decode4<CODE>(w[j], x);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (4 * j + e < live) store_elem(o, 4 * j + e, x[e] * scale);
-          }
-        }
-      }
-    }
+    return;
   }
+  // Thread: unit `unit` of the rows of dims d0, d0 + ROWS ...; the unit's cells are of one block.
+  constexpr int UPR = 64 / E, ROWS = 256 / UPR, N = DH / ROWS;
+  const int unit = tid % UPR, d0 = tid / UPR, at = base + unit * E, block = unit * E / kBlockCells;
+  const bool any = at - at % kBlockCells < cells;  // (a block without a cell may have no page)
+  const int live = min(max(cells - at, 0), E);     // of the unit
+  const int cell = at & ((1 << v.shift) - 1), inner = cell % kBlockCells;
+  const BlockAt page = block_at(v, layer_off, any ? l.a[at >> v.shift] : l.a[0], 1, head, any ? cell - inner : 0);
+  sess += c0 + at;
   if constexpr (TO_PAGES) {
-    if (lane == 0) *page.scale = scale;
+    if (tid < 4) tops[tid] = 0;
+    uint4 x[N];  // (the session's rows hold whole blocks of 64 cells)
+#pragma unroll
+    for (int p = 0; p < N; ++p) x[p] = load(sess + (int64_t)(d0 + p * ROWS) * cap);
+    float f[N][E];
+    uint32_t top = 0;
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+      unit_values<T>(x[p], f[p]);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (e >= live) f[p][e] = 0.f;  // (whatever lies behind the last cell)
+        top = max(top, magnitude(f[p][e]));
+      }
+    }
+    __syncthreads();
+    // over the wave's lanes of the block: those of its other rows, and of its other units
+#pragma unroll
+    for (int o = 32; o >= UPR; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+#pragma unroll
+    for (int o = kBlockCells / E / 2; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    if (lane < UPR && inner == 0) atomicMax(&tops[block], top);
+    __syncthreads();
+    const float scale = scale_for<CODE>(tops[block]), inv = inverse(scale);
+    if (!any) return;
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+      uint32_t* dst = reinterpret_cast<uint32_t*>(page.codes + ((d0 + p * ROWS) << v.shift) + inner);
+      const uint32_t w0 = encode4<CODE>(f[p][0] * inv, f[p][1] * inv, f[p][2] * inv, f[p][3] * inv);
+      if constexpr (E == 8)
+        *reinterpret_cast<uint2*>(dst) =
+            make_uint2(w0, encode4<CODE>(f[p][4] * inv, f[p][5] * inv, f[p][6] * inv, f[p][7] * inv));
+      else
+        *dst = w0;
+    }
+    if (d0 == 0 && inner == 0) *page.scale = scale;
+  } else {
+    if (live == 0) return;
+    const float scale = *page.scale;
+    uint32_t w[N][E / 4];
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(page.codes + ((d0 + p * ROWS) << v.shift) + inner);
+#pragma unroll
+      for (int k = 0; k < E / 4; ++k) w[p][k] = __builtin_nontemporal_load(src + k);
+    }
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+      T* o = sess + (int64_t)(d0 + p * ROWS) * cap;
+#pragma unroll
+      for (int k = 0; k < E / 4; ++k) {
+        if (live == E) {
+          values4<CODE>(w[p][k], scale, o + 4 * k);
+        } else {
+          float x[4];
+          decode4<CODE>(w[p][k], x);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (4 * k + e < live) store_elem(o, 4 * k + e, x[e] * scale);
+        }
+      }
+    }
   }
 }
 
@@ -726,8 +799,10 @@ hipError_t launch_attn(const PageView& v, int64_t layer_off, const PagedAttn& a,
     }                                                                                                    \
   } while (0)
 
+// The most blocks that a sequence's cells are in.
+int row_blocks(const CellRows& c) { return (c.max_cells + kBlockCells - 2) / kBlockCells + 1; }
 dim3 rows_grid(const PageView& v, const CellRows& c) {
-  return dim3((c.max_cells + kBlockCells - 2) / kBlockCells + 1, 2 * v.n_kv, c.n);
+  return dim3((unsigned)(((int64_t)row_blocks(c) * 2 * v.n_kv + 3) / 4), c.n);
 }
 
 }  // namespace
@@ -773,7 +848,7 @@ hipError_t code_epilogue(const Shape& s, const StepView& sv, int n_rows, int lay
 
 hipError_t code_write(const PageView& v, int layer, const CellRows& c, hipStream_t st) {
   const int64_t off = v.layer() * layer;
-#define SPP_WRITE(T, C, D, W) SPP_LAUNCH((write_kernel<T, C, D>), rows_grid(v, c), dim3(64), 0, st, v, off, c)
+#define SPP_WRITE(T, C, D, W) SPP_LAUNCH((write_kernel<T, C, D>), rows_grid(v, c), dim3(256), 0, st, v, off, c, row_blocks(c))
   SPP_CODES(SPP_WRITE, c.bf16, 0);
 #undef SPP_WRITE
   return hipGetLastError();
@@ -781,7 +856,7 @@ hipError_t code_write(const PageView& v, int layer, const CellRows& c, hipStream
 
 hipError_t code_read(const PageView& v, int layer, const CellRows& c, hipStream_t st) {
   const int64_t off = v.layer() * layer;
-#define SPP_READ(T, C, D, W) SPP_LAUNCH((read_kernel<T, C, D>), rows_grid(v, c), dim3(64), 0, st, v, off, c)
+#define SPP_READ(T, C, D, W) SPP_LAUNCH((read_kernel<T, C, D>), rows_grid(v, c), dim3(256), 0, st, v, off, c, row_blocks(c))
   SPP_CODES(SPP_READ, c.bf16, 0);
 #undef SPP_READ
   return hipGetLastError();
