@@ -195,16 +195,18 @@ __global__ __launch_bounds__(256) void write_kernel(PageView v, int64_t layer_of
   const int job = blockIdx.x * 4 + wave, hw = job / blocks, head = hw >> 1, which = hw & 1;
   if (head >= v.n_kv) return;
   const BlockRows b = block_rows(v, c, job % blocks, blockIdx.y);
-  if (!b.any || (unsigned)b.page >= (unsigned)v.n_pages) return;
-  const BlockAt to = block_at(v, layer_off, b.page, which, head, b.cell);
+  if (!b.any) return;
   const int64_t stride = which ? c.v_stride : c.k_stride;
   const int unit = lane % M::UPR, cell0 = lane / M::UPR * M::C;
   const T* src = static_cast<const T*>(which ? c.v : c.k) + head * DH + unit * M::E;
-  const float old = b.lo ? *to.scale : 0.f;
   uint4 x[M::C];  // (rows outside [lo, hi) repeat one inside)
 #pragma unroll
   for (int p = 0; p < M::C; ++p)
     x[p] = *reinterpret_cast<const uint4*>(src + (b.row + min(max(cell0 + p, b.lo), b.hi - 1)) * stride);
+  __builtin_amdgcn_sched_barrier(0);  // (the rows are on their way before the page's number is looked at)
+  if ((unsigned)b.page >= (unsigned)v.n_pages) return;
+  const BlockAt to = block_at(v, layer_off, b.page, which, head, b.cell);
+  const float old = b.lo ? *to.scale : 0.f;
   float f[M::C][M::E];
   uint32_t top = 0;
 #pragma unroll
@@ -596,8 +598,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void code_attn_kernel(PageView v, i
   const int range = range_cells(len, splits, KT * kWaves);
   const int r0 = split * range;
   if (r0 >= len && split > 0) return;  // (the join counts the ranges alike)
-  const int r1 = min(len, r0 + range), share = range / kWaves;
-  const int k_begin = r0 + wave * share, k_end = min(r1, k_begin + share);
+  // The waves take the steps of the range in turn, so that the halves of a line of V^T (pages of 128 cells
+  // and more) are read by neighbours at about the same time.
+  const int r1 = min(len, r0 + range), k_begin = r0 + wave * KT, k_end = r1;
+  constexpr int STEP = KT * kWaves;
   const bool solo = range >= len;  // (an empty sequence: range 0, this writes its zeros)
 
   uint4 qh[2 * NK], ql[2 * NK];
@@ -618,11 +622,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void code_attn_kernel(PageView v, i
   const char* sbase = v.base + layer_off + 2 * half + (int64_t)head * v.blocks() * 4;
   const int64_t v_scales = (int64_t)v.n_kv * v.blocks() * 4;
   const int last_page = (len - 1) >> v.shift;
-  const int trips = k_begin < k_end ? (k_end - k_begin + KT - 1) / KT : 0;
+  const int trips = k_begin < k_end ? (k_end - k_begin + STEP - 1) / STEP : 0;
 
   int kp, vp, vq;
   auto pages = [&](int k) {
-    const int k0 = k_begin + k * KT;
+    const int k0 = k_begin + k * STEP;
     kp = tab[min((k0 + B * (i >> 2)) >> v.shift, last_page)];
     vp = tab[min((k0 + B * g) >> v.shift, last_page)];
   };
@@ -630,7 +634,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void code_attn_kernel(PageView v, i
   float ks, vs;
   int nl;
   auto issue_keys = [&](int k) {
-    const int kb = k_begin + k * KT + B * (i >> 2);
+    const int kb = k_begin + k * STEP + B * (i >> 2);
     const char* kr = kbase + ((unsigned)kp < (unsigned)v.n_pages ? kp : 0) * page_bytes +
                      ((kb & P1) + (i & 3)) * DH + g * 16;
     vq = vp;
@@ -641,7 +645,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void code_attn_kernel(PageView v, i
       for (int c = 0; c < NK; ++c) kf[t][c] = ld_global(kr + t * 4 * DH + c * 64);
   };
   auto issue_values = [&](int k) {
-    const int vb = k_begin + k * KT + B * g;
+    const int vb = k_begin + k * STEP + B * g;
     const bool ok = (unsigned)vq < (unsigned)v.n_pages;
     nl = ok ? min(k_end - vb, B) : 0;
     const int64_t page = (ok ? vq : 0) * page_bytes;
