@@ -636,11 +636,11 @@ spp_status spp_pool_scale_layout(const spp_pool_config* cfg, spp_scale_layout* o
  * spp_paged_attention.  A sequence with first[i] < 0 or rows[i] < 0, rows from n_rows on, rows of a
  * sequence past max_cells and cells past its table are left out. */
 typedef struct {
-  spp_pool_t pool;           /* of 8-bit codes                                            */
+  spp_pool_t pool;           /* of 8-bit codes, at most 32767 kv heads                    */
   int32_t layer;
   int32_t n_seqs;            /* 0..65535 (0: nothing is done)                             */
   const int32_t* table;      /* device, [n_seqs] rows of max_pages page numbers           */
-  int64_t table_stride;      /* entries between rows, >= max_pages                        */
+  int64_t table_stride;      /* entries between rows, max_pages..2^31 - 1                 */
   int32_t max_pages;         /* >= 1; max_pages*page_cells <= 2^30                        */
   const int32_t* first;      /* device, [n_seqs]                                          */
   const int32_t* rows;       /* device, [n_seqs + 1]                                      */
@@ -648,7 +648,8 @@ typedef struct {
   int32_t max_cells;         /* most cells of a sequence, 1..2^24; times n_kv_heads <= 2^33 */
   int32_t io_dtype;          /* spp_dtype of k and v                                      */
   void* k;                   /* device, [n_rows] rows of [n_kv_heads][head_dim]           */
-  int64_t k_stride;          /* elements between rows, a multiple of 8; k 16-byte aligned */
+  int64_t k_stride;          /* elements between rows, a multiple of 8 below 2^35; k 16-byte
+                                aligned                                                   */
   void* v;                   /* as k                                                      */
   int64_t v_stride;
 } spp_paged_cells;

@@ -19,18 +19,20 @@ spp_status check_cells(const spp_paged_cells* a, const PageView** view, int* dev
     return fail(SPP_E_INVALID_ARG, "max_pages < 1 or over 2^30 cells");
   if (a->max_cells < 1 || a->max_cells > (1 << 24)) return fail(SPP_E_INVALID_ARG, "max_cells outside [1, 2^24]");
   if (a->io_dtype != SPP_DTYPE_BF16 && a->io_dtype != SPP_DTYPE_F32) return fail(SPP_E_INVALID_ARG, "io_dtype");
-  if ((int64_t)a->max_cells * v.n_kv > 1ll << 33)
-    return fail(SPP_E_INVALID_ARG, "max_cells times %d kv heads is over 2^33", v.n_kv);
+  if (v.n_kv > 32767 || (int64_t)a->max_cells * v.n_kv > 1ll << 33)
+    return fail(SPP_E_INVALID_ARG, "%d kv heads (at most 32767, times max_cells at most 2^33)", v.n_kv);
   if (a->n_rows < 0) return fail(SPP_E_INVALID_ARG, "n_rows < 0");
   if (a->n_seqs == 0) return SPP_OK;
   if (!a->table || !a->first || !a->rows || (a->n_rows && (!a->k || !a->v)))
     return fail(SPP_E_INVALID_ARG, "null pointer");
   const int64_t row = (int64_t)v.n_kv * v.dh;
-  if (a->k_stride < row || a->v_stride < row || a->k_stride % 8 || a->v_stride % 8 || !aligned(a->k, 16) ||
+  constexpr int64_t most = 8ll * UINT32_MAX;  // (the kernels' form of a stride)
+  if (a->k_stride < row || a->v_stride < row || a->k_stride > most || a->v_stride > most || a->k_stride % 8 || a->v_stride % 8 || !aligned(a->k, 16) ||
       !aligned(a->v, 16))
     return fail(SPP_E_INVALID_ARG, "rows of k and v: %lld elements at least, multiples of 8, 16-byte aligned",
                 (long long)row);
-  if (a->table_stride < a->max_pages) return fail(SPP_E_INVALID_ARG, "table_stride < max_pages");
+  if (a->table_stride < a->max_pages || a->table_stride > INT32_MAX)
+    return fail(SPP_E_INVALID_ARG, "table_stride below max_pages or over 2^31 - 1");
   if (!aligned(a->table, 4) || !aligned(a->first, 4) || !aligned(a->rows, 4))
     return fail(SPP_E_INVALID_ARG, "table, first and rows are 4-byte aligned");
   return SPP_OK;

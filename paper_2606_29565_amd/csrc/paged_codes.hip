@@ -89,11 +89,8 @@ __device__ __forceinline__ void values4(uint32_t w, float scale, float* out) {
   *reinterpret_cast<float4*>(out) = make_float4(x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale);
 }
 
-__device__ __forceinline__ uint32_t wave_top(uint32_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-  return v;
-}
+// The largest magnitude of the wave (below 2^31: in the order of integers, which ~ turns over).
+__device__ __forceinline__ uint32_t wave_top(uint32_t v) { return (uint32_t)~wave_min_all((int)~v); }
 
 // Where a head's block is: its codes (K: the block's first cell, V: its first cell of dim 0) and scale.
 struct BlockAt {
@@ -138,28 +135,56 @@ __device__ __forceinline__ uint4 merge_values(uint4 was, uint4 fresh, int kept, 
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+// A write or read as its kernel takes it: within 100 bytes, as a launch with more takes the host 0.6 us
+// longer (3.4 instead of 2.8).
+struct RowsArg {
+  char* layer;                   // the layer in page 0
+  int64_t page;                  // bytes between pages
+  const int32_t *table, *first, *rows;
+  void *k, *v;
+  uint32_t k_stride8, v_stride8;  // elements between rows, by eight
+  int32_t table_stride, max_pages, n_pages, n_rows, max_cells;
+  uint16_t shift, heads2;        // log2 of a page's cells; kv heads, keys and values apart
+};
+static_assert(sizeof(RowsArg) <= 96, "a short launch");
+__device__ __forceinline__ int row_blocks(int max_cells) { return (max_cells + kBlockCells - 2) / kBlockCells + 1; }
+
 // What a wave of a write or a read has: a block of one head's keys or values, and the rows of the
 // caller that are its cells lo .. hi - 1.
 struct BlockRows {
   bool any;
+  int which, head;
   int page, cell, lo, hi;  // the block's first cell in its page; lo: cells before it are kept
   int64_t row;             // of cell 0 of the block (before the sequence's first row for cells < lo)
 };
-__device__ __forceinline__ BlockRows block_rows(const PageView& v, const CellRows& c, int b, int seq) {
+__device__ __forceinline__ BlockRows block_rows(const RowsArg& c, int wave, int seq) {
   BlockRows r{};
+  const int blocks = row_blocks(c.max_cells), job = (int)blockIdx.x * 4 + wave, hw = job / blocks;
+  if (hw >= c.heads2) return r;
+  r.which = hw & 1;
+  r.head = hw >> 1;
   const int first = c.first[seq], r0 = c.rows[seq], r1 = min(max(c.rows[seq + 1], 0), c.n_rows);
   if (first < 0 || r0 < 0) return r;
-  const int count = min(min(r1 - r0, c.max_cells), (c.max_pages << v.shift) - first);
+  const int count = min(min(r1 - r0, c.max_cells), (c.max_pages << c.shift) - first);
   if (count <= 0) return r;  // (so first is below 2^30)
-  const int at = (first & -kBlockCells) + kBlockCells * b;
+  const int at = (first & -kBlockCells) + kBlockCells * (job % blocks);
   if (at >= first + count) return r;
   r.any = true;
-  r.page = c.table[seq * c.table_stride + (at >> v.shift)];
-  r.cell = at & ((1 << v.shift) - 1);
+  r.page = c.table[(int64_t)seq * c.table_stride + (at >> c.shift)];
+  r.cell = at & ((1 << c.shift) - 1);
   r.lo = max(first - at, 0);
   r.hi = min(first + count - at, kBlockCells);
   r.row = (int64_t)r0 + at - first;
   return r;
+}
+template <int DH>
+__device__ __forceinline__ BlockAt block_at(const RowsArg& c, const BlockRows& b, int page) {
+  const int heads = c.heads2 >> 1;
+  const int64_t half = (int64_t)heads * DH << c.shift;
+  char* layer = c.layer + page * c.page;
+  char* codes = layer + b.which * half + ((int64_t)b.head * DH << c.shift) + (b.which ? b.cell : b.cell * DH);
+  float* scales = reinterpret_cast<float*>(layer + 2 * half) + ((b.which * heads + b.head) << (c.shift - 4));
+  return BlockAt{reinterpret_cast<uint8_t*>(codes), scales + b.cell / kBlockCells};
 }
 
 // A wave's rows of 16 cells of one head: lane l has unit l % UPR (16 bytes, E dims) of the C cells from
@@ -188,25 +213,31 @@ __device__ __forceinline__ void wave_lds_sync() {
 //
 // Bound by memory: 15000 cells of 5 prompts, 8 heads of 128 in bf16, 79 MB.
 template <typename T, int CODE, int DH>
-__global__ __launch_bounds__(256) void write_kernel(PageView v, int64_t layer_off, CellRows c, int blocks) {
+__global__ __launch_bounds__(256) void write_kernel(RowsArg c) {
   using M = RowMap<T, DH>;
   __shared__ __align__(16) uint8_t lds[4 * M::kBytes];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int job = blockIdx.x * 4 + wave, hw = job / blocks, head = hw >> 1, which = hw & 1;
-  if (head >= v.n_kv) return;
-  const BlockRows b = block_rows(v, c, job % blocks, blockIdx.y);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const BlockRows b = block_rows(c, wave, blockIdx.y);
   if (!b.any) return;
-  const int64_t stride = which ? c.v_stride : c.k_stride;
+  const int64_t stride = 8ll * (b.which ? c.v_stride8 : c.k_stride8);
   const int unit = lane % M::UPR, cell0 = lane / M::UPR * M::C;
-  const T* src = static_cast<const T*>(which ? c.v : c.k) + head * DH + unit * M::E;
+  const T* src = static_cast<const T*>(b.which ? c.v : c.k) + b.head * DH + unit * M::E;
   uint4 x[M::C];  // (rows outside [lo, hi) repeat one inside)
 #pragma unroll
   for (int p = 0; p < M::C; ++p)
     x[p] = *reinterpret_cast<const uint4*>(src + (b.row + min(max(cell0 + p, b.lo), b.hi - 1)) * stride);
   __builtin_amdgcn_sched_barrier(0);  // (the rows are on their way before the page's number is looked at)
-  if ((unsigned)b.page >= (unsigned)v.n_pages) return;
-  const BlockAt to = block_at(v, layer_off, b.page, which, head, b.cell);
-  const float old = b.lo ? *to.scale : 0.f;
+  if ((unsigned)b.page >= (unsigned)c.n_pages) return;
+  const BlockAt to = block_at<DH>(c, b, b.page);
+  // what the block keeps: its scale, and of values the lane's dims
+  float old = 0.f;
+  uint4 was[M::D];
+  if (b.lo) {
+    old = *to.scale;
+    if (b.which)
+#pragma unroll
+      for (int d = 0; d < M::D; ++d) was[d] = *reinterpret_cast<const uint4*>(to.codes + ((lane + 64 * d) << c.shift));
+  }
   float f[M::C][M::E];
   uint32_t top = 0;
 #pragma unroll
@@ -218,7 +249,7 @@ __global__ __launch_bounds__(256) void write_kernel(PageView v, int64_t layer_of
   top = wave_top(top);
   const float scale = grown<CODE>(old, b.lo, top), inv = inverse(scale);
   if (lane == 0) *to.scale = scale;
-  if (which == 0) {
+  if (b.which == 0) {
     if (b.lo && scale > old) shrink_keys<CODE>(to.codes, b.lo, DH, old * inv, lane);
 #pragma unroll
     for (int p = 0; p < M::C; ++p) {
@@ -251,31 +282,29 @@ __global__ __launch_bounds__(256) void write_kernel(PageView v, int64_t layer_of
 #pragma unroll
   for (int d = 0; d < M::D; ++d) {
     const int dim = lane + 64 * d;
-    uint4* dst = reinterpret_cast<uint4*>(to.codes + (dim << v.shift));
+    uint4* dst = reinterpret_cast<uint4*>(to.codes + (dim << c.shift));
     uint4 o = *reinterpret_cast<const uint4*>(mine + M::at(dim));
-    if (b.lo) o = merge_values<CODE>(*dst, o, b.lo, scale > old, old * inv);
+    if (b.lo) o = merge_values<CODE>(was[d], o, b.lo, scale > old, old * inv);
     *dst = o;
   }
 }
 
 // The same grid: cells as values into the caller's rows; zeros where the page is not listed.
 template <typename T, int CODE, int DH>
-__global__ __launch_bounds__(256) void read_kernel(PageView v, int64_t layer_off, CellRows c, int blocks) {
+__global__ __launch_bounds__(256) void read_kernel(RowsArg c) {
   using M = RowMap<T, DH>;
   __shared__ __align__(16) uint8_t lds[4 * M::kBytes];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int job = blockIdx.x * 4 + wave, hw = job / blocks, head = hw >> 1, which = hw & 1;
-  if (head >= v.n_kv) return;
-  const BlockRows b = block_rows(v, c, job % blocks, blockIdx.y);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const BlockRows b = block_rows(c, wave, blockIdx.y);
   if (!b.any) return;
-  const int64_t stride = which ? c.v_stride : c.k_stride;
-  const bool listed = (unsigned)b.page < (unsigned)v.n_pages;
-  const BlockAt at = block_at(v, layer_off, listed ? b.page : 0, which, head, b.cell);
+  const int64_t stride = 8ll * (b.which ? c.v_stride8 : c.k_stride8);
+  const bool listed = (unsigned)b.page < (unsigned)c.n_pages;
+  const BlockAt at = block_at<DH>(c, b, listed ? b.page : 0);
   const float held = *at.scale, scale = listed ? held : 0.f;
   const int unit = lane % M::UPR, cell0 = lane / M::UPR * M::C;
-  T* dst = static_cast<T*>(which ? c.v : c.k) + head * DH + unit * M::E;
+  T* dst = static_cast<T*>(b.which ? c.v : c.k) + b.head * DH + unit * M::E;
   uint32_t w[M::C][M::E / 4];  // codes of the lane's dims, cell by cell
-  if (which == 0) {
+  if (b.which == 0) {
 #pragma unroll
     for (int p = 0; p < M::C; ++p) {
       const uint32_t* src = reinterpret_cast<const uint32_t*>(at.codes + (cell0 + p) * DH + unit * M::E);
@@ -287,7 +316,7 @@ __global__ __launch_bounds__(256) void read_kernel(PageView v, int64_t layer_off
 #pragma unroll
     for (int d = 0; d < M::D; ++d) {
       const int dim = lane + 64 * d;
-      *reinterpret_cast<uint4*>(mine + M::at(dim)) = *reinterpret_cast<const uint4*>(at.codes + (dim << v.shift));
+      *reinterpret_cast<uint4*>(mine + M::at(dim)) = *reinterpret_cast<const uint4*>(at.codes + (dim << c.shift));
     }
     wave_lds_sync();
 #pragma unroll
@@ -803,10 +832,14 @@ hipError_t launch_attn(const PageView& v, int64_t layer_off, const PagedAttn& a,
     }                                                                                                    \
   } while (0)
 
-// The most blocks that a sequence's cells are in.
-int row_blocks(const CellRows& c) { return (c.max_cells + kBlockCells - 2) / kBlockCells + 1; }
+RowsArg rows_arg(const PageView& v, int layer, const CellRows& c) {
+  return RowsArg{v.base + v.layer() * layer, v.page(), c.table, c.first, c.rows, c.k, c.v,
+                 (uint32_t)(c.k_stride / 8), (uint32_t)(c.v_stride / 8), (int32_t)c.table_stride, c.max_pages,
+                 v.n_pages, c.n_rows, c.max_cells, (uint16_t)v.shift, (uint16_t)(2 * v.n_kv)};
+}
 dim3 rows_grid(const PageView& v, const CellRows& c) {
-  return dim3((unsigned)(((int64_t)row_blocks(c) * 2 * v.n_kv + 3) / 4), c.n);
+  const int64_t blocks = (c.max_cells + kBlockCells - 2) / kBlockCells + 1;
+  return dim3((unsigned)((blocks * 2 * v.n_kv + 3) / 4), c.n);
 }
 
 }  // namespace
@@ -851,16 +884,16 @@ hipError_t code_epilogue(const Shape& s, const StepView& sv, int n_rows, int lay
 }
 
 hipError_t code_write(const PageView& v, int layer, const CellRows& c, hipStream_t st) {
-  const int64_t off = v.layer() * layer;
-#define SPP_WRITE(T, C, D, W) SPP_LAUNCH((write_kernel<T, C, D>), rows_grid(v, c), dim3(256), 0, st, v, off, c, row_blocks(c))
+  const RowsArg arg = rows_arg(v, layer, c);
+#define SPP_WRITE(T, C, D, W) SPP_LAUNCH((write_kernel<T, C, D>), rows_grid(v, c), dim3(256), 0, st, arg)
   SPP_CODES(SPP_WRITE, c.bf16, 0);
 #undef SPP_WRITE
   return hipGetLastError();
 }
 
 hipError_t code_read(const PageView& v, int layer, const CellRows& c, hipStream_t st) {
-  const int64_t off = v.layer() * layer;
-#define SPP_READ(T, C, D, W) SPP_LAUNCH((read_kernel<T, C, D>), rows_grid(v, c), dim3(256), 0, st, v, off, c, row_blocks(c))
+  const RowsArg arg = rows_arg(v, layer, c);
+#define SPP_READ(T, C, D, W) SPP_LAUNCH((read_kernel<T, C, D>), rows_grid(v, c), dim3(256), 0, st, arg)
   SPP_CODES(SPP_READ, c.bf16, 0);
 #undef SPP_READ
   return hipGetLastError();
