@@ -25,9 +25,10 @@ namespace spp {
 namespace {
 
 constexpr int kTpb = 256;
-constexpr int kMergeTpb = 512;                  // of the merge, whose steps wait for each other
+constexpr int kMergeTpb = 1024;                 // of the merge: few instructions a thread between its waits
 constexpr int kList = 1024;                     // entries of the list of alternatives, and groups they are in
-constexpr int kHeld = 16;                       // groups a thread of the merge keeps in registers
+constexpr int kHeld = 8;                        // groups a thread of the merge keeps in registers,
+constexpr int kNear = 5;                        // of which the last three are of rows over 163840 tokens
 constexpr int kGroup = 32;                      // tokens of a group: 8 units
 constexpr int kRows = 96;                       // rows of a launch, within 4 KB of arguments
 template <int R>
@@ -84,21 +85,29 @@ __device__ __forceinline__ uint32_t wave_floor(uint32_t u, uint32_t hi, int c) {
   return lo;
 }
 
-// A number that `top` of the workgroup's threads' values reach, W waves: the least of the waves' floors of
-// a Wth of them, or, where a wave has too few (a mask, or the row's end), the largest of their floors of all,
-// or the lowest number.  All of the workgroup; `lds` 2 W words.
+// A number that `top` of the workgroup's threads' values reach, W <= 16 waves: with c a Wth of `top`, what
+// top / c of the waves' floors of c reach, or, where so many waves have too few values (a mask, or the row's
+// end), the largest of their floors of `top`, or the lowest number.  All of the workgroup; `lds` 2 W words.
 template <int W>
 __device__ __forceinline__ float workgroup_floor(float mine, float wave_most, int top, uint32_t* lds) {
-  const int wave = threadIdx.x >> 6, c = (top + W - 1) / W;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int c = (top + W - 1) / W, need = (top + c - 1) / c;
   const uint32_t u = ordered(mine), hi = ordered(wave_most), f = c == 1 ? hi : wave_floor(u, hi, c);
-  if ((threadIdx.x & 63) == 0) lds[wave] = f;
+  if (lane == 0) lds[wave] = f;
   __syncthreads();
-  uint32_t floor = lds[0];
+  // the floor that has need - 1 others above it (equal ones in order)
+  const uint32_t own = lds[lane % W];
+  int above = 0;
 #pragma unroll
-  for (int k = 1; k < W; ++k) floor = min(floor, lds[k]);
+  for (int k = 0; k < W; ++k) {
+    const uint32_t o = lds[k];
+    above += o > own || (o == own && k < lane % W);
+  }
+  const int at = __ffsll((unsigned long long)__ballot(above == need - 1)) - 1;
+  uint32_t floor = (uint32_t)__builtin_amdgcn_readlane((int)own, at);
   if (floor == 0) {
     const uint32_t g = wave_floor(u, hi, top);
-    if ((threadIdx.x & 63) == 0) lds[W + wave] = g;
+    if (lane == 0) lds[W + wave] = g;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < W; ++k) floor = max(floor, lds[W + k]);
@@ -484,18 +493,14 @@ __global__ __launch_bounds__(kMergeTpb) void logprob_merge_kernel(int V, Logprob
   // All loads go out together: a slice and a token a thread, and the groups' largest values.
   Sums own{-INFINITY, 0.f, 0.f};
   if (tid < slices) own = parts[tid];
+  const bool more = n_groups > kNear * kMergeTpb;
   float held[kHeld], mine = -INFINITY;
   if (top > 0) {
 #pragma unroll
-    for (int h = 0; h < kHeld; h += 8) {
-      if (h * kMergeTpb < n_groups) {
+    for (int j = 0; j < kNear; ++j) held[j] = maxima[min(j * kMergeTpb + tid, n_groups - 1)];
+    if (more)
 #pragma unroll
-        for (int j = h; j < h + 8; ++j) held[j] = maxima[min(j * kMergeTpb + tid, n_groups - 1)];
-      } else {
-#pragma unroll
-        for (int j = h; j < h + 8; ++j) held[j] = -INFINITY;
-      }
-    }
+      for (int j = kNear; j < kHeld; ++j) held[j] = maxima[min(j * kMergeTpb + tid, n_groups - 1)];
   }
   const Given given = first_given(job, V);
   if (tid < 4) count[tid] = 0;
@@ -506,11 +511,15 @@ __global__ __launch_bounds__(kMergeTpb) void logprob_merge_kernel(int V, Logprob
   if (lane == 0) red[wave] = wm;
   float least = 0.f;
   if (top > 0) {
+    auto most_of = [&](int h, int to) {
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j) {
-      held[j] = j * kMergeTpb + tid < n_groups ? held[j] : -INFINITY;
-      mine = fmaxf(mine, held[j]);
-    }
+      for (int j = h; j < to; ++j) {
+        held[j] = j * kMergeTpb + tid < n_groups ? held[j] : -INFINITY;
+        mine = fmaxf(mine, held[j]);
+      }
+    };
+    most_of(0, kNear);
+    if (more) most_of(kNear, kHeld);
     for (int g = kHeld * kMergeTpb + tid; g < n_groups; g += kMergeTpb) mine = fmaxf(mine, maxima[g]);
     least = workgroup_floor<W>(mine, wave_max_all(mine), top, floors);
   } else {
@@ -527,9 +536,13 @@ __global__ __launch_bounds__(kMergeTpb) void logprob_merge_kernel(int V, Logprob
   a.t = wave_sum_all(a.t);
   if (lane == 0) red_r[wave] = a.r, red_t[wave] = a.t;
   if (top > 0) {
-    append<kHeld>(
+    append<kNear>(
         count + 1, kList, [&](int j) { return held[j] >= least; },
         [&](int j, int at) { groups[at] = j * kMergeTpb + tid; });
+    if (more)
+      append<kHeld - kNear>(
+          count + 1, kList, [&](int j) { return held[kNear + j] >= least; },
+          [&](int j, int at) { groups[at] = (kNear + j) * kMergeTpb + tid; });
     for (int g0 = kHeld * kMergeTpb; g0 < n_groups; g0 += kMergeTpb) {
       const int g = g0 + tid;
       const float v = g < n_groups ? maxima[g] : -INFINITY;
@@ -541,18 +554,13 @@ __global__ __launch_bounds__(kMergeTpb) void logprob_merge_kernel(int V, Logprob
   const RowUnits row(job.logits, V);
   const int n = top > 0 ? 8 * min(count[1], kList + 1) : 0;  // units of the groups
   const bool listed = n <= 8 * kList;
-  constexpr int AHEAD = 2;
-  float x[AHEAD][4];
-  int t[AHEAD];
-  auto units_at = [&](int i0) {
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      const int i = i0 + k * kMergeTpb + tid;
-      t[k] = i < n ? group_token<UNITS>(row.a, groups[min(i, n - 1) >> 3], i & 7) : V;
-      row.load_long(t[k], x[k]);
-    }
+  float x[4];
+  int t = 0;
+  auto unit_at = [&](int i) {
+    t = i < n ? group_token<UNITS>(row.a, groups[min(i, n - 1) >> 3], i & 7) : V;
+    row.load_long(t, x);
   };
-  if (top > 0 && listed) units_at(0);
+  if (top > 0 && listed) unit_at(tid);
   a.r = red_r[0];
   a.t = red_t[0];
 #pragma unroll
@@ -589,11 +597,11 @@ __global__ __launch_bounds__(kMergeTpb) void logprob_merge_kernel(int V, Logprob
   const RowLog log = finish_sums(job, blockIdx.x, V, a, given, out);
   if (top == 0) return;
   if (listed) {
-    for (int i0 = 0; i0 < n; i0 += AHEAD * kMergeTpb) {
-      append<4 * AHEAD>(
-          count, kList, [&](int j) { return x[j / 4][j % 4] >= least; },
-          [&](int j, int at) { list[at] = entry(ordered(x[j / 4][j % 4]), t[j / 4] + j % 4); });
-      if (i0 + AHEAD * kMergeTpb < n) units_at(i0 + AHEAD * kMergeTpb);
+    for (int i0 = 0; i0 < n; i0 += kMergeTpb) {
+      append<4>(
+          count, kList, [&](int j) { return x[j] >= least; },
+          [&](int j, int at) { list[at] = entry(ordered(x[j]), t + j); });
+      if (i0 + kMergeTpb < n) unit_at(i0 + kMergeTpb + tid);
     }
     __syncthreads();
   }
