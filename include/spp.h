@@ -609,13 +609,13 @@ spp_status spp_paged_attention(const spp_paged_attn* a, void* work, size_t work_
  *   code = x / s rounded to the nearest, ties to even,   Q = 127 (I8) or 448 (E4M3).
  * Cells appended to a block that holds cells already (a decode step, spp_paged_write) keep its s
  * at least what it was; where it grows, the codes there are rounded to the new one.  So what a
- * block holds depends on what was written and in which order, and the error of an element is at
- * most s / 2 (I8) or 2^-4 of it and 2^-10 s (E4M3) as it is written, and after any growth less than s (I8), or
- * the same relative to it and 2^-9 s (E4M3).  A block that is given an infinity or a NaN has
- * the scale NaN and reads as NaN from then on, until it is written from its first cell;
- * magnitudes of 2^127 and more may come back infinite.  Cells of a block past the last
- * written one are undefined.  I8 keeps about twice as many bits of cells that are alike in size; E4M3
- * keeps 4 bits of each element of a block whose elements differ by up to 2^14.
+ * block holds depends on what was written and in which order.  The error of an element is at
+ * most s / 2 (I8), or 2^-4 of it and 2^-10 s (E4M3), as it is written, and after any growth less
+ * than s (I8), or 2^-4 of it and 2^-9 s (E4M3): I8 keeps 6 to 7 bits below the block's largest
+ * element, E4M3 keeps 4 bits of each element down to 2^-13 of it.  A block that is given an
+ * infinity or a NaN has the scale NaN and reads as NaN from then on, until it is written from its
+ * first cell; magnitudes of 2^127 and more may come back infinite.  Cells of a block past the
+ * last written one are undefined.
  *
  * All calls of a pool serve such pools too: import and export convert, decode steps append,
  * forks, reserves and compaction copy pages with their scales. */
@@ -654,13 +654,14 @@ typedef struct {
   int64_t v_stride;
 } spp_paged_cells;
 
-/* Quantises rows into cells (k and v are only read).  In the block of a sequence's first new cell, the cells
- * before that one keep their values as described above; the cells past the last new one are undefined
- * afterwards.  Cells whose page is not listed are left out.  No two sequences of a call write
- * into the same block (a spp_seq_reserve gives them pages of their own).  Only launches a kernel on
- * `stream` and may be captured into a graph, whose replays read tables, first, rows, k and v as they
- * are then; it is the caller's to order against the pool's other work, as spp_paged_attention.
- * SPP_E_INVALID_ARG for a null pointer or a value outside what the fields say. */
+/* Quantises rows into cells (k and v are only read).  In the block of a sequence's first new cell,
+ * the cells before that one, which have been written (their scale counts), keep their values as
+ * described above; the cells past the last new one are undefined afterwards.  Cells whose page is
+ * not listed are left out.  No two sequences of a call write into the same block (a
+ * spp_seq_reserve gives them pages of their own).  Only launches a kernel on `stream` and may be
+ * captured into a graph, whose replays read tables, first, rows, k and v as they are then; it is
+ * the caller's to order against the pool's other work, as spp_paged_attention.  SPP_E_INVALID_ARG
+ * for a null pointer or a value outside what the fields say. */
 spp_status spp_paged_write(const spp_paged_cells* a, void* stream);
 /* The cells' values, code times scale, into the rows (exact in bf16, but for what lies beyond its
  * range).  Rows of cells whose page is not listed are zeros; rows that are no cell's stay as they
@@ -734,21 +735,22 @@ typedef struct {
 /* Bytes of workspace that suffice for n rows, and for fewer (0 for bad arguments). */
 size_t spp_logprobs_work_bytes(int32_t n, int32_t vocab, int32_t n_top);
 /* Log probabilities of given tokens over n rows of logits -- those of a resume, a decode step or
- * adjusted ones -- by which continuations of one state are compared, with what tells how sure
- * the model was: per row (each nullable) lse[i], the log of the sum of exp(x), and entropy[i] =
- * -sum p log p in nats; and the n_top (0..SPP_MAX_TOP) most probable tokens, top_tokens and
- * top_logprobs (device, [n][n_top]), in order, of equal logits the lower index first.
- * A logit of -inf has probability 0, log probability -inf, and is no alternative; where fewer than n_top
- * tokens are, the rest are -1 with -inf.  A NaN or +inf makes its row's log probabilities, lse and
- * entropy NaN (alternatives are still in the order of the logits, NaN left out); a row without any
- * logit above -inf has lse -inf, and NaN for its log probabilities and entropy.  Sums are of fp32; the largest logit's own
- * term is kept apart, so a log probability near 0 keeps its relative precision.
- * rows: host array, read during the call.  No result overlaps another or a logit.  The workspace (device, 16-byte
- * aligned) is written before it is read; two calls that may run at once need two.  Every pointer
- * is 4-byte aligned and on the current device.  Only launches kernels on `stream`: it may be
- * captured into a graph, whose replays read logits and tokens as they are then.
- * SPP_E_INVALID_ARG for n outside [0, 2^20], vocab outside [1, 2^24], a null pointer or a value
- * outside what the fields say (then nothing ran). */
+ * adjusted ones -- by which continuations of one state are compared, with what tells how sure the
+ * model was: per row (each nullable) lse[i], the log of the sum of exp(x), and entropy[i] = -sum p
+ * log p in nats; and the n_top (0..SPP_MAX_TOP) most probable tokens, top_tokens and top_logprobs
+ * (device, [n][n_top]), in order, of equal logits the lower index first.
+ * A logit of -inf has probability 0, log probability -inf, and is no alternative; where fewer
+ * than n_top tokens are, the rest are -1 with -inf.  A NaN or +inf makes its row's log
+ * probabilities, lse and entropy NaN (alternatives are still in the order of the logits, NaN left
+ * out); a row without any logit above -inf has lse -inf, and NaN for its log probabilities and
+ * entropy.  Sums are of fp32; the largest logit's own term is kept apart, so a log probability
+ * near 0 keeps its relative precision.
+ * rows: host array, read during the call.  No result overlaps another or a logit.  The workspace
+ * (device, 16-byte aligned) is written before it is read; two calls that may run at once need
+ * two.  Every pointer is 4-byte aligned and on the current device.  Only launches kernels on
+ * `stream`: it may be captured into a graph, whose replays read logits and tokens as they are
+ * then.  SPP_E_INVALID_ARG for n outside [0, 2^20], vocab outside [1, 2^24], a null pointer or a
+ * value outside what the fields say (then nothing ran). */
 spp_status spp_logprobs(int32_t n, int32_t vocab, const spp_logprob_row* rows, int32_t n_top,
                         int32_t* top_tokens, float* top_logprobs, float* lse, float* entropy,
                         void* work, size_t work_bytes, void* stream);

@@ -14,8 +14,13 @@
 // every group of 32 tokens, a 32nd of what it reads, with no work on alternatives of its own; the merge finds the
 // floor, reads again the few groups that reach it, and counts the order of the few values that do.  Ties go to the
 // lower index: an entry of that list is the value's bits, made to order as unsigned integers, above
-// the complement of the index.  (The first form had a list in order from every slice: 64 rows of
-// 128256, with 8 alternatives 11.8 us and 4.6 of merge, with 50 14.2 and 6.1; without any 7.8 and 3.3.)
+// the complement of the index.  (With a list in order from every slice instead: 64 rows of 128256 with 8
+// alternatives 11.8 us and 4.6 of merge, with 50 14.2 and 6.1, one row with 50 6.6 and 77; without any 7.8 and 3.3.)
+//
+// Measured: 64 rows of 128256, 33 MB, read in 8.0 us (4.1 TB/s) and merged in 6.5 with 8 alternatives; 17 rows of
+// 152063, half of each masked, 4.5 and 8.9 with 50; one row 3.1 and 5.9 with 20; one of 4096, one launch, 4.2.  The merge is
+// a chain of waits (two loads, five barriers, a few LDS round trips and 700 instructions a wave: 13000 cycles), and
+// what it waits for is not the fetch of its code: a part run twice in a row takes as long again.
 #include <algorithm>
 
 #include "common.hpp"
@@ -615,8 +620,10 @@ __global__ __launch_bounds__(kMergeTpb) void logprob_merge_kernel(int V, Logprob
   finish_top(blockIdx.x, log, sorted, top, out);
 }
 
-// Tokens of a slice: 8192 where that makes one of a row, which is then done in one launch; else 2048
-// while that makes no more than 1024 workgroups, else 8192.
+// Tokens of a slice: 8192 where that makes one of a row, which is then done in one launch (from a graph, a row of
+// 4096 with 8 alternatives 5.9 us, in two slices 8.1); else 2048 while that makes no more than 1024 workgroups (one
+// row of 128256 with 20 9.1, in slices of 8192 10.0; 8 rows 9.8 and 10.5), else 8192, a quarter of the parts (64 rows
+// with 8 13.3 and 13.6).
 int slice_units(int n, int vocab) {
   return vocab + 3 > 8 * 4 * kTpb && (int64_t)vocab * n <= kShortSliceTokens ? 2 : 8;
 }

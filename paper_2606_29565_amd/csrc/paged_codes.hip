@@ -211,7 +211,10 @@ __device__ __forceinline__ void wave_lds_sync() {
 // Grid (blocks of a sequence, fastest, times K and V of each head, four to a workgroup; sequences), a
 // wave to a block.  Values change from rows of dims to rows of cells in LDS.
 //
-// Bound by memory: 15000 cells of 5 prompts, 8 heads of 128 in bf16, 79 MB.
+// Bound by memory: 12844 cells of 5 prompts, 8 heads of 128, 79 MB from bf16 rows to e4m3 cells in 19.4 us
+// (4.1 TB/s) and back in 16.2; with values loaded a dim or two of all 16 cells a lane and stored as they come 26.9 and
+// 21.2.  One token: what is looked up one after the other (the rows, the page, what the block keeps), 2.7 us and 2.8
+// for one sequence of 4 heads of 64, 5.0 and 3.9 for 64 of 8 heads of 128.
 template <typename T, int CODE, int DH>
 __global__ __launch_bounds__(256) void write_kernel(RowsArg c) {
   using M = RowMap<T, DH>;
@@ -363,6 +366,8 @@ __global__ __launch_bounds__(256) void read_kernel(RowsArg c) {
 // cells, so that whole lines move; a block's largest value is put together over the workgroup.  Only live
 // cells move; the cells of the session past the last stay as they are.  The loads pass the L2 by (they are
 // read once).
+// Bound by memory: 8100 cells of 4 layers of the 8B shape, 199 MB, in 36.5 us (5.5 TB/s) and out in 34.4; with 32
+// bytes of a row of cells to a wave 58 both ways.
 template <typename T, int CODE, int DH, bool TO_PAGES>
 __global__ __launch_bounds__(256) void session_kernel(PageView v, PageList l, int groups, T* kv, int64_t cap,
                                                       int64_t c0, int cells) {
@@ -608,7 +613,14 @@ __device__ __forceinline__ uint4 keep_codes(const uint4& v, int n) {
 //   s_j = scale log2(e) sk q.ck_j,   o = sum_j (p_j sv) cv_j / sum_j p_j.
 // Row r of key tile t stands for key 16 (r / 4) + 4 t + r % 4.  A 16-byte load of a key's row is 16
 // dims, two operands of the 16x16x32 products; the queries are laid out alike.
-// HBM bounds it: a cell is 2 (dh + 1/4) bytes and 4 G dh operations.
+// HBM bounds it: a cell is 2 (dh + 1/4) bytes and 4 G dh operations.  64 sequences of U[1024, 8192] cells, 8
+// heads of 128, 569 MB: 114-117 us, 5.0 TB/s, where bf16 cells take 212-221; three of 32749 in e4m3 43.5 (4.6 TB/s);
+// one of 8192 6.6.  A step is 744 vector instructions, half of them an integer's way to bf16 by fp32, a third of the
+// time.  That is not what it waits for: with both products on operands that cost less (q as integers of two
+// 7-bit parts on 16x16x64 integer products, probabilities and values in fp16) it took 116, and 7.9 for one sequence.
+// Two steps a trip, 204 registers: 156 where this took 127 (both with a graph's own time); three workgroups to a CU 127 and
+// one 125, against 116.  Waves with a stretch of the range each: 151 against 140 in pages of 128 cells, 162 against 147 of
+// 256, 129 against 127 of 64.
 template <int CODE, int DH, bool QLO>
 __global__ __launch_bounds__(64 * kWaves, 2) void code_attn_kernel(PageView v, int64_t layer_off, PagedAttn a,
                                                                 float scale2, int tiles, float* o_part,
@@ -820,17 +832,21 @@ hipError_t launch_attn(const PageView& v, int64_t layer_off, const PagedAttn& a,
   return hipGetLastError();
 }
 
-// Calls F<T, CODE, DH> for the types at hand.
-#define SPP_CODES(F, BF16, ...)                                                                          \
-  do {                                                                                                   \
-    if (v.code == SPP_CELLS_I8) {                                                                        \
-      if (v.dh == 128) { if (BF16) F(bf16_t, SPP_CELLS_I8, 128, __VA_ARGS__); else F(float, SPP_CELLS_I8, 128, __VA_ARGS__); } \
-      else { if (BF16) F(bf16_t, SPP_CELLS_I8, 64, __VA_ARGS__); else F(float, SPP_CELLS_I8, 64, __VA_ARGS__); }               \
-    } else {                                                                                             \
-      if (v.dh == 128) { if (BF16) F(bf16_t, SPP_CELLS_E4M3, 128, __VA_ARGS__); else F(float, SPP_CELLS_E4M3, 128, __VA_ARGS__); } \
-      else { if (BF16) F(bf16_t, SPP_CELLS_E4M3, 64, __VA_ARGS__); else F(float, SPP_CELLS_E4M3, 64, __VA_ARGS__); }               \
-    }                                                                                                    \
-  } while (0)
+template <typename T, int DH>
+hipError_t launch_session(const PageView& v, const PageList& l, void* kv, int64_t cap, int64_t c0, int cells,
+                          bool to_pages, hipStream_t st) {
+  const int groups = (cells + 63) / 64;
+  const dim3 grid(groups * 2 * v.n_kv * v.n_layers), block(256);
+#define SPP_SESSION(C, W) \
+  SPP_LAUNCH((session_kernel<T, C, DH, W>), grid, block, 0, st, v, l, groups, static_cast<T*>(kv), cap, c0, cells)
+  if (v.code == SPP_CELLS_I8) {
+    if (to_pages) SPP_SESSION(SPP_CELLS_I8, true); else SPP_SESSION(SPP_CELLS_I8, false);
+  } else {
+    if (to_pages) SPP_SESSION(SPP_CELLS_E4M3, true); else SPP_SESSION(SPP_CELLS_E4M3, false);
+  }
+#undef SPP_SESSION
+  return hipGetLastError();
+}
 
 RowsArg rows_arg(const PageView& v, int layer, const CellRows& c) {
   return RowsArg{v.base + v.layer() * layer, v.page(), c.table, c.first, c.rows, c.k, c.v,
@@ -840,6 +856,16 @@ RowsArg rows_arg(const PageView& v, int layer, const CellRows& c) {
 dim3 rows_grid(const PageView& v, const CellRows& c) {
   const int64_t blocks = (c.max_cells + kBlockCells - 2) / kBlockCells + 1;
   return dim3((unsigned)((blocks * 2 * v.n_kv + 3) / 4), c.n);
+}
+template <typename T, int CODE, int DH>
+hipError_t launch_write(const PageView& v, int layer, const CellRows& c, hipStream_t st) {
+  SPP_LAUNCH((write_kernel<T, CODE, DH>), rows_grid(v, c), dim3(256), 0, st, rows_arg(v, layer, c));
+  return hipGetLastError();
+}
+template <typename T, int CODE, int DH>
+hipError_t launch_read(const PageView& v, int layer, const CellRows& c, hipStream_t st) {
+  SPP_LAUNCH((read_kernel<T, CODE, DH>), rows_grid(v, c), dim3(256), 0, st, rows_arg(v, layer, c));
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -857,16 +883,11 @@ hipError_t code_attention(const PageView& v, int layer, const PagedAttn& a, int 
 
 hipError_t code_session(const PageView& v, const PageList& l, int n, void* kv, int64_t cap, int64_t c0, int cells,
                         bool to_pages, hipStream_t st) {
-  const int groups = (cells + 4 * kBlockCells - 1) / (4 * kBlockCells);
-  const dim3 grid(groups * 2 * v.n_kv * v.n_layers), block(256);
-#define SPP_SESSION(T, C, D, W) \
-  SPP_LAUNCH((session_kernel<T, C, D, W>), grid, block, 0, st, v, l, groups, static_cast<T*>(kv), cap, c0, cells)
-  if (to_pages)
-    SPP_CODES(SPP_SESSION, v.given == 2, true);
-  else
-    SPP_CODES(SPP_SESSION, v.given == 2, false);
-#undef SPP_SESSION
-  return hipGetLastError();
+  (void)n;  // (the cells say how many pages)
+  if (v.given == 4)  // (fp32 models have heads of 64)
+    return v.dh == 64 ? launch_session<float, 64>(v, l, kv, cap, c0, cells, to_pages, st) : hipErrorInvalidValue;
+  return v.dh == 128 ? launch_session<bf16_t, 128>(v, l, kv, cap, c0, cells, to_pages, st)
+                     : launch_session<bf16_t, 64>(v, l, kv, cap, c0, cells, to_pages, st);
 }
 
 hipError_t code_epilogue(const Shape& s, const StepView& sv, int n_rows, int layer, const PageView& v,
@@ -884,19 +905,21 @@ hipError_t code_epilogue(const Shape& s, const StepView& sv, int n_rows, int lay
 }
 
 hipError_t code_write(const PageView& v, int layer, const CellRows& c, hipStream_t st) {
-  const RowsArg arg = rows_arg(v, layer, c);
-#define SPP_WRITE(T, C, D, W) SPP_LAUNCH((write_kernel<T, C, D>), rows_grid(v, c), dim3(256), 0, st, arg)
-  SPP_CODES(SPP_WRITE, c.bf16, 0);
-#undef SPP_WRITE
-  return hipGetLastError();
+  const bool i8 = v.code == SPP_CELLS_I8;
+  if (v.dh == 128)
+    return c.bf16 ? (i8 ? launch_write<bf16_t, SPP_CELLS_I8, 128> : launch_write<bf16_t, SPP_CELLS_E4M3, 128>)(v, layer, c, st)
+                  : (i8 ? launch_write<float, SPP_CELLS_I8, 128> : launch_write<float, SPP_CELLS_E4M3, 128>)(v, layer, c, st);
+  return c.bf16 ? (i8 ? launch_write<bf16_t, SPP_CELLS_I8, 64> : launch_write<bf16_t, SPP_CELLS_E4M3, 64>)(v, layer, c, st)
+                : (i8 ? launch_write<float, SPP_CELLS_I8, 64> : launch_write<float, SPP_CELLS_E4M3, 64>)(v, layer, c, st);
 }
 
 hipError_t code_read(const PageView& v, int layer, const CellRows& c, hipStream_t st) {
-  const RowsArg arg = rows_arg(v, layer, c);
-#define SPP_READ(T, C, D, W) SPP_LAUNCH((read_kernel<T, C, D>), rows_grid(v, c), dim3(256), 0, st, arg)
-  SPP_CODES(SPP_READ, c.bf16, 0);
-#undef SPP_READ
-  return hipGetLastError();
+  const bool i8 = v.code == SPP_CELLS_I8;
+  if (v.dh == 128)
+    return c.bf16 ? (i8 ? launch_read<bf16_t, SPP_CELLS_I8, 128> : launch_read<bf16_t, SPP_CELLS_E4M3, 128>)(v, layer, c, st)
+                  : (i8 ? launch_read<float, SPP_CELLS_I8, 128> : launch_read<float, SPP_CELLS_E4M3, 128>)(v, layer, c, st);
+  return c.bf16 ? (i8 ? launch_read<bf16_t, SPP_CELLS_I8, 64> : launch_read<bf16_t, SPP_CELLS_E4M3, 64>)(v, layer, c, st)
+                : (i8 ? launch_read<float, SPP_CELLS_I8, 64> : launch_read<float, SPP_CELLS_E4M3, 64>)(v, layer, c, st);
 }
 
 }  // namespace k
