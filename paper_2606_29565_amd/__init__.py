@@ -870,16 +870,17 @@ class PagedCells:
         check(lib().spp_paged_read(self._ref, None), "spp_paged_read")
 
     def _call(self, fn, name, k, v, stream):
-        if k.dtype != self._dtype or v.dtype != self._dtype or k.shape != v.shape or \
-                k.dim() != 3 or k.shape[1:] != self._shape:
-            raise ValueError(f"k and v: {self._dtype} of shape (rows, {self._shape[0]}, {self._shape[1]})")
-        if k.get_device() != self._dev or v.get_device() != self._dev or not self._keep[0].handle:
+        shape, dtype, dev, (heads, dim) = k.shape, self._dtype, self._dev, self._shape
+        if k.dtype != dtype or v.dtype != dtype or v.shape != shape or len(shape) != 3 or \
+                shape[1] != heads or shape[2] != dim:
+            raise ValueError(f"k and v: {dtype} of shape (rows, {heads}, {dim})")
+        if k.get_device() != dev or v.get_device() != dev or not self._keep[0].handle:
             raise ValueError("k and v are on the pool's device, the pool is open")
-        a, row = self._a, self._shape[0] * self._shape[1]
-        a.n_rows = k.shape[0]
+        a, row = self._a, heads * dim
+        a.n_rows = shape[0]
         a.k, a.k_stride = k.data_ptr(), row if k.is_contiguous() else _row_stride(k, "k")
         a.v, a.v_stride = v.data_ptr(), row if v.is_contiguous() else _row_stride(v, "v")
-        rc = fn(self._ref, ctypes.c_void_p(_stream_of(stream, self._dev)))
+        rc = fn(self._ref, ctypes.c_void_p(_stream_of(stream, dev)))
         if rc < 0:
             raise SppError(rc, name)
 
