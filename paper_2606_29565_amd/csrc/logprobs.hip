@@ -31,10 +31,13 @@ namespace {
 
 constexpr int kTpb = 256;
 constexpr int kMergeTpb = 1024;                 // of the merge: few instructions a thread between its waits
-constexpr int kList = 1024;                     // entries of the list of alternatives, and groups they are in
+constexpr int kGroup = 32;                      // tokens of a group: 8 units
+// Entries of the list of alternatives, and groups they are in.  The values of fewer than n_top groups always fit,
+// and more entries than that are of more than n_top groups.
+constexpr int kList = 2048;
+static_assert(kList / kGroup >= SPP_MAX_TOP, "the values of n_top groups");
 constexpr int kHeld = 8;                        // groups a thread of the merge keeps in registers,
 constexpr int kNear = 5;                        // of which the last three are of rows over 163840 tokens
-constexpr int kGroup = 32;                      // tokens of a group: 8 units
 constexpr int kRows = 96;                       // rows of a launch, within 4 KB of arguments
 template <int R>
 struct LogprobBatch {
@@ -255,70 +258,63 @@ __device__ __forceinline__ void finish_top(int64_t row, const RowLog& log, const
   }
 }
 
-// The alternatives of a row in which too many values reach the floor (the same value over and over, as
-// behind a mask's finite fill): the n_top-th largest value exactly, eight bits at a time by how many have
-// them, then what is above it and the first of its equals.  All of the workgroup, a few times over the row.
-__device__ __attribute__((noinline)) void exact_top(const float* src, int V, int top, uint32_t* bins, uint64_t* list, int* count,
-                          uint64_t* sorted) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  uint32_t prefix = 0;  // the value's upper bits so far
-  int need = top;       // of those with these bits, so many are still to be found
-  bool all = false;     // fewer than n_top values at all
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int b = tid; b < 256; b += blockDim.x) bins[b] = 0;
+// Rows in which too many values reach the floor (the same value over and over, as behind a mask's finite
+// fill): the largest number that `top` values reach, bit by bit.  count(u): how many of the wave's values reach
+// u.  All of the workgroup; `lds` 2 W numbers.  (A row of 128256, 20 alternatives: 24 us in all, 46 where the equals
+// begin in its middle; 252 and 556 by bins of eight bits over the whole row.)
+template <int W, typename C>
+__device__ __forceinline__ uint32_t exact_floor(int top, int* lds, C count) {
+  uint32_t v = 0;
+  for (int b = 31; b >= 0; --b) {
+    const uint32_t next = v | 1u << b;
+    const int mine = count(next);
+    int* at = lds + (b & 1) * W;  // (the other half may still be read)
+    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = mine;
     __syncthreads();
-    for (int i0 = 0; i0 < V; i0 += blockDim.x) {
-      const int i = i0 + tid;
-      const uint32_t u = i < V ? ordered(src[i]) : 0u;
-      const bool in = u && (shift == 24 || u >> (shift + 8) == prefix >> (shift + 8));
-      const uint32_t bin = u >> shift & 255u;
-      const uint64_t who = __ballot(in);
-      if (who == 0) continue;
-      // (lanes of one bin, the common case here, add up first)
-      const int lead = __ffsll((unsigned long long)who) - 1;
-      const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)bin, lead);
-      if (__ballot(in && bin == one) == who) {
-        if (lane == lead) atomicAdd(bins + one, (uint32_t)__popcll(who));
-      } else if (in) {
-        atomicAdd(bins + bin, 1u);
-      }
-    }
-    __syncthreads();
-    if (tid == 0) {
-      int b = 255, above = 0;
-      while (b > 0 && above + (int)bins[b] < need) above += bins[b--];
-      count[0] = b;
-      count[1] = need - above;
-      count[2] = b == 0 && above + (int)bins[0] < need;
-    }
-    __syncthreads();
-    prefix |= (uint32_t)count[0] << shift;
-    need = count[1];
-    all = all || count[2] != 0;
-    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int k = 0; k < W; ++k) all += at[k];
+    if (all >= top) v = next;
   }
-  // what is above it (fewer than n_top), then the first of its equals; fewer than n_top at all: each
-  const uint32_t least = all ? 1u : prefix + 1;  // (no value's bits are all ones: that is a NaN)
-  if (tid == 0) count[0] = 0, count[1] = 0;
-  __syncthreads();
-  for (int i = tid; i < V; i += blockDim.x) {
-    const uint32_t u = ordered(src[i]);
-    if (u >= least) list[atomicAdd(count, 1)] = entry(u, i);
-  }
-  for (int i0 = 0; !all && i0 < V && count[1] < need; i0 += 64) {  // (the first wave's, in order)
-    __syncthreads();
-    if (tid < 64) {
-      const int i = i0 + lane, had = count[1];
-      const bool is = i < V && ordered(src[i]) == prefix;
+  return v;
+}
+// The first `need` tokens whose value is v, as entries of the list from `at` on: the row in order, until they
+// are found.  All of the workgroup; `lds` 2 W numbers.
+template <int W>
+__device__ void append_equal(const RowUnits& row, uint32_t v, int need, uint64_t* list, int at, int* lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int had = 0;
+  for (int i0 = 0, k = 0; 4 * i0 - row.a < row.V && had < need; i0 += 64 * W, k ^= 1) {
+    const int t = 4 * (i0 + (int)threadIdx.x) - row.a;
+    float x[4];
+    row.load(t, x);
+    int before = 0, mine = 0, all = 0;  // equals in lanes below, of the lane, of the wave
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool is = ordered(x[e]) == v;
       const uint64_t who = __ballot(is);
-      const int at = had + __popcll(who & ((1ull << lane) - 1));
-      if (is && at < need) list[top - need + at] = entry(prefix, i);
-      if (lane == 0) count[1] = min(need, had + __popcll(who));
+      before += __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+      all += __popcll(who);
+      mine |= is ? 1 << e : 0;
     }
+    if (lane == 0) lds[k * W + wave] = all;  // (the other half may still be read)
     __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      const int n = lds[k * W + j];
+      before += j < wave ? n : 0;
+      total += n;
+    }
+    before += had;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (mine >> e & 1) {
+        if (before < need) list[at + before] = entry(v, t + e);
+        ++before;
+      }
+    had += total;
   }
-  __syncthreads();
-  store_top(list, all ? count[0] : top, top, sorted);
 }
 
 // The slice's tokens into registers.
@@ -443,36 +439,52 @@ __device__ __forceinline__ int group_token(int a, int g, int j) {
 // Grid (rows): a row of one slice, start to end.
 template <int R>
 __global__ __launch_bounds__(kTpb) void logprob_row_kernel(int V, LogprobBatch<R> jobs, int top, LogprobOut out) {
-  constexpr int UNITS = 8;
-  __shared__ Sums wave_sums[4];
-  __shared__ uint32_t floors[8], bins[256];
+  constexpr int UNITS = 8, W = kTpb / 64;
+  __shared__ Sums wave_sums[W];
+  __shared__ uint32_t floors[2 * W];
   __shared__ uint64_t list[kList], sorted[SPP_MAX_TOP];
-  __shared__ int count[4];
+  __shared__ int count, counts[2 * W];
   const spp_logprob_row job = jobs.row[blockIdx.x];
   const RowUnits row(job.logits, V);
   const int tid = threadIdx.x;
   float x[UNITS][4], mine, most;
   load_slice<UNITS>(row, -row.a, x);
   const Given given = first_given(job, V);
-  if (tid == 0) count[0] = 0;
+  if (tid == 0) count = 0;
   const Sums all = slice_sums<UNITS>(x, mine, most, wave_sums);
   if (top > 0) {
-    const float least = workgroup_floor<4>(mine, most, top, floors);  // (NaN and -inf compare false with it)
+    // the values above `least`, or that and more (NaN and -inf compare false)
+    auto list_from = [&](auto above) {
 #pragma unroll
-    for (int u = 0; u < UNITS; u += 2)
-      append<8>(
-          count, kList, [&](int j) { return x[u + j / 4][j % 4] >= least; },
-          [&](int j, int at) {
-            list[at] = entry(ordered(x[u + j / 4][j % 4]), 4 * ((u + j / 4) * kTpb + tid) + j % 4 - row.a);
-          });
-    __syncthreads();
-    const int n = count[0];
-    if (n <= kList) {
-      store_top(list, n, top, sorted);
-    } else {
+      for (int u = 0; u < UNITS; u += 2)
+        append<8>(
+            &count, kList, [&](int j) { return above(x[u + j / 4][j % 4]); },
+            [&](int j, int at) {
+              list[at] = entry(ordered(x[u + j / 4][j % 4]), 4 * ((u + j / 4) * kTpb + tid) + j % 4 - row.a);
+            });
       __syncthreads();
-      exact_top(job.logits, V, top, bins, list, count, sorted);
+    };
+    const float least = workgroup_floor<W>(mine, most, top, floors);
+    list_from([&](float y) { return y >= least; });
+    int n = count;
+    if (n > kList) {
+      const uint32_t v = exact_floor<W>(top, counts, [&](uint32_t u) {
+        int c = 0;
+#pragma unroll
+        for (int k = 0; k < UNITS; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c += __popcll(__ballot(ordered(x[k][e]) >= u));
+        return c;
+      });
+      if (tid == 0) count = 0;
+      __syncthreads();
+      list_from([&](float y) { return ordered(y) > v; });
+      n = count;  // (below top)
+      append_equal<W>(row, v, top - n, list, n, counts);
+      n = top;
+      __syncthreads();
     }
+    store_top(list, n, top, sorted);
     __syncthreads();
   }
   finish_top(blockIdx.x, finish_sums(job, blockIdx.x, V, all, given, out), sorted, top, out);
@@ -486,8 +498,8 @@ __global__ __launch_bounds__(kMergeTpb) void logprob_merge_kernel(int V, Logprob
                                                                   LogprobOut out) {
   constexpr int W = kMergeTpb / 64, GROUPS = UNITS * 4 * kTpb / kGroup;
   __shared__ float red[W], red_r[W], red_t[W];
-  __shared__ int red_p[W], count[4], groups[kList];
-  __shared__ uint32_t floors[2 * W], bins[256];
+  __shared__ int red_p[W], count[2], counts[2 * W], groups[kList];
+  __shared__ uint32_t floors[2 * W];
   __shared__ uint64_t list[kList], sorted[SPP_MAX_TOP];
   const spp_logprob_row job = jobs.row[blockIdx.x];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -508,7 +520,7 @@ __global__ __launch_bounds__(kMergeTpb) void logprob_merge_kernel(int V, Logprob
       for (int j = kNear; j < kHeld; ++j) held[j] = maxima[min(j * kMergeTpb + tid, n_groups - 1)];
   }
   const Given given = first_given(job, V);
-  if (tid < 4) count[tid] = 0;
+  if (tid < 2) count[tid] = 0;
 
   float m = own.m;
   for (int s = tid + kMergeTpb; s < slices; s += kMergeTpb) m = fmaxf(m, parts[s].m);
@@ -540,30 +552,43 @@ __global__ __launch_bounds__(kMergeTpb) void logprob_merge_kernel(int V, Logprob
   a.r = wave_sum_all(a.r);
   a.t = wave_sum_all(a.t);
   if (lane == 0) red_r[wave] = a.r, red_t[wave] = a.t;
-  if (top > 0) {
+  auto groups_from = [&](auto above) {
     append<kNear>(
-        count + 1, kList, [&](int j) { return held[j] >= least; },
+        count + 1, kList, [&](int j) { return above(held[j]); },
         [&](int j, int at) { groups[at] = j * kMergeTpb + tid; });
     if (more)
       append<kHeld - kNear>(
-          count + 1, kList, [&](int j) { return held[kNear + j] >= least; },
+          count + 1, kList, [&](int j) { return above(held[kNear + j]); },
           [&](int j, int at) { groups[at] = (kNear + j) * kMergeTpb + tid; });
     for (int g0 = kHeld * kMergeTpb; g0 < n_groups; g0 += kMergeTpb) {
       const int g = g0 + tid;
-      const float v = g < n_groups ? maxima[g] : -INFINITY;
+      const float y = g < n_groups ? maxima[g] : -INFINITY;
       append<1>(
-          count + 1, kList, [&](int) { return v >= least; }, [&](int, int at) { groups[at] = g; });
+          count + 1, kList, [&](int) { return above(y); }, [&](int, int at) { groups[at] = g; });
     }
+  };
+  if (top > 0) {
+    groups_from([&](float y) { return y >= least; });
   }
   __syncthreads();
   const RowUnits row(job.logits, V);
-  const int n = top > 0 ? 8 * min(count[1], kList + 1) : 0;  // units of the groups
+  int n = top > 0 ? 8 * min(count[1], kList + 1) : 0;  // units of the groups
   const bool listed = n <= 8 * kList;
   float x[4];
   int t = 0;
   auto unit_at = [&](int i) {
     t = i < n ? group_token<UNITS>(row.a, groups[min(i, n - 1) >> 3], i & 7) : V;
     row.load_long(t, x);
+  };
+  // (the first units are on their way already)
+  auto list_from = [&](auto above) {
+    for (int i0 = 0; i0 < n; i0 += kMergeTpb) {
+      append<4>(
+          count, kList, [&](int j) { return above(x[j]); },
+          [&](int j, int at) { list[at] = entry(ordered(x[j]), t + j); });
+      if (i0 + kMergeTpb < n) unit_at(i0 + kMergeTpb + tid);
+    }
+    __syncthreads();
   };
   if (top > 0 && listed) unit_at(tid);
   a.r = red_r[0];
@@ -601,21 +626,37 @@ __global__ __launch_bounds__(kMergeTpb) void logprob_merge_kernel(int V, Logprob
   }
   const RowLog log = finish_sums(job, blockIdx.x, V, a, given, out);
   if (top == 0) return;
-  if (listed) {
-    for (int i0 = 0; i0 < n; i0 += kMergeTpb) {
-      append<4>(
-          count, kList, [&](int j) { return x[j] >= least; },
-          [&](int j, int at) { list[at] = entry(ordered(x[j]), t + j); });
-      if (i0 + kMergeTpb < n) unit_at(i0 + kMergeTpb + tid);
+  if (listed) list_from([&](float y) { return y >= least; });
+  int found = count[0];
+  if (!listed || found > kList) {
+    // The groups' n_top-th largest value exactly: fewer groups are above it, so what they have above it
+    // fits, and where that is not enough the rest are its equals.
+    const uint32_t v = exact_floor<W>(top, counts, [&](uint32_t u) {
+      int c = 0;
+#pragma unroll
+      for (int j = 0; j < kNear; ++j) c += __popcll(__ballot(ordered(held[j]) >= u));
+      if (more)
+#pragma unroll
+        for (int j = kNear; j < kHeld; ++j) c += __popcll(__ballot(ordered(held[j]) >= u));
+      for (int g0 = kHeld * kMergeTpb; g0 < n_groups; g0 += kMergeTpb)
+        c += __popcll(__ballot(g0 + tid < n_groups && ordered(maxima[g0 + tid]) >= u));
+      return c;
+    });
+    if (tid < 2) count[tid] = 0;
+    __syncthreads();
+    groups_from([&](float y) { return ordered(y) > v; });
+    __syncthreads();
+    n = 8 * count[1];
+    if (n > 0) unit_at(tid);
+    list_from([&](float y) { return ordered(y) > v; });
+    found = count[0];
+    if (found < top) {
+      append_equal<W>(row, v, top - found, list, found, counts);
+      found = top;
+      __syncthreads();
     }
-    __syncthreads();
   }
-  if (listed && count[0] <= kList) {
-    store_top(list, count[0], top, sorted);
-  } else {
-    __syncthreads();
-    exact_top(job.logits, V, top, bins, list, count, sorted);
-  }
+  store_top(list, found, top, sorted);
   __syncthreads();
   finish_top(blockIdx.x, log, sorted, top, out);
 }

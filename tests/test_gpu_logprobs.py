@@ -144,6 +144,37 @@ def test_ties_and_rows_of_one_value():
             _check(spp.LogProbs(size, part, top=top)(), part, None, top)
 
 
+@pytest.mark.parametrize("V,offset", [(2500, 1), (8189, 0), (8193, 3), (40003, 2), (128256, 0), (300001, 1)])
+def test_more_equals_than_a_list_holds(V, offset):
+    """Some values above one that most of the row has: none, one or `top` - 1 of them, all in a group of 32 tokens or
+    far apart, the equals from the start, behind what is masked, or every 33rd token; in infinities too."""
+    import torch
+    import paper_2606_29565_amd as spp
+    g = torch.Generator(device="cuda").manual_seed(V)
+    idx = torch.arange(V, device="cuda")
+    for top in (1, 20, 64):
+        rows = []
+        for fill in (0.0, -3.402823466e38, math.inf):
+            for above in sorted({0, 1, top - 1}):
+                for how in range(4):
+                    x = torch.full((V,), fill, device="cuda")
+                    if how == 1:
+                        x[:V * 5 // 8 - 3] = -math.inf
+                    elif how == 2:
+                        x[idx % 33 != 0] = -2.0
+                    if above and fill != math.inf:
+                        at = (torch.arange(above, device="cuda") + V // 3 if how == 3
+                              else torch.randperm(V, device="cuda", generator=g)[:above])
+                        x[at] = 1.0 + torch.rand(above, device="cuda", generator=g)
+                    rows.append(x)
+        buf = torch.empty(len(rows), V + 4, device="cuda")
+        part = buf[:, offset:offset + V]
+        part.copy_(torch.stack(rows))
+        with np.errstate(all="ignore"):
+            _check(spp.LogProbs(V, list(part), top=top)(), part, None, top)
+    log(f"vocab {V}: in order")
+
+
 def test_masked_rows_and_values_that_are_not_finite():
     import torch
     import paper_2606_29565_amd as spp
