@@ -545,8 +545,9 @@ spp_status spp_pool_compact(spp_pool_t pool, void* stream, int32_t* n_moved);
  * it go to dists[i] (host array of device pointers, fp32[vocab] each); n_cells grows by one.
  * Every weight is read once for up to the model's max_sessions (and max_tokens) sequences;
  * more take further passes.  The model has the pool's layers, kv heads, head_dim and dtype (any,
- * where the pool's cells are 8-bit codes) and lives on its device.  Asynchronous on `stream`.  SPP_E_INVALID_ARG for a null pointer,
- * n < 1, a sequence that does not exist or is listed twice, a token outside [0, vocab);
+ * where the pool's cells are 8-bit codes) and lives on its device.  Asynchronous on `stream`.
+ * SPP_E_INVALID_ARG for a null pointer, n < 1, a sequence that does not exist or is listed
+ * twice, a token outside [0, vocab);
  * SPP_E_CAPACITY when the pages run out or a sequence is SPP_MAX_CAPACITY cells long (then
  * nothing ran).  After SPP_E_HIP the sequences of finished passes have grown, the others not. */
 spp_status spp_decode_batch(spp_pool_t pool, spp_model_t model, int32_t n, const int32_t* seqs,
@@ -657,8 +658,9 @@ typedef struct {
 /* Quantises rows into cells (k and v are only read).  In the block of a sequence's first new cell,
  * the cells before that one, which have been written (their scale counts), keep their values as
  * described above; the cells past the last new one are undefined afterwards.  Cells whose page is
- * not listed are left out.  No two sequences of a call write into the same block (a
- * spp_seq_reserve gives them pages of their own).  Only launches a kernel on `stream` and may be
+ * not listed are left out.  No block is written from two places of a call, in two sequences or
+ * through a page that one lists twice (a spp_seq_reserve gives them pages of their own); what such
+ * a block holds afterwards is undefined.  Only launches a kernel on `stream` and may be
  * captured into a graph, whose replays read tables, first, rows, k and v as they are then; it is
  * the caller's to order against the pool's other work, as spp_paged_attention.  SPP_E_INVALID_ARG
  * for a null pointer or a value outside what the fields say. */

@@ -838,7 +838,8 @@ class PagedCells:
     """spp_paged_write and spp_paged_read over fixed tables of a pool of 8-bit codes: rows rows[i] ..
     rows[i + 1] - 1 of k and v, [n_rows][n_kv_heads][head_dim], are the cells first[i] .. of sequence
     i, at most max_cells of each.  table [n][max_pages], first [n] and rows [n + 1] are int32 device
-    tensors whose values may change between calls; the object lives until its calls have finished."""
+    tensors whose values may change between calls; the object lives until its calls have finished and
+    is called by one host thread at a time."""
 
     def __init__(self, pool: PagePool, layer: int, table, first, rows, max_cells: int,
                  io_bf16: bool = True):

@@ -27,8 +27,8 @@ spp_status check_cells(const spp_paged_cells* a, const PageView** view, int* dev
     return fail(SPP_E_INVALID_ARG, "null pointer");
   const int64_t row = (int64_t)v.n_kv * v.dh;
   constexpr int64_t most = 8ll * UINT32_MAX;  // (the kernels' form of a stride)
-  if (a->k_stride < row || a->v_stride < row || a->k_stride > most || a->v_stride > most || a->k_stride % 8 || a->v_stride % 8 || !aligned(a->k, 16) ||
-      !aligned(a->v, 16))
+  const auto bad = [&](int64_t stride) { return stride < row || stride > most || stride % 8; };
+  if (bad(a->k_stride) || bad(a->v_stride) || !aligned(a->k, 16) || !aligned(a->v, 16))
     return fail(SPP_E_INVALID_ARG, "rows of k and v: %lld elements at least, multiples of 8, 16-byte aligned",
                 (long long)row);
   if (a->table_stride < a->max_pages || a->table_stride > INT32_MAX)
