@@ -147,7 +147,19 @@ struct RowsArg {
   uint16_t shift, heads2;        // log2 of a page's cells; kv heads, keys and values apart
 };
 static_assert(sizeof(RowsArg) <= 96, "a short launch");
-__device__ __forceinline__ int row_blocks(int max_cells) { return (max_cells + kBlockCells - 2) / kBlockCells + 1; }
+// A workgroup has the four blocks of 64 cells of one head, so that the rows of V^T that it shares lines of are its
+// own, where sequences are long and a page's rows are not blocks themselves; else any four.  An odd number of such
+// groups to a head: those past the last cell are of other XCDs for each head.  Written and read in groups / by any
+// four, us, 8 heads of 128: pages of 64, 5 sequences of 4096 cells 21.2 and 20.8 / 25.6 and 23.6, 64 of 512 32.7 and
+// 32.0 / 40.3 and 36.6, of 400 26.1 and 25.9 / 29.1 and 29.3, of 300 21.0 and 20.8 / 20.4 and 19.8, of 80 10.3 and 9.5 /
+// 8.1 and 7.4; pages of 16, 64 of 512 33.8 and 34.9 / 31.4 and 31.5.
+__host__ __device__ __forceinline__ int row_span(int max_cells, int shift) {
+  return shift > 4 && max_cells >= 384 ? 64 : kBlockCells;
+}
+__host__ __device__ __forceinline__ int row_blocks(int max_cells, int shift) {
+  const int span = row_span(max_cells, shift), spans = (max_cells + span - 2) / span + 1;
+  return span == kBlockCells ? spans : (spans | 1) * (span / kBlockCells);
+}
 
 // What a wave of a write or a read has: a block of one head's keys or values, and the rows of the
 // caller that are its cells lo .. hi - 1.
@@ -159,7 +171,7 @@ struct BlockRows {
 };
 __device__ __forceinline__ BlockRows block_rows(const RowsArg& c, int wave, int seq) {
   BlockRows r{};
-  const int blocks = row_blocks(c.max_cells), job = (int)blockIdx.x * 4 + wave, hw = job / blocks;
+  const int blocks = row_blocks(c.max_cells, c.shift), job = (int)blockIdx.x * 4 + wave, hw = job / blocks;
   if (hw >= c.heads2) return r;
   r.which = hw & 1;
   r.head = hw >> 1;
@@ -167,8 +179,8 @@ __device__ __forceinline__ BlockRows block_rows(const RowsArg& c, int wave, int 
   if (first < 0 || r0 < 0) return r;
   const int count = min(min(r1 - r0, c.max_cells), (c.max_pages << c.shift) - first);
   if (count <= 0) return r;  // (so first is below 2^30)
-  const int at = (first & -kBlockCells) + kBlockCells * (job % blocks);
-  if (at >= first + count) return r;
+  const int at = (first & -row_span(c.max_cells, c.shift)) + kBlockCells * (job % blocks);
+  if (at >= first + count || at + kBlockCells <= first) return r;
   r.any = true;
   r.page = c.table[(int64_t)seq * c.table_stride + (at >> c.shift)];
   r.cell = at & ((1 << c.shift) - 1);
@@ -211,9 +223,9 @@ __device__ __forceinline__ void wave_lds_sync() {
 // Grid (blocks of a sequence, fastest, times K and V of each head, four to a workgroup; sequences), a
 // wave to a block.  Values change from rows of dims to rows of cells in LDS.
 //
-// Bound by memory: 12844 cells of 5 prompts, 8 heads of 128, 79 MB from bf16 rows to e4m3 cells in 19.4 us
-// (4.1 TB/s) and back in 16.2; with values loaded a dim or two of all 16 cells a lane and stored as they come 26.9 and
-// 21.2.  One token: what is looked up one after the other (the rows, the page, what the block keeps), 2.7 us and 2.8
+// Bound by memory: 12844 cells of 5 prompts, 8 heads of 128, 79 MB from bf16 rows to e4m3 cells in 16.5 us
+// (4.8 TB/s) and back in 14.2 (5.6); 19.4 and 16.2 by any four blocks to a workgroup, and then, with values loaded a dim
+// or two of all 16 cells a lane and stored as they come, 26.9 and 21.2.  One token: what is looked up one after the other (the rows, the page, what the block keeps), 2.7 us and 2.8
 // for one sequence of 4 heads of 64, 5.0 and 3.9 for 64 of 8 heads of 128.
 template <typename T, int CODE, int DH>
 __global__ __launch_bounds__(256) void write_kernel(RowsArg c) {
@@ -854,7 +866,7 @@ RowsArg rows_arg(const PageView& v, int layer, const CellRows& c) {
                  v.n_pages, c.n_rows, c.max_cells, (uint16_t)v.shift, (uint16_t)(2 * v.n_kv)};
 }
 dim3 rows_grid(const PageView& v, const CellRows& c) {
-  const int64_t blocks = (c.max_cells + kBlockCells - 2) / kBlockCells + 1;
+  const int64_t blocks = row_blocks(c.max_cells, v.shift);
   return dim3((unsigned)((blocks * 2 * v.n_kv + 3) / 4), c.n);
 }
 template <typename T, int CODE, int DH>

@@ -130,6 +130,11 @@ WRITES = [
     (3, 128, "e4m3", False, 128, [[(0, 129)], [(129, 1)], [(130, 100)]]),
     (2, 128, "e4m3", True, 256, [[(250, 20), (0, 1)], [(270, 2), (1, 1)]]),
     (5, 64, "e4m3", True, 64, [[(0, 1)] * 9, [(1, 1)] * 9, [(2, 1)] * 9]),
+    # long spans that start and end anywhere in 64 cells
+    (2, 64, "i8", True, 16, [[(0, 50), (0, 63)], [(50, 65), (63, 66)], [(115, 64), (129, 127)], [(179, 1), (256, 129)]]),
+    (3, 128, "e4m3", False, 32, [[(47, 385), (0, 0), (63, 386)], [(432, 384), (63, 3), (449, 66)]]),
+    (1, 64, "e4m3", True, 64, [[(63, 386)], [(449, 450)], [(899, 384)]]),
+    (2, 64, "i8", True, 256, [[(0, 383), (0, 384)], [(383, 130), (384, 641)]]),
 ]
 
 
