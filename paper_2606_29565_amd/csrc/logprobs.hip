@@ -24,6 +24,7 @@
 #include <algorithm>
 
 #include "common.hpp"
+#include "floors.hpp"
 #include "paged.hpp"
 
 namespace spp {
@@ -78,19 +79,13 @@ __device__ __forceinline__ float unordered(uint32_t u) {
 }
 __device__ __forceinline__ uint64_t entry(uint32_t u, int index) { return (uint64_t)u << 32 | (uint32_t)~index; }
 
-// A number that c lanes of the wave reach, at most 2^17 numbers below the largest such; hi: the wave's
-// largest.  (0: so many have no value.)
+// A number that c lanes of the wave reach, and of values that differ few more, whatever their size and spread (0: so many
+// have no value); hi: the wave's largest.
 __device__ __forceinline__ uint32_t wave_floor(uint32_t u, uint32_t hi, int c) {
-  uint32_t lo = (uint32_t)wave_min_all((int)(u ^ 0x80000000u)) ^ 0x80000000u;  // (the order of signed integers)
-  hi = __builtin_amdgcn_readfirstlane(hi);
-  while (hi - lo > 0x20000u) {
-    const uint32_t mid = lo + (hi - lo) / 2;
-    if (__popcll(__ballot(u >= mid)) >= c)
-      lo = mid;
-    else
-      hi = mid;
-  }
-  return lo;
+  if (__popcll(__ballot(u != 0)) < c) return 0;
+  const int least = wave_min_all((int)((u ? u : ~0u) ^ 0x80000000u));  // (the order of signed integers)
+  return narrow_floor((uint32_t)least ^ 0x80000000u, __builtin_amdgcn_readfirstlane(hi), c,
+                      [&](uint32_t m) { return __popcll(__ballot(u >= m)); });
 }
 
 // A number that `top` of the workgroup's threads' values reach, W <= 16 waves: with c a Wth of `top`, what
