@@ -646,7 +646,8 @@ typedef struct {
   const int32_t* first;      /* device, [n_seqs]                                          */
   const int32_t* rows;       /* device, [n_seqs + 1]                                      */
   int32_t n_rows;            /* rows of k and v, >= 0                                     */
-  int32_t max_cells;         /* most cells of a sequence, 1..2^24; times n_kv_heads <= 2^33 */
+  int32_t max_cells;         /* most cells of a sequence, 1..2^24; times n_kv_heads at most
+                                63 * 2^23                                                 */
   int32_t io_dtype;          /* spp_dtype of k and v                                      */
   void* k;                   /* device, [n_rows] rows of [n_kv_heads][head_dim]           */
   int64_t k_stride;          /* elements between rows, a multiple of 8 below 2^35; k 16-byte

@@ -19,8 +19,9 @@ spp_status check_cells(const spp_paged_cells* a, const PageView** view, int* dev
     return fail(SPP_E_INVALID_ARG, "max_pages < 1 or over 2^30 cells");
   if (a->max_cells < 1 || a->max_cells > (1 << 24)) return fail(SPP_E_INVALID_ARG, "max_cells outside [1, 2^24]");
   if (a->io_dtype != SPP_DTYPE_BF16 && a->io_dtype != SPP_DTYPE_F32) return fail(SPP_E_INVALID_ARG, "io_dtype");
-  if (v.n_kv > 32767 || (int64_t)a->max_cells * v.n_kv > 1ll << 33)
-    return fail(SPP_E_INVALID_ARG, "%d kv heads (at most 32767, times max_cells at most 2^33)", v.n_kv);
+  // (a launch has fewer than 2^32 threads along the blocks, 128 for each of a head: row_workgroups)
+  if (v.n_kv > 32767 || (int64_t)a->max_cells * v.n_kv > 63ll << 23)
+    return fail(SPP_E_INVALID_ARG, "%d kv heads (at most 32767, times max_cells at most 63 * 2^23)", v.n_kv);
   if (a->n_rows < 0) return fail(SPP_E_INVALID_ARG, "n_rows < 0");
   if (a->n_seqs == 0) return SPP_OK;
   if (!a->table || !a->first || !a->rows || (a->n_rows && (!a->k || !a->v)))

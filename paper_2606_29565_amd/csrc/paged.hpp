@@ -58,6 +58,25 @@ struct CellRows {
   int64_t v_stride;
 };
 
+// A workgroup has the four blocks of 64 cells of one head, so that the rows of V^T that it shares lines of are its
+// own, where sequences are long and a page's rows are not blocks themselves; else any four.  An odd number of such
+// groups to a head: those past the last cell are of other XCDs for each head.  Written and read in groups / by any
+// four, us, 8 heads of 128: pages of 64, 5 sequences of 4096 cells 21.2 and 20.8 / 25.6 and 23.6, 64 of 512 32.7 and
+// 32.0 / 40.3 and 36.6, of 400 26.1 and 25.9 / 29.1 and 29.3, of 300 21.0 and 20.8 / 20.4 and 19.8, of 80 10.3 and 9.5 /
+// 8.1 and 7.4; pages of 16, 64 of 512 33.8 and 34.9 / 31.4 and 31.5 (the last three with even numbers of groups too,
+// in an order turned by one for each head).
+__host__ __device__ inline int row_span(int max_cells, int shift) {
+  return shift > 4 && max_cells >= 384 ? 64 : kBlockCells;
+}
+__host__ __device__ inline int row_blocks(int max_cells, int shift) {
+  const int span = row_span(max_cells, shift), spans = (max_cells + span - 2) / span + 1;
+  return span == kBlockCells ? spans : (spans | 1) * (span / kBlockCells);
+}
+// Workgroups of a write or a read for each of its sequences: two sides of every head's blocks, four to one.
+inline int64_t row_workgroups(const PageView& v, int max_cells) {
+  return (2ll * v.n_kv * row_blocks(max_cells, v.shift) + 3) / 4;
+}
+
 // Keys of a step of a wave of the attention over 8-bit codes.
 constexpr int kCodeStep = 64;
 

@@ -147,21 +147,6 @@ struct RowsArg {
   uint16_t shift, heads2;        // log2 of a page's cells; kv heads, keys and values apart
 };
 static_assert(sizeof(RowsArg) <= 96, "a short launch");
-// A workgroup has the four blocks of 64 cells of one head, so that the rows of V^T that it shares lines of are its
-// own, where sequences are long and a page's rows are not blocks themselves; else any four.  An odd number of such
-// groups to a head: those past the last cell are of other XCDs for each head.  Written and read in groups / by any
-// four, us, 8 heads of 128: pages of 64, 5 sequences of 4096 cells 21.2 and 20.8 / 25.6 and 23.6, 64 of 512 32.7 and
-// 32.0 / 40.3 and 36.6, of 400 26.1 and 25.9 / 29.1 and 29.3, of 300 21.0 and 20.8 / 20.4 and 19.8, of 80 10.3 and 9.5 /
-// 8.1 and 7.4; pages of 16, 64 of 512 33.8 and 34.9 / 31.4 and 31.5 (the last three with even numbers of groups too,
-// in an order turned by one for each head).
-__host__ __device__ __forceinline__ int row_span(int max_cells, int shift) {
-  return shift > 4 && max_cells >= 384 ? 64 : kBlockCells;
-}
-__host__ __device__ __forceinline__ int row_blocks(int max_cells, int shift) {
-  const int span = row_span(max_cells, shift), spans = (max_cells + span - 2) / span + 1;
-  return span == kBlockCells ? spans : (spans | 1) * (span / kBlockCells);
-}
-
 // What a wave of a write or a read has: a block of one head's keys or values, and the rows of the
 // caller that are its cells lo .. hi - 1.
 struct BlockRows {
@@ -866,10 +851,7 @@ RowsArg rows_arg(const PageView& v, int layer, const CellRows& c) {
                  (uint32_t)(c.k_stride / 8), (uint32_t)(c.v_stride / 8), (int32_t)c.table_stride, c.max_pages,
                  v.n_pages, c.n_rows, c.max_cells, (uint16_t)v.shift, (uint16_t)(2 * v.n_kv)};
 }
-dim3 rows_grid(const PageView& v, const CellRows& c) {
-  const int64_t blocks = row_blocks(c.max_cells, v.shift);
-  return dim3((unsigned)((blocks * 2 * v.n_kv + 3) / 4), c.n);
-}
+dim3 rows_grid(const PageView& v, const CellRows& c) { return dim3((unsigned)row_workgroups(v, c.max_cells), c.n); }
 template <typename T, int CODE, int DH>
 hipError_t launch_write(const PageView& v, int layer, const CellRows& c, hipStream_t st) {
   SPP_LAUNCH((write_kernel<T, CODE, DH>), rows_grid(v, c), dim3(256), 0, st, rows_arg(v, layer, c));
