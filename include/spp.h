@@ -747,7 +747,8 @@ size_t spp_logprobs_work_bytes(int32_t n, int32_t vocab, int32_t n_top);
  * probabilities, lse and entropy NaN (alternatives are still in the order of the logits, NaN left
  * out); a row without any logit above -inf has lse -inf, and NaN for its log probabilities and
  * entropy.  Sums are of fp32; the largest logit's own term is kept apart, so a log probability
- * near 0 keeps its relative precision.
+ * near 0 keeps its relative precision, but for terms below 2^-126 of the largest (logits over 87 below
+ * it), which may be lost.
  * rows: host array, read during the call.  No result overlaps another or a logit.  The workspace
  * (device, 16-byte aligned) is written before it is read; two calls that may run at once need
  * two.  Every pointer is 4-byte aligned and on the current device.  Only launches kernels on

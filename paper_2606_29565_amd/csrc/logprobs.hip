@@ -4,7 +4,7 @@
 //   log p_t = (x_t - m) - log(1 + R),  H = log(1 + R) - (sum e^(x - m) (x - m)) / (1 + R)
 // The largest logit is left out of R (one of them, where there are several) so that nothing
 // cancels: a token of probability near one keeps the relative precision of its log probability, and H is a sum
-// of terms of one sign.
+// of terms of one sign.  (Terms below 2^-126, the smallest normal number, may be lost.)
 //
 // Bound by memory: a row is read once, into registers, a slice of it to a workgroup; a second launch puts
 // the slices together (a row of one slice is done in the first).
