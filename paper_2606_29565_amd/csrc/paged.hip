@@ -503,9 +503,11 @@ hipError_t paged_join(const PageView& v, const PagedAttn& a, int splits, int uni
 //    cells, 4 heads of 64 in fp32: 6.5 us, in two ranges 7.7), and one of four where
 //    the sequences and heads are 128 workgroups already (32 sequences of 1000 cells, 8 heads of
 //    128 in bf16, 256 workgroups: 27.8 us, in four ranges 32.9; 16 of them 19.1 and 17.4, of 700
-//    cells 14.5 and 16.0; one of them 17.7 and 9.8).  Of 8-bit codes, whose steps are shorter, one range of three
-//    steps (through the binding: 37 sequences of 700 cells, 2 heads of 64, 6.6 us, in three ranges 8.1; one of 768, 8
-//    heads of 128, 9.5 and 9.1; of four steps 7.9 and 9.0, 11.3 and 9.2).
+//    cells 14.5 and 16.0; one of them 17.7 and 9.8).  Of 8-bit codes, whose steps are shorter,
+//    one range of three steps as well where heads are 64, half the bytes a step: i8, from a graph, 1 / 8 / 64 sequences
+//    of 600 cells, 2 heads of 64, 6.3 / 6.4 / 6.5 us, in three ranges 6.5 / 6.7 / 8.0 (e4m3 5.6 / 5.7 / 5.9 and 6.2 / 6.4 / 7.4);
+//    but 8 heads of 128, 1 / 8 / 16 of them 9.3 / 9.5 / 9.6, in three ranges 7.9 / 8.3 / 10.5 (e4m3 8.3 / 8.5 / 8.6 and
+//    7.5 / 7.9 / 9.9).
 //  - Else about 1024 workgroups over all, two rounds of two to a CU (three sequences of 32749
 //    cells, 8 heads of 128: 77 us; aiming at 2048 83, at 4096 89), but up to four ranges of eight
 //    steps or more each, which even out sequences of unequal lengths (64 of U[1024, 8192] cells,
@@ -515,7 +517,7 @@ int paged_splits(const PageView& v, int n, int n_q, int max_pages) {
   const int tiles = (n_q / v.n_kv + 15) / 16;
   const int unit = (v.code ? kCodeStep : v.elem == 2 ? step_keys<bf16_t>() : step_keys<float>()) * kWaves;
   const int64_t most = (((int64_t)max_pages << v.shift) + unit - 1) / unit, wgs = (int64_t)n * v.n_kv * tiles;
-  if (most <= (wgs >= 128 ? 4 : v.code ? 3 : 2)) return 1;
+  if (most <= (wgs >= 128 ? 4 : v.code && v.dh == 64 ? 3 : 2)) return 1;
   const int64_t want = std::max<int64_t>(std::min<int64_t>(4, most / 8), kSplitWorkgroups / wgs);
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, (int64_t)kMaxSplits}));
 }

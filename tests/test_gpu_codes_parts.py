@@ -78,3 +78,35 @@ def test_attention_with_a_bound_for_each_row(nq, nkv, dh, code, io_bf16, page, l
             assert (share <= 1).all(), (m, h, float(share.max()))
             most = max(most, float(share.max()))
     log(f"attention {code} {nq}/{nkv}x{dh}: {most:.2f} of the bound")
+
+
+@pytest.mark.parametrize("nq,nkv,dh,page,cells,ranges", [
+    (32, 8, 128, 64, 512, 1), (32, 8, 128, 64, 513, 3), (32, 8, 128, 64, 768, 3), (32, 8, 128, 256, 1000, 4),
+    (4, 2, 64, 16, 513, 1), (4, 2, 64, 16, 768, 1), (4, 2, 64, 16, 769, 4),
+])
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+def test_a_short_sequence_alone_is_dealt_out_by_its_head_size(code, nq, nkv, dh, page, cells, ranges):
+    """One sequence of three steps of 256 cells: a workgroup for each step of heads of 128, one for all of heads of 64; and
+    what it gives."""
+    import ctypes
+
+    import torch
+    import paper_2606_29565_amd as spp
+    width = -(-cells // page)
+    pool, pages, g = _pool(torch, spp, 1, nkv, dh, code, page, width, seed=cells)
+    if code == "e4m3":
+        for t in _views(torch, pool, pages)[:2]:
+            bits = t.view(torch.uint8)
+            bits[(bits & 0x7F) == 0x7F] = 0x30
+    table = torch.randperm(width, generator=g, device="cuda").view(1, width).int()
+    att = spp.PagedAttention(pool, 0, nq, table, torch.tensor([cells], dtype=torch.int32, device="cuda"), io_bf16=False)
+    nbytes = spp.lib().spp_paged_attention_work_bytes(ctypes.byref(att._a))
+    assert nbytes == (0 if ranges == 1 else nq * ranges * (dh + 2) * 4)
+    q = torch.empty(1, nq, dh, device="cuda").normal_(0, 1.5, generator=g)
+    got = att(q, torch.empty_like(q))[0].double().cpu().numpy()
+    K, V = (t.numpy() for t in _values(torch, pool, pages, 0))
+    at, T = np.arange(cells), table[0].cpu().numpy()
+    for h in range(nq):
+        k1, v1 = (x[T[at // page], h // (nq // nkv), at % page] for x in (K, V))
+        want, off = row(q[0, h].double().cpu().numpy(), k1, v1, 1 / math.sqrt(dh), False)
+        assert (np.abs(got[h] - want) <= off).all(), h
