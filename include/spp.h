@@ -515,7 +515,8 @@ spp_status spp_seq_reserve(spp_pool_t pool, int32_t n, const int32_t* seqs, int3
 /* Declares the next `cells` cells written: n_cells <- n_cells + cells.  SPP_E_STATE unless
  * pages of the sequence's own hold them, as after spp_seq_reserve. */
 spp_status spp_seq_commit(spp_pool_t pool, int32_t seq, int32_t cells);
-/* Discards cells: n_cells <- min(n_cells, n), and gives up the pages past them. */
+/* Discards cells: n_cells <- min(n_cells, n), and gives up the pages past them.  (What a discarded
+ * cell made of its block's scale stays where the pool's cells are 8-bit codes.) */
 spp_status spp_seq_truncate(spp_pool_t pool, int32_t seq, int32_t n);
 
 /* The sequence becomes a copy of the session's committed cells (its former cells are given
@@ -616,7 +617,10 @@ spp_status spp_paged_attention(const spp_paged_attn* a, void* work, size_t work_
  * element, E4M3 keeps 4 bits of each element down to 2^-13 of it.  A block that is given an
  * infinity or a NaN has the scale NaN and reads as NaN from then on, until it is written from its
  * first cell; magnitudes of 2^127 and more may come back infinite.  Cells of a block past the
- * last written one are undefined.
+ * last written one are undefined.  So, unlike in a pool of values, an append (a decode step,
+ * spp_paged_write) writes the scale and the codes of up to 15 earlier cells of its sequence again: what
+ * reads those is ordered against it.  And spp_seq_truncate takes cells away, not what they did to the
+ * block that is cut: a scale that they made larger stays so, one that is NaN stays NaN.
  *
  * All calls of a pool serve such pools too: import and export convert, decode steps append,
  * forks, reserves and compaction copy pages with their scales. */

@@ -17,8 +17,8 @@
 // the complement of the index.  (With a list in order from every slice instead: 64 rows of 128256 with 8
 // alternatives 11.8 us and 4.6 of merge, with 50 14.2 and 6.1, one row with 50 6.6 and 77; without any 7.8 and 3.3.)
 //
-// Measured: 64 rows of 128256, 33 MB, read in 8.0 us (4.1 TB/s) and merged in 6.5 with 8 alternatives; 17 rows of
-// 152063, half of each masked, 4.5 and 8.9 with 50; one row 3.1 and 5.9 with 20; one of 4096, one launch, 4.2.  The merge is
+// Measured: 64 rows of 128256, 33 MB, read in 8.0 us (4.1 TB/s) and merged in 6.7 with 8 alternatives; 17 rows of
+// 152063, half of each masked, 4.7 and 9.1 with 50; one row 3.1 and 6.0 with 20; one of 4096, one launch, 4.2.  The merge is
 // a chain of waits (two loads, five barriers, a few LDS round trips and 700 instructions a wave: 13000 cycles), and
 // what it waits for is not the fetch of its code: a part run twice in a row takes as long again.
 #include <algorithm>

@@ -211,8 +211,9 @@ __device__ __forceinline__ void wave_lds_sync() {
 //
 // Bound by memory: 12844 cells of 5 prompts, 8 heads of 128, 79 MB from bf16 rows to e4m3 cells in 16.5 us
 // (4.8 TB/s) and back in 14.2 (5.6); 19.4 and 16.2 by any four blocks to a workgroup, and then, with values loaded a dim
-// or two of all 16 cells a lane and stored as they come, 26.9 and 21.2.  One token: what is looked up one after the other (the rows, the page, what the block keeps), 2.7 us and 2.8
-// for one sequence of 4 heads of 64, 5.0 and 3.9 for 64 of 8 heads of 128.
+// or two of all 16 cells a lane and stored as they come, 26.9 and 21.2.  fp32 rows, 131 MB, 25.3 (5.2) and 21.4.  One
+// token: what is looked up one after the other (the rows, the page, what the block keeps), 2.7 us and 2.8
+// for one sequence of 4 heads of 64, 5.1 and 4.0 for 64 of 8 heads of 128.
 template <typename T, int CODE, int DH>
 __global__ __launch_bounds__(256) void write_kernel(RowsArg c) {
   using M = RowMap<T, DH>;
@@ -611,6 +612,10 @@ __device__ __forceinline__ uint4 keep_codes(const uint4& v, int n) {
 //   s_j = scale log2(e) sk q.ck_j,   o = sum_j (p_j sv) cv_j / sum_j p_j.
 // Row r of key tile t stands for key 16 (r / 4) + 4 t + r % 4.  A 16-byte load of a key's row is 16
 // dims, two operands of the 16x16x32 products; the queries are laid out alike.
+// Codes are exact in bf16; what multiplies them, p_j sv and queries in fp32, goes in two bf16 parts each, which leave 2^-17
+// of it (one part would leave 2^-8 of a weight, more than a bf16 output's own rounding where values cancel).  Scores, maxima,
+// the sums of p and of the output are fp32.  The query's second part, half as many products again: 121 us against 115 for
+// the 64 sequences below, 7.8 against 6.8 for the one.
 // HBM bounds it: a cell is 2 (dh + 1/4) bytes and 4 G dh operations.  64 sequences of U[1024, 8192] cells, 8
 // heads of 128, 569 MB: 114-117 us, 5.0 TB/s, where bf16 cells take 212-221; three of 32749 in e4m3 43.5 (4.6 TB/s);
 // one of 8192 6.6.  A step is 744 vector instructions, half of them an integer's way to bf16 by fp32, a third of the
